@@ -330,6 +330,102 @@ int kvh_loader_destroy(kvh_loader* loader);
 int kvh_load_static(const kvh_load_item* items, int n_items, kvh_dtype dt, int l, int c, const kvh_kv_view* dst,
                     int block_tokens, int32_t* status_dev, void* stream);
 
+/* ---- Serving cache ----------------------------------------------------------------------------------
+ * What a serving program does with the paged cache that entries are decoded into: keys and values of new tokens are
+ * appended to it, and queries attend over it.  The cache is the paged view of kvh_decode, [layers][pages][block_tokens][c]
+ * with c = heads * head_dim channels, and holds either the 16-bit type of the call (KVH_CACHE_16: the very tensors kvh_decode
+ * writes) or 8-bit codes with one fp32 scale per page and KV head, for K and V apart: the value of a code is code * scale,
+ * the code an int8 (KVH_CACHE_I8, -127 .. 127) or an OCP e4m3 float (KVH_CACHE_E4M3, up to 448).
+ *
+ * A batch holds n_requests requests; the new tokens of request b are the rows starts[b] .. starts[b + 1] - 1 of the packed
+ * tensors, lens[b] counts its tokens in the cache WITH the new ones, and its new token i therefore has the logical position
+ * p = lens[b] - n_b + i, which is row p % block_tokens of page page_table[b][p / block_tokens].  starts, lens and page_table are
+ * int32 arrays in device memory, which the host cannot vet.  What the kernels enforce: a request with n_b < 0 or
+ * > max_new, with rows outside [0, n_tokens), with lens[b] < n_b in kvh_append, with lens[b] < 0 or with more tokens than its row of the table has
+ * pages for is refused as a whole (nothing of it is read or written); a page outside [0, pages) is never accessed: tokens on it
+ * are not stored by kvh_append and not seen by kvh_attention (a query that should see nothing else gets NaN).  Either sets status_dev[b] (if status_dev is not NULL; zeroed
+ * by the caller, one int32 a request) to KVH_DEV_BAD_REQUEST.  Table entries past a request's last page are not read. */
+#define KVH_DEV_BAD_REQUEST 2
+
+typedef enum { KVH_CACHE_16 = 0, KVH_CACHE_I8 = 1, KVH_CACHE_E4M3 = 2 } kvh_cache_kind;
+
+/* Host struct holding device pointers.  Bases 16-byte aligned, channel stride 1, token_stride (elements from one row of a page to
+ * the next, pages dense as for kvh_decode) a multiple of 16 bytes, >= heads * head_dim and < 2^20, layer_stride a multiple of 16
+ * bytes.  head_dim is 64 or 128, heads 1 .. 4096.  Scales (8-bit kinds only, NULL otherwise) are [layers][pages][heads] floats with
+ * the given strides, heads dense. */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t layer_stride, token_stride;            /* elements */
+  int64_t scale_layer_stride, scale_page_stride; /* floats */
+  int32_t layers, pages, block_tokens, heads, head_dim;
+  int32_t kind; /* kvh_cache_kind */
+} kvh_cache;
+
+typedef struct {
+  const int32_t* starts;     /* n_requests + 1 */
+  const int32_t* lens;       /* n_requests */
+  const int32_t* page_table; /* [n_requests][table_pages] */
+  int64_t table_stride;      /* entries from one request's row to the next */
+  int32_t table_pages;
+  int32_t n_requests;        /* 1 .. 65535 */
+  int32_t max_new;           /* no request brings more new tokens; >= 1 */
+  int32_t n_tokens;          /* rows of the packed tensors; 0: nothing is done */
+} kvh_requests;
+
+/* Rows of 16-bit elements, [layers][n_tokens][channels]; strides in elements, multiples of 8; base 16-byte aligned. */
+typedef struct {
+  void* p;
+  int64_t layer_stride, token_stride;
+} kvh_rows;
+
+/* Position rotation of the first `rot` channels of each head by the angles of a table: row `pos` holds the cosines of the rot / 2
+ * angles and then their sines.  pairs == 0: channel i turns with channel i + rot / 2; pairs != 0: channel 2 i with 2 i + 1.  With
+ * (a, b) such a pair: a' = a cos - b sin, b' = b cos + a sin in fp32, each product and sum rounded.  pos is positions[row] (row
+ * of the packed tensors; int32, device memory) or, where positions is NULL, the token's logical position.  A token whose pos lies
+ * outside [0, n_positions) is not stored (KVH_DEV_BAD_REQUEST), nor is its query.  rot is a multiple of 16, at most head_dim. */
+typedef struct {
+  const float* table;
+  const int32_t* positions;
+  int64_t table_stride; /* floats from one position to the next, a multiple of 4 */
+  int32_t n_positions, rot, pairs;
+} kvh_rotation;
+
+/* Append: K rows (rotated) and V rows of all new tokens go into their pages, for every layer of the cache in one launch; q rows
+ * (NULL: none), with q_heads heads of head_dim, are rotated into q_out, which may be q itself.  kv: k, v [layers][n_tokens][c].
+ * rotation NULL: nothing is rotated.
+ * 16 bits: the value rounded to the nearest (what is not rotated is stored as it is).
+ * 8 bits, for K and V of each page and KV head apart: a = the largest |x| among the new tokens on the page;
+ * t = a < 2^-100 ? 0 : a / 127 (e4m3: a / 448); the scale becomes s = max(t, the scale it had), or t where no earlier token is on
+ * the page (what was stored there before is of no account); code = rne(x * (1 / s)), 0 where s is 0.  Where s grew from s0 > 0,
+ * the codes that the page's earlier tokens have become rne(code * (s0 / s)): a page is always described by one scale, and every
+ * growth costs its earlier tokens one more rounding.  Inputs must be finite for 8 bits (anything else gives unspecified codes
+ * and scales on that page and head). New tokens of one call must lie on pages that no other request of the call appends to.
+ * Errors: KVH_E_ARG (null pointer, type, kind, negative stride, count), KVH_E_SHAPE (head_dim, heads, layers, pages,
+ * block_tokens, rot), KVH_E_ALIGN. */
+int kvh_append(const kvh_cache* cache, const kvh_requests* requests, kvh_dtype dt, const kvh_kv_view* kv, const kvh_rows* q,
+               const kvh_rows* q_out, int q_heads, const kvh_rotation* rotation, int32_t* status_dev, void* stream);
+
+/* Attention of the new tokens over one layer of the cache, which holds them already: out_i = sum_j w_ij v_j / sum_j w_ij with
+ * w_ij = exp(scale * q_i . k_j) over the tokens j of the request that query i, at logical position p, sees: j < lens[b]; j <= p
+ * if causal; and, if window > 0, j > p - window or j < sink (the last `window` tokens and the first `sink` ones: what
+ * kvh_encode_kept keeps of an entry).  window needs causal.  q_heads is a multiple of the cache's heads; query head u reads KV head
+ * u / (q_heads / heads).  A query that sees nothing gets zeros, and minus infinity in lse.  lse (nullable): [n_tokens][q_heads]
+ * floats, the natural logarithm of sum_j w_ij.
+ * Precision: products in the matrix cores, sums, maxima and the softmax in fp32; the weights are rounded to 16 bits before they
+ * meet the values.  What a query does not see does not reach its result, whatever it is; infinities and NaN in what it sees do
+ * as in the formula.
+ * workspace_dev: device memory for partial results where few queries meet many tokens and the tokens of a request are split over
+ * the GPU; 16-byte aligned.  kvh_attention_workspace says how much serves a batch best; with less (or none) the call splits
+ * less (or not at all) and is slower.  It needs no preparation, is used by this call alone until it has finished, and keeps
+ * nothing that another call reads. */
+size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim);
+int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q,
+                  const kvh_rows* out, int q_heads, float* lse_dev, float scale, int causal, int sink, int window,
+                  void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream);
+
 /* ---- Storage policy (host only; no device work) -------------------------------------------------------
  * The paper's policy optimizer (Design section): Utility(i) = Freq(i) * (alpha * Quality(i, M_i, R_i) -
  * size(i, M_i, R_i) / Bandwidth); the marginal utility drop of going from rate m to rate n is
@@ -383,7 +479,7 @@ int kvh_stream_probe(void* dst_dev, const void* src_dev, size_t n_units, int rea
 
 /* Timing of one launch, for callers that profile (not part of the codec; Design section, Estimator: the decompression
  * overhead of an entry is something to be measured).  The two events (hipEvent_t, created by the caller with timing
- * enabled) are recorded by the NEXT encode, decode or transcode kernel that this host thread launches through the
+ * enabled) are recorded by the NEXT encode, decode, transcode, append or attention kernel that this host thread launches through the
  * library: `start_event` when that kernel starts executing, `stop_event` when it has finished, on the launch's
  * stream, so that hipEventElapsedTime(start, stop) is the kernel's own duration - what a kernel trace reports -
  * without the queue packets that events recorded around a launch put between neighbouring kernels.  The pair is

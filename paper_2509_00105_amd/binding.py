@@ -25,6 +25,29 @@ class _KVView(ctypes.Structure):
                 ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("scale_layer_stride", ctypes.c_int64), ("scale_page_stride", ctypes.c_int64),
+                ("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("kind", ctypes.c_int32)]
+
+
+class _Requests(ctypes.Structure):
+    _fields_ = [("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("table_pages", ctypes.c_int32), ("n_requests", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("n_positions", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32)]
+
+
 # Device-resident job descriptors, built as structured numpy arrays and uploaded by the caller.
 ENC_ITEM = np.dtype([("blob", "<u8"), ("src_token0", "<i8"), ("n_tokens", "<i4"), ("level", "<i4")], align=True)
 DEC_ITEM = np.dtype([("blob", "<u8"), ("n_tokens", "<i4"), ("level", "<i4"), ("dst_token0", "<i8"),
@@ -100,6 +123,13 @@ def lib() -> ctypes.CDLL:
         L.kvh_loader_destroy.argtypes = [vp]
         L.kvh_load_static.restype = i32
         L.kvh_load_static.argtypes = [vp, i32, i32, i32, i32, view, i32, vp, vp]
+        cache, requests, rows = ctypes.POINTER(_Cache), ctypes.POINTER(_Requests), ctypes.POINTER(_Rows)
+        L.kvh_append.restype = i32
+        L.kvh_append.argtypes = [cache, requests, i32, view, rows, rows, i32, ctypes.POINTER(_Rotation), vp, vp]
+        L.kvh_attention_workspace.restype = sz
+        L.kvh_attention_workspace.argtypes = [i32] * 6
+        L.kvh_attention.restype = i32
+        L.kvh_attention.argtypes = [cache, i32, requests, i32, rows, rows, i32, vp, ctypes.c_float, i32, i32, i32, vp, sz, vp, vp]
         f64 = ctypes.c_double
         L.kvh_policy_utility.restype = f64
         L.kvh_policy_utility.argtypes = [f64] * 5
@@ -545,6 +575,155 @@ class Loader:
             self.close()
         except Exception:
             pass
+
+
+# ---- serving cache ------------------------------------------------------------------------------------------------
+CACHE_16, CACHE_I8, CACHE_E4M3 = 0, 1, 2
+_CODES = {torch.int8: CACHE_I8, torch.float8_e4m3fn: CACHE_E4M3}
+
+
+def _cache(k_cache, v_cache, k_scale, v_scale, head_dim, dtype):
+    """kvh_cache of [l][P][block][c] tensors (codes or the 16-bit type of the call) and [l][P][heads] scales."""
+    _require_cuda(k_cache, v_cache, k_scale, v_scale)
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+        raise ValueError("the K and V caches must be [l][P][block][c] with equal shapes, strides and types")
+    kind = CACHE_16 if k_cache.dtype == dtype else _CODES.get(k_cache.dtype)
+    if kind is None:
+        raise ValueError("the cache must hold the type of the call, int8 or float8_e4m3fn")
+    l, pages, block, c = k_cache.shape
+    if k_cache.stride(3) != 1 or (k_cache.stride(1) != k_cache.stride(2) * block and pages > 1):
+        raise ValueError("channel stride must be 1 and blocks of a paged cache densely packed")
+    if head_dim < 1 or c % head_dim:
+        raise ValueError("c must be a multiple of head_dim")
+    heads, ls, ps = c // head_dim, 0, 0
+    if kind == CACHE_16:
+        if k_scale is not None or v_scale is not None:
+            raise ValueError("a 16-bit cache has no scales")
+    else:
+        for t in (k_scale, v_scale):
+            if t is None or t.dtype != torch.float32 or t.shape != (l, pages, heads) or t.stride() != k_scale.stride():
+                raise ValueError("an 8-bit cache needs float32 scales [l][P][heads] for K and V, of equal strides")
+        if k_scale.stride(2) != 1 and heads > 1:
+            raise ValueError("the heads of a page's scales must be dense")
+        ls, ps = k_scale.stride(0), k_scale.stride(1) if pages > 1 else heads
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), k_cache.stride(0), k_cache.stride(2) if block > 1 or pages > 1 else c,
+                  ls, ps, l, pages, block, heads, head_dim, kind)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory that the call's stream may use at once: the allocator orders what it hands out by the stream it is asked on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _int32(t, name, dim, least=0):
+    if t is not None:
+        _require_cuda(t)
+        if t.dtype != torch.int32 or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1) or t.shape[0] < least:
+            raise ValueError("%s must be a dense int32 tensor of %d dimension(s) with enough entries" % (name, dim))
+
+
+def _requests(starts, lens, page_table, max_new, n_tokens, status):
+    _int32(lens, "lens", 1)
+    n = lens.shape[0]
+    _int32(starts, "starts", 1, n + 1)
+    _int32(page_table, "page_table", 2, n)
+    _int32(status, "status", 1, n)
+    return _Requests(starts.data_ptr(), lens.data_ptr(), page_table.data_ptr(), page_table.stride(0), page_table.shape[1], n, max_new, n_tokens)
+
+
+def _rows(t, layers, n_tokens, head_dim, dtype, name):
+    """kvh_rows of [l][T][heads * head_dim], and its heads."""
+    _require_cuda(t)
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != layers or t.shape[1] != n_tokens or t.shape[2] % head_dim or t.stride(2) != 1:
+        raise ValueError("%s must be [l][T][heads * head_dim] of the call's type, with channel stride 1" % name)
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1) if n_tokens > 1 else max(t.stride(1), t.shape[2])), t.shape[2] // head_dim
+
+
+def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+           page_table: torch.Tensor, max_new: int, head_dim: int = 128, k_scale: torch.Tensor | None = None,
+           v_scale: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+           rotation: torch.Tensor | None = None, positions: torch.Tensor | None = None, pairs: bool = False,
+           status: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """kvh_append: K/V [l][T][c] of the requests' new tokens -> the pages of [l][P][block][c] caches (16-bit, int8 or float8_e4m3fn
+    with scales [l][P][heads]).  K and q [l][T][q_heads * head_dim] are rotated by `rotation`, float32 [positions][rot]: cosines, then sines.
+    Returns q_out (made here if none is given; may be q)."""
+    view, dt = _view(k, v)
+    l, T, c = k.shape
+    cache = _cache(k_cache, v_cache, k_scale, v_scale, head_dim, k.dtype)
+    if (l, c) != (cache.layers, cache.heads * head_dim):
+        raise ValueError("K and V must have the cache's layers and channels")
+    if T <= 1:
+        view.token_stride = max(view.token_stride, c)
+    req = _requests(starts, lens, page_table, max_new, T, status)
+    rows = out = rot = None
+    q_heads = 0
+    if q is not None:
+        if q_out is None:
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
+        rows, q_heads = _rows(q, l, T, head_dim, k.dtype, "q")
+        out, out_heads = _rows(q_out, l, T, head_dim, k.dtype, "q_out")
+        if out_heads != q_heads:
+            raise ValueError("q_out must have the shape of q")
+    if rotation is not None:
+        _require_cuda(rotation)
+        if rotation.dtype != torch.float32 or rotation.dim() != 2 or rotation.stride(1) != 1:
+            raise ValueError("rotation must be float32 [positions][rot], dense in rot")
+        _int32(positions, "positions", 1, T)
+        rot = _Rotation(rotation.data_ptr(), _ptr(positions), rotation.stride(0), rotation.shape[0], rotation.shape[1], int(pairs))
+    elif positions is not None:
+        raise ValueError("positions without a rotation")
+    if q is not None and rotation is None:
+        raise ValueError("q is taken to be rotated: without a rotation it is used as it is")
+    ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    _check(lib().kvh_append(ctypes.byref(cache), ctypes.byref(req), dt, ctypes.byref(view), ref(rows), ref(out), q_heads, ref(rot), _ptr(status),
+                            _stream_ptr(stream)), "kvh_append")
+    return q_out
+
+
+def attention_workspace(n_requests: int, max_new: int, n_tokens: int, heads: int, q_heads: int, head_dim: int = 128) -> int:
+    """kvh_attention_workspace: bytes that serve such a batch best; 0 where the arguments are none of an attention."""
+    return lib().kvh_attention_workspace(n_requests, max_new, n_tokens, heads, q_heads, head_dim)
+
+
+def attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, layer: int, starts: torch.Tensor, lens: torch.Tensor,
+              page_table: torch.Tensor, max_new: int, head_dim: int = 128, k_scale: torch.Tensor | None = None,
+              v_scale: torch.Tensor | None = None, scale: float | None = None, causal: bool = True, sink: int = 0, window: int = 0,
+              out: torch.Tensor | None = None, lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+              status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """kvh_attention: queries [T][q_heads * head_dim] of the requests' new tokens over layer `layer` of the cache they were appended to.
+    scale: head_dim ** -0.5 if not given.  lse: float32 [T][q_heads] or None.  workspace: uint8, kept by programs that call often (see
+    attention_workspace); made here if none is given."""
+    _require_cuda(q, lse, workspace)
+    if q.dtype not in _TORCH_DT:
+        raise ValueError("q must be float16 or bfloat16")
+    if q.dim() != 2:
+        raise ValueError("q must be [T][q_heads * head_dim]")
+    cache = _cache(k_cache, v_cache, k_scale, v_scale, head_dim, q.dtype)
+    T = q.shape[0]
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    rows, q_heads = _rows(q.unsqueeze(0), 1, T, head_dim, q.dtype, "q")
+    to, out_heads = _rows(out.unsqueeze(0), 1, T, head_dim, q.dtype, "out")
+    if out_heads != q_heads:
+        raise ValueError("out must have the shape of q")
+    req = _requests(starts, lens, page_table, max_new, T, status)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (T, q_heads) or not lse.is_contiguous()):
+        raise ValueError("lse must be a dense float32 [T][q_heads]")
+    if workspace is None:
+        workspace = _empty(attention_workspace(req.n_requests, max_new, T, cache.heads, q_heads, head_dim), torch.uint8, q.device, stream)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a dense uint8 tensor")
+    _check(lib().kvh_attention(ctypes.byref(cache), layer, ctypes.byref(req), _TORCH_DT[q.dtype], ctypes.byref(rows), ctypes.byref(to), q_heads, _ptr(lse),
+                               head_dim ** -0.5 if scale is None else scale, int(causal), sink, window, workspace.data_ptr(), workspace.numel(), _ptr(status),
+                               _stream_ptr(stream)), "kvh_attention")
+    return out
 
 
 def policy_utility(freq: float, alpha: float, quality: float, size_bytes: float, bandwidth: float) -> float:

@@ -6,21 +6,25 @@ import shlex
 import shutil
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvh.so")
 CALLS = os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))  # for the interpreter that builds it alone
 SOURCES = ["kvh_api.hip", "kvh_decode.hip", "kvh_encode.hip", "kvh_transcode.hip", "kvh_loader.hip", "kvh_policy.cpp"]
+CACHE_SOURCES = ["kvh_append.hip", "kvh_attention.hip"]  # what reads a caller's cache as it is: NaN and infinities are values there
 
 # -ffp-contract=off: the codec's arithmetic fuses only where the source says fma.
-# -fno-honor-nans: inputs are finite by contract; without it every min/max of a value unpacked with
+# -fno-honor-nans (the codec's sources only): inputs are finite by contract; without it every min/max of a value unpacked with
 # integer ops is preceded by a canonicalising v_max (sNaN quieting).
 # packed-fp32-ops off: hipcc must not form v_pk_*_f32 from the scalar float code.
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off", "-fno-honor-nans",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+CODEC_FLAGS = ["-fno-honor-nans"]
 
 
 def _compile(target: str, cmd: list, verbose: bool) -> None:
@@ -51,7 +55,13 @@ def _build_calls(verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    _compile(LIB, [hipcc, *HIPCC_FLAGS, *[os.path.join(CSRC, s) for s in SOURCES]], verbose)
+    jobs = [(s, CODEC_FLAGS) for s in SOURCES] + [(s, []) for s in CACHE_SOURCES]
+    with tempfile.TemporaryDirectory(prefix="kvh_build_") as work, ThreadPoolExecutor(len(jobs)) as pool:
+        objects = [os.path.join(work, s + ".o") for s, _ in jobs]
+        for done in [pool.submit(_compile, o, [hipcc, *HIPCC_FLAGS, *more, "-c", os.path.join(CSRC, s)], verbose)
+                     for o, (s, more) in zip(objects, jobs)]:
+            done.result()
+        _compile(LIB, [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects], verbose)
     _build_calls(verbose)
     return LIB
 

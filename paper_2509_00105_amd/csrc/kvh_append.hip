@@ -1,0 +1,361 @@
+// kvh_append: keys and values of new tokens go into the pages of the serving cache, keys and queries rotated on the way.
+//
+// A wave takes a unit: one head of K, of V or of q, and some rows of one request.  The rows of a 16-bit cache are independent
+// and come in tiles of 16; an 8-bit page is described by one scale a head, so there the unit is a page: its new rows are read
+// and rotated, their largest magnitude is found across the wave, and they are stored as codes.  A lane holds 8 neighbouring
+// channels (one 16-byte load, one 16- or 8-byte store), D / 8 lanes a row; the other half of a rotated pair is 0 lanes away or
+// rot / 16 lanes, and comes by a lane exchange, which also makes q_out == q safe.
+#include "kvh_cache.hpp"
+
+namespace kvh {
+namespace {
+
+constexpr int kTileRows = 16;
+
+struct AppendParams {
+  Requests req;
+  const uint16_t *k, *v, *q;
+  uint16_t* q_out;
+  int64_t kv_ls, kv_ts, q_ls, q_ts, o_ls, o_ts;  // elements
+  uint8_t *ck, *cv;
+  float *sk, *sv;
+  int64_t c_ls, c_ts;  // elements of the cache
+  int64_t s_ls, s_ps;  // floats
+  int pages, block_tokens, heads, q_heads;
+  const float* table;
+  const int32_t* positions;
+  int64_t table_stride;
+  int n_positions, rot, pairs;  // rot 0: nothing is rotated
+  int32_t* status;
+  uint32_t kv_units, units;  // of a request and layer
+  Divisor by_block, by_kv, by_q;  // block_tokens; 2 heads; q_heads
+};
+
+// One head's rows [i0, i0 + 16) of a request (i < i_end) in registers: D / 8 lanes a row.
+template <int DT, int D>
+struct Tile {
+  static constexpr int kLanes = D / 8;
+  static constexpr int kRows = kWave / kLanes;  // of one access of the wave
+  static constexpr int kSteps = kTileRows / kRows;
+  u32x4 raw[kSteps];
+  float x[kSteps][8];
+  bool valid[kSteps];
+
+  // `turn`: rotate into x; otherwise x is the value itself.  Returns whether a token had no position in the table.
+  __device__ __forceinline__ bool load(const AppendParams& a, const uint16_t* src, int64_t ts, const Request& rq, int i0, int i_end,
+                                       bool turn, int lane) {
+    const int col = lane % kLanes, sub = lane / kLanes;
+    bool bad = false;
+    int pos[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int i = i0 + s * kRows + sub;
+      valid[s] = i < i_end;
+      raw[s] = u32x4{0, 0, 0, 0};
+      pos[s] = 0;
+      if (valid[s]) {
+        raw[s] = *reinterpret_cast<const u32x4*>(src + ((int64_t)rq.start + i) * ts + col * 8);
+        if (turn) {
+          pos[s] = a.positions != nullptr ? a.positions[rq.start + i] : rq.len - rq.n + i;
+          if (pos[s] < 0 || pos[s] >= a.n_positions) {
+            bad = true;
+            valid[s] = false;
+            pos[s] = 0;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) widen8<DT>(raw[s], x[s]);
+    if (!turn) return false;
+    const int cb = col * 8;
+    if (a.pairs) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        if (valid[s] && cb < a.rot) {
+          const float* t = a.table + (int64_t)pos[s] * a.table_stride + cb / 2;
+          const f32x4 c = *reinterpret_cast<const f32x4*>(t), n = *reinterpret_cast<const f32x4*>(t + a.rot / 2);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x1 = x[s][2 * e], x2 = x[s][2 * e + 1];
+            x[s][2 * e] = x1 * c[e] - x2 * n[e];
+            x[s][2 * e + 1] = x2 * c[e] + x1 * n[e];
+          }
+        }
+    } else {
+      const int half = a.rot / 2, far = half / 8;
+      const bool low = cb < half;
+      const int other = cb < a.rot ? (low ? lane + far : lane - far) : lane;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        u32x4 ow;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ow[e] = (uint32_t)__shfl((int)raw[s][e], other);
+        if (valid[s] && cb < a.rot) {
+          float y[8];
+          widen8<DT>(ow, y);
+          const float* t = a.table + (int64_t)pos[s] * a.table_stride + (low ? cb : cb - half);
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const f32x4 c = *reinterpret_cast<const f32x4*>(t + 4 * p), n = *reinterpret_cast<const f32x4*>(t + half + 4 * p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float& v = x[s][4 * p + e];
+              const float far_part = y[4 * p + e] * n[e];
+              v = low ? v * c[e] - far_part : v * c[e] + far_part;
+            }
+          }
+        }
+      }
+    }
+    return bad;
+  }
+
+  __device__ __forceinline__ u32x4 packed(int s, bool turned) const {
+    if (!turned) return raw[s];
+    return u32x4{narrow2<DT>(x[s][0], x[s][1]), narrow2<DT>(x[s][2], x[s][3]), narrow2<DT>(x[s][4], x[s][5]),
+                 narrow2<DT>(x[s][6], x[s][7])};
+  }
+};
+
+template <int KIND>
+__device__ __forceinline__ u32x2 codes8(const float (&y)[8]) {
+  u32x2 w;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    if constexpr (KIND == KVH_CACHE_I8) {
+      uint32_t b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = (uint32_t)(int)__builtin_rintf(y[4 * p + e]) & 0xffu;
+      w[p] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+    } else {
+      int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * p], y[4 * p + 1], 0, false);
+      w[p] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * p + 2], y[4 * p + 3], r, true);
+    }
+  }
+  return w;
+}
+
+template <int KIND>
+__device__ __forceinline__ void values8(const u32x2& w, float (&y)[8]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    if constexpr (KIND == KVH_CACHE_I8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[4 * p + e] = (float)(int8_t)(w[p] >> 8 * e);
+    } else {
+      y[4 * p] = __builtin_amdgcn_cvt_f32_fp8((int)w[p], 0);
+      y[4 * p + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[p], 1);
+      y[4 * p + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[p], 2);
+      y[4 * p + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[p], 3);
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+template <int DT, int KIND, int D>
+__global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
+  using T = Tile<DT, D>;
+  const int lane = threadIdx.x % kWave;
+  const uint32_t u = uniform((int32_t)(blockIdx.x * kWavesPerBlock + threadIdx.x / kWave));
+  if (u >= a.units) return;
+  const int b = blockIdx.y, layer = blockIdx.z;
+  Request rq;
+  rq.start = a.req.starts[b];
+  const int32_t end = a.req.starts[b + 1];
+  rq.len = a.req.lens[b];
+  rq.n = end - rq.start;
+  rq.ok = request_ok(a.req, rq.start, end, rq.len) && rq.len >= rq.n;
+  const bool tells = lane == 0 && a.status != nullptr;
+  if (!rq.ok) {
+    if (tells && u == 0) a.status[b] = KVH_DEV_BAD_REQUEST;
+    return;
+  }
+  const int before = rq.len - rq.n, col = lane % T::kLanes, sub = lane / T::kLanes;
+  const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
+  bool bad = false;
+  T t;
+  if (u >= a.kv_units) {  // queries
+    const uint32_t w = u - a.kv_units, tile = a.by_q.quotient(w), head = w - tile * (uint32_t)a.q_heads;
+    const int i0 = (int)tile * kTileRows;
+    if (i0 >= rq.n) return;
+    bad = t.load(a, a.q + layer * a.q_ls + head * D, a.q_ts, rq, i0, rq.n, a.rot != 0, lane);
+#pragma unroll
+    for (int s = 0; s < T::kSteps; ++s)
+      if (t.valid[s]) {
+        const int64_t row = (int64_t)rq.start + i0 + s * T::kRows + sub;
+        *reinterpret_cast<u32x4*>(a.q_out + layer * a.o_ls + row * a.o_ts + head * D + col * 8) = t.packed(s, a.rot != 0);
+      }
+  } else {
+    const uint32_t part = a.by_kv.quotient(u);
+    uint32_t head = u - part * 2u * (uint32_t)a.heads;
+    const bool is_v = head >= (uint32_t)a.heads;
+    if (is_v) head -= a.heads;
+    const uint16_t* src = (is_v ? a.v : a.k) + layer * a.kv_ls + head * D;
+    const bool turn = !is_v && a.rot != 0;
+    uint8_t* cache = (is_v ? a.cv : a.ck) + (layer * a.c_ls + head * D) * (KIND == KVH_CACHE_16 ? 2 : 1);
+    if constexpr (KIND == KVH_CACHE_16) {
+      const int i0 = (int)part * kTileRows;
+      if (i0 >= rq.n) return;
+      bad = t.load(a, src, a.kv_ts, rq, i0, rq.n, turn, lane);
+#pragma unroll
+      for (int s = 0; s < T::kSteps; ++s) {
+        const int slot = before + i0 + s * T::kRows + sub;
+        if (!t.valid[s]) continue;
+        const int at = (int)a.by_block.quotient((uint32_t)slot), page = table[at];
+        if (page < 0 || page >= a.pages) {
+          bad = true;
+          continue;
+        }
+        const int64_t row = (int64_t)page * a.block_tokens + (slot - at * a.block_tokens);
+        *reinterpret_cast<u32x4*>(cache + (row * a.c_ts + col * 8) * 2) = t.packed(s, turn);
+      }
+    } else {
+      const int at = (int)a.by_block.quotient((uint32_t)before) + (int)part;  // the page's place in the request
+      const int64_t page_slot = (int64_t)at * a.block_tokens;
+      const int i0 = page_slot > before ? (int)(page_slot - before) : 0;
+      if (i0 >= rq.n) return;
+      const int64_t past = page_slot + a.block_tokens - before;
+      const int i_end = past < rq.n ? (int)past : rq.n;
+      const int page = table[at];
+      if (page < 0 || page >= a.pages) {
+        if (tells) a.status[b] = KVH_DEV_BAD_REQUEST;
+        return;
+      }
+      const int row0 = (int)(before + i0 - page_slot);  // the first new row of the page
+      float* scale_at = (is_v ? a.sv : a.sk) + layer * a.s_ls + (int64_t)page * a.s_ps + head;
+      const float old = row0 > 0 ? *scale_at : 0.0f;
+      float most = 0.0f;
+      for (int i = i0; i < i_end; i += kTileRows) {
+        bad |= t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);
+#pragma unroll
+        for (int s = 0; s < T::kSteps; ++s)
+          if (t.valid[s]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(t.x[s][e]));
+          }
+      }
+      most = wave_max(most);
+      constexpr float kTop = KIND == KVH_CACHE_I8 ? 127.0f : 448.0f;
+      const float now = fmaxf(old, most < 0x1p-100f ? 0.0f : most / kTop);
+      const float inv = now > 0.0f ? 1.0f / now : 0.0f;
+      uint8_t* rows = cache + (int64_t)page * a.block_tokens * a.c_ts + col * 8;
+      if (now > old && old > 0.0f) {  // earlier rows of the page under its new scale
+        const float rate = old / now;
+        for (int r = sub; r < row0; r += T::kRows) {
+          u32x2* p = reinterpret_cast<u32x2*>(rows + (int64_t)r * a.c_ts);
+          float y[8];
+          values8<KIND>(*p, y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] *= rate;
+          *p = codes8<KIND>(y);
+        }
+      }
+      for (int i = i0; i < i_end; i += kTileRows) {
+        if (i_end - i0 > kTileRows) t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);  // otherwise the rows are still here
+#pragma unroll
+        for (int s = 0; s < T::kSteps; ++s)
+          if (t.valid[s]) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = t.x[s][e] * inv;
+            const int r = row0 + (i - i0) + s * T::kRows + sub;
+            *reinterpret_cast<u32x2*>(rows + (int64_t)r * a.c_ts) = codes8<KIND>(y);
+          }
+      }
+      if (lane == 0) *scale_at = now;
+    }
+  }
+  if (__any(bad) && tells) a.status[b] = KVH_DEV_BAD_REQUEST;
+}
+
+template <int DT, int KIND>
+void launch_dim(const AppendParams& a, int head_dim, dim3 grid, hipStream_t stream) {
+  if (head_dim == 128)
+    launch_kernel(append_kernel<DT, KIND, 128>, grid, dim3(kBlockThreads), 0, stream, a);
+  else
+    launch_kernel(append_kernel<DT, KIND, 64>, grid, dim3(kBlockThreads), 0, stream, a);
+}
+
+template <int DT>
+void launch_kind(const AppendParams& a, int kind, int head_dim, dim3 grid, hipStream_t stream) {
+  switch (kind) {
+    case KVH_CACHE_16: return launch_dim<DT, KVH_CACHE_16>(a, head_dim, grid, stream);
+    case KVH_CACHE_I8: return launch_dim<DT, KVH_CACHE_I8>(a, head_dim, grid, stream);
+    default: return launch_dim<DT, KVH_CACHE_E4M3>(a, head_dim, grid, stream);
+  }
+}
+
+}  // namespace
+}  // namespace kvh
+
+using namespace kvh;
+
+extern "C" int kvh_append(const kvh_cache* cache, const kvh_requests* requests, kvh_dtype dt, const kvh_kv_view* kv, const kvh_rows* q,
+                          const kvh_rows* q_out, int q_heads, const kvh_rotation* rotation, int32_t* status_dev, void* stream) {
+  if (dt != KVH_F16 && dt != KVH_BF16) return KVH_E_ARG;
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_requests(requests)) return rc;
+  if (kv == nullptr || kv->k == nullptr || kv->v == nullptr) return KVH_E_ARG;
+  const int64_t c = (int64_t)cache->heads * cache->head_dim;
+  for (void* p : {kv->k, kv->v}) {
+    const kvh_rows rows{p, kv->layer_stride, kv->token_stride};
+    if (int rc = check_rows(&rows, c)) return rc;
+  }
+  AppendParams a{};
+  if (q != nullptr) {
+    if (q_out == nullptr) return KVH_E_ARG;
+    if (q_heads < 1 || q_heads > 65536) return KVH_E_SHAPE;
+    for (const kvh_rows* r : {q, q_out})
+      if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim)) return rc;
+    a.q = static_cast<const uint16_t*>(q->p);
+    a.q_out = static_cast<uint16_t*>(q_out->p);
+    a.q_ls = q->layer_stride, a.q_ts = q->token_stride;
+    a.o_ls = q_out->layer_stride, a.o_ts = q_out->token_stride;
+    a.q_heads = q_heads;
+  }
+  if (rotation != nullptr) {
+    if (rotation->table == nullptr || rotation->n_positions < 1 || rotation->table_stride < 0) return KVH_E_ARG;
+    if (rotation->rot < 16 || rotation->rot % 16 != 0 || rotation->rot > cache->head_dim) return KVH_E_SHAPE;
+    if (!is_aligned16(rotation->table) || rotation->table_stride % 4 != 0) return KVH_E_ALIGN;
+    a.table = rotation->table;
+    a.positions = rotation->positions;
+    a.table_stride = rotation->table_stride;
+    a.n_positions = rotation->n_positions;
+    a.rot = rotation->rot;
+    a.pairs = rotation->pairs;
+  }
+  if (requests->n_tokens == 0) return KVH_OK;
+  a.req = Requests(*requests, cache->block_tokens);
+  a.k = static_cast<const uint16_t*>(kv->k), a.v = static_cast<const uint16_t*>(kv->v);
+  a.kv_ls = kv->layer_stride, a.kv_ts = kv->token_stride;
+  a.ck = static_cast<uint8_t*>(cache->k), a.cv = static_cast<uint8_t*>(cache->v);
+  a.sk = cache->k_scale, a.sv = cache->v_scale;
+  a.c_ls = cache->layer_stride, a.c_ts = cache->token_stride;
+  a.s_ls = cache->scale_layer_stride, a.s_ps = cache->scale_page_stride;
+  a.pages = cache->pages, a.block_tokens = cache->block_tokens, a.heads = cache->heads;
+  a.status = status_dev;
+  a.by_block = Divisor((uint32_t)cache->block_tokens);
+  a.by_kv = Divisor(2u * (uint32_t)cache->heads);
+  a.by_q = Divisor((uint32_t)(a.q_heads > 0 ? a.q_heads : 1));
+  const int most = requests->max_new < requests->n_tokens ? requests->max_new : requests->n_tokens;
+  a.req.max_new = most;
+  const int64_t tiles = (most + kTileRows - 1) / kTileRows;
+  const int64_t spread = ((int64_t)most + cache->block_tokens - 2) / cache->block_tokens + 1;  // pages that `most` tokens touch at most
+  const int64_t parts = cache->kind == KVH_CACHE_16 ? tiles : spread < most ? spread : most;
+  const int64_t kv_units = parts * 2 * cache->heads, units = kv_units + tiles * a.q_heads;
+  if (units >= (int64_t)1 << 31) return KVH_E_SHAPE;
+  a.kv_units = (uint32_t)kv_units, a.units = (uint32_t)units;
+  const dim3 grid((unsigned)((units + kWavesPerBlock - 1) / kWavesPerBlock), (unsigned)requests->n_requests, (unsigned)cache->layers);
+  if (dt == KVH_F16)
+    launch_kind<KVH_F16>(a, cache->kind, cache->head_dim, grid, static_cast<hipStream_t>(stream));
+  else
+    launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, grid, static_cast<hipStream_t>(stream));
+  KVH_HIP_CHECK_LAUNCH();
+  return KVH_OK;
+}

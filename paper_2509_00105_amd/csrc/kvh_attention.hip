@@ -1,0 +1,894 @@
+// kvh_attention: the queries of a request's new tokens over one layer of the paged cache.
+//
+// S^T = K Q^T and O^T = V^T P^T, tile by tile, with a running maximum and sum (one pass over the cache).  Both products put the
+// query rows on the columns of the matrix instruction (16x16x32: lane l holds column l % 16), so everything that belongs to a
+// query row - its maximum, its sum, the factor that rescales its output - is a value of the lane's own, and the weights leave
+// the first product in the very lanes in which the second one wants them: the order of the tokens inside its sum is free, and
+// is chosen so.  The rows of one KV head are the (new token, query head) pairs that read it, token-major: 16 of them a tile.
+//
+// A code enters the products as the number it is (an int8 or e4m3 is exact in fp16; the queries are brought to fp16 with a power of
+// two of their row's own), the K scale of its page multiplies the finished dot product, and the V scale sv of its page enters the
+// exponent: with s' = s + log2 sv and m' = max s', the weight exp2(s' - m') <= 1 multiplies the code and exp2(s' - m') / sv adds
+// to the sum.  A weight is thus as exact as fp16 is, however the scales of a request's pages differ.
+#include "kvh_cache.hpp"
+
+namespace kvh {
+namespace {
+
+constexpr int kStep = 32;  // tokens a wave takes at once: two tiles of 16
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLeastScale = 0x1p-60f;  // V scales below it keep it in the exponent; the rest goes onto the weight
+
+struct AttnParams {
+  Requests req;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  int64_t q_ts, o_ts;  // elements
+  const uint8_t *ck, *cv;  // of the layer
+  const float *sk, *sv;
+  int64_t c_ts, s_ps;
+  int pages, block_tokens, heads, group;
+  float scale;
+  int causal, sink, window;
+  int32_t* status;
+  float* part;       // partial outputs [slot][rows][D], then (maximum, sum) [slot][rows][2]; nullptr: nothing is split
+  float* part_ml;
+  int target;        // items that the batch is cut into, about
+  int least;         // steps of an item at least, where a request is cut
+  int64_t items;     // partial results that there is room for, of each head
+  Divisor by_block, by_group;
+};
+
+// ---- items --------------------------------------------------------------------------------------------------------
+// A request's rows come in tiles of `tile_rows`, its tokens in steps of 32, and an item is a tile and a run of `chunk` steps.  All
+// blocks work out the same list from the lengths: no block is idle while another has two requests' worth of tokens, and the host
+// need not know the lengths.
+__device__ __forceinline__ int steps_of(const AttnParams& a, const Request& rq, int tile_rows) {
+  if (!rq.ok || rq.n == 0) return 0;
+  const int all = (rq.len + kStep - 1) / kStep;
+  if (a.window == 0) return all;
+  const int64_t reach = (int64_t)a.window + tile_rows + 2 * kStep;  // of a tile's rows, with a step begun on either side
+  const int64_t some = reach / kStep + (a.sink + kStep - 1) / kStep;
+  return all < some ? all : (int)some;
+}
+
+struct Item {
+  int b, tile, part, parts;  // parts: of the request's tokens
+  int chunk;
+  Request rq;
+};
+
+__device__ __forceinline__ Request read_request(const AttnParams& a, int b) {
+  Request rq{0, 0, 0, false};
+  if (b < a.req.n) {
+    rq.start = a.req.starts[b];
+    const int32_t end = a.req.starts[b + 1];
+    rq.len = a.req.lens[b];
+    rq.n = end - rq.start;
+    rq.ok = request_ok(a.req, rq.start, end, rq.len);
+  }
+  return rq;
+}
+
+// Steps of an item, from the steps of the batch.
+__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows, int lane) {
+  if (a.part == nullptr) return 0x7fffffff;
+  int64_t total = 0;
+  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
+    const Request rq = read_request(a, b0 + lane);
+    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
+    int64_t s = (int64_t)tiles * steps_of(a, rq, tile_rows);
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) s += __shfl_xor((long long)s, d);
+    total += s;
+  }
+  int64_t chunk = (total + a.target - 1) / a.target;
+  if (chunk < a.least) chunk = a.least;
+  chunk = (chunk + 3) & ~(int64_t)3;  // four waves share it
+  return chunk < 0x7fffffff ? (int)chunk : 0x7fffffff;
+}
+
+// The request whose item (or, with by_row, whose packed row) `want` is.  Returns false where there is none.
+__device__ __forceinline__ bool find_item(const AttnParams& a, int tile_rows, int64_t want, bool by_row, int lane, Item& it) {
+  it.chunk = chunk_of(a, tile_rows, lane);
+  int64_t base = 0;
+  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
+    const Request rq = read_request(a, b0 + lane);
+    const int steps = steps_of(a, rq, tile_rows);
+    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
+    int parts = steps == 0 ? 1 : 1 + (steps - 1) / it.chunk;
+    const int64_t mine = (int64_t)tiles * parts;
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int64_t o = __shfl_up((long long)upto, d);
+      if (lane >= d) upto += o;
+    }
+    const bool here = by_row ? rq.ok && want >= rq.start && want < (int64_t)rq.start + rq.n
+                             : want >= base + upto - mine && want < base + upto;
+    const uint64_t who = __ballot(here);
+    if (who != 0) {
+      const int l = __builtin_ctzll(who);
+      it.b = b0 + l;
+      it.rq.start = uniform(__shfl(rq.start, l));
+      it.rq.n = uniform(__shfl(rq.n, l));
+      it.rq.len = uniform(__shfl(rq.len, l));
+      it.rq.ok = true;
+      it.parts = uniform(__shfl(parts, l));
+      const int64_t first = base + __shfl((long long)(upto - mine), l);
+      if (by_row) {
+        it.tile = 0;
+        it.part = (int)first;  // the request's first item
+      } else {
+        const int in = uniform((int)(want - first));
+        it.tile = in / it.parts;
+        it.part = in - it.tile * it.parts;
+      }
+      return true;
+    }
+    base += __shfl((long long)upto, kWave - 1);
+  }
+  return false;
+}
+
+// ---- operands -----------------------------------------------------------------------------------------------------
+template <int DT, int KIND>
+constexpr bool kBf16 = KIND == KVH_CACHE_16 && DT == KVH_BF16;  // the products' type; fp16 otherwise
+
+template <bool BF>
+__device__ __forceinline__ f32x4 mfma(const u32x4& x, const u32x4& y, const f32x4& c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+}
+
+// bytes (lo, hi) of offset-binary codes q + 128 in the low byte of each half, 0x64 above: 1024 + 128 + q in fp16
+__device__ __forceinline__ uint32_t less_1152(uint32_t w) {
+  const f16x2 h = __builtin_bit_cast(f16x2, w), o = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+  return __builtin_bit_cast(uint32_t, h + o);
+}
+
+// 4 codes of one word -> 2 words of fp16 pairs, in order.
+template <int KIND>
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if constexpr (KIND == KVH_CACHE_I8) {
+    w ^= 0x80808080u;
+    lo = less_1152(__builtin_amdgcn_perm(0x64646464u, w, 0x04010400u));
+    hi = less_1152(__builtin_amdgcn_perm(0x64646464u, w, 0x04030402u));
+  } else {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  }
+}
+
+// The same 4 channels of two tokens x, y -> pairs (x, y) of each channel.
+template <int KIND>
+__device__ __forceinline__ void zip4(uint32_t x, uint32_t y, uint32_t (&p)[4]) {
+  widen4<KIND>(__builtin_amdgcn_perm(y, x, 0x05010400u), p[0], p[1]);
+  widen4<KIND>(__builtin_amdgcn_perm(y, x, 0x07030602u), p[2], p[3]);
+}
+
+template <int N>
+struct Words {
+  uint32_t w[N];
+};
+// N words from memory, in the widest accesses (N a power of two; the address is aligned to 4 N bytes, 16 at most).
+template <int N>
+__device__ __forceinline__ Words<N> fetch(const uint8_t* p) {
+  Words<N> r;
+  if constexpr (N == 1) {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+    r.w[0] = v[0], r.w[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(p + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.w[4 * i + e] = v[e];
+    }
+  }
+  return r;
+}
+
+__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float over_groups_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// ---- the page table, 64 entries at a time in the lanes ---------------------------------------------------------------
+struct PageRun {
+  int base, entry;  // entry of page base + lane; -1 where it is none of the cache's
+
+  __device__ __forceinline__ void load(const AttnParams& a, const int32_t* table, int first, int last, int lane) {
+    base = first;
+    entry = -1;
+    if (first + lane <= last) {
+      entry = table[first + lane];
+      if (entry >= a.pages) entry = -1;
+    }
+  }
+};
+
+// ---- the kernel ---------------------------------------------------------------------------------------------------
+// NR tiles of 16 query rows share each K and V tile that is read.  PAGE16: pages hold a multiple of 16 tokens, so a tile lies on
+// one page and its address and scales are the wave's; otherwise every lane looks its tokens' pages up.
+template <int DT, int KIND, int D, int NR, bool PAGE16>
+struct Worker {
+  static constexpr bool kBf = kBf16<DT, KIND>;
+  static constexpr int kWidth = KIND == KVH_CACHE_16 ? 2 : 1;
+  static constexpr int kSums = D / 32;           // matrix instructions of a dot product
+  static constexpr int kChans = D / 16;          // channels of V that a lane reads of a token, and channel tiles of the output
+  static constexpr int kKWords = D * kWidth / 16;       // words of K that a lane reads of a tile
+  static constexpr int kVWords = kChans * kWidth / 4;   // words of V that a lane reads of a token
+
+  const AttnParams& a;
+  Request rq;
+  int head, row0, rows;  // of the tile: its first row, rows it has
+  int lane, l16, grp;
+  int end;               // tokens at and past it are seen by no row
+  int p_least, p_most;   // logical positions of the tile's first and last row
+
+  u32x4 q[NR][kSums];
+  float coef[NR];  // what turns a dot product into an exponent of 2
+  int pos[NR];
+  f32x4 o[NR][kChans];
+  float m[NR], l[NR];
+  PageRun run;
+  bool bad;  // a token that a row should see lies on no page of the cache
+
+  __device__ __forceinline__ Worker(const AttnParams& a_) : a(a_) {}
+
+  // Channel of element i of sum kk in lane group g, the same for K and Q.  K is read in 16-byte pieces: 8 channels of 16 bits, or 16 of 8
+  // bits for two sums.
+  static __device__ __forceinline__ int channel(int kk, int g) {
+    return KIND == KVH_CACHE_16 ? kk * 32 + g * 8 : (kk / 2) * 64 + g * 16 + (kk % 2) * 8;
+  }
+
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+      const int r = t * 16 + l16;
+      const bool real = r < rows;
+      const int at = row0 + (real ? r : 0), token = (int)a.by_group.quotient((uint32_t)at), u = at - token * a.group;
+      pos[t] = rq.len - rq.n + token;
+      const uint16_t* src = a.q + ((int64_t)rq.start + token) * a.q_ts + ((int64_t)head * a.group + u) * D;
+      float most = 0.0f;
+      u32x4 raw[kSums];
+#pragma unroll
+      for (int kk = 0; kk < kSums; ++kk) {
+        raw[kk] = u32x4{0, 0, 0, 0};
+        if (real) raw[kk] = *reinterpret_cast<const u32x4*>(src + channel(kk, grp));
+      }
+      coef[t] = a.scale * kLog2e;
+      if constexpr (KIND != KVH_CACHE_16 && DT == KVH_BF16) {
+        // bf16 -> fp16 with a power of two that brings the row's largest value to [1, 2)
+#pragma unroll
+        for (int kk = 0; kk < kSums; ++kk) {
+          float x[8];
+          widen8<DT>(raw[kk], x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+        }
+        most = over_groups_max(most);
+        int ex = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
+        if (ex < -100 || ex > 127) ex = 0;  // nothing but zeros (or next to it); infinities stay what they are
+        const float down = __builtin_bit_cast(float, (uint32_t)(127 - (ex > 126 ? 126 : ex)) << 23), up = 1.0f / down;
+        coef[t] *= up;
+#pragma unroll
+        for (int kk = 0; kk < kSums; ++kk) {
+          float x[8];
+          widen8<DT>(raw[kk], x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) q[t][kk][e] = narrow2<KVH_F16>(x[2 * e] * down, x[2 * e + 1] * down);
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < kSums; ++kk) q[t][kk] = raw[kk];
+      }
+      m[t] = -INFINITY;
+      l[t] = 0.0f;
+#pragma unroll
+      for (int ct = 0; ct < kChans; ++ct) o[t][ct] = f32x4{0, 0, 0, 0};
+    }
+    bad = false;
+    run.base = -1000;
+  }
+
+  __device__ __forceinline__ bool sees(int p, int token) const {
+    return token < end && (!a.causal || token <= p) && (a.window == 0 || token > p - a.window || token < a.sink);
+  }
+
+  // One step: tokens [t0, t0 + 32), t0 < end, a multiple of 32.
+  __device__ __forceinline__ void step(const int32_t* table, int t0) {
+    const int last = end - 1;
+    Words<kKWords> k[2];
+    Words<kVWords> v[8];
+    float ks[8], lsv[8], inv[8], rest[8];  // by token slot: 4 i + r is token 16 i + 4 grp + r
+    bool hidden_any = false;
+    uint32_t absent = 0;  // token slots on no page of the cache
+    const int64_t row_bytes = a.c_ts * kWidth;
+    const int64_t head_at = (int64_t)head * D * kWidth;
+    if constexpr (PAGE16) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int t = t0 + 16 * i;
+        if (t > last) t = last & ~15;  // a tile past the end reads the last one again, and is masked
+        const int at = (int)a.by_block.quotient((uint32_t)t);
+        if ((unsigned)(at - run.base) >= (unsigned)kWave) run.load(a, table, at, (int)a.by_block.quotient((uint32_t)last), lane);
+        int page = uniform(__builtin_amdgcn_readlane(run.entry, at - run.base));
+        if (page < 0) {
+          page = 0;
+          absent |= 15u << 4 * i;
+        }
+        const int64_t row = (int64_t)page * a.block_tokens + (t - at * a.block_tokens);
+        const uint8_t *kt = a.ck + head_at + row * row_bytes, *vt = a.cv + head_at + row * row_bytes;
+        const int most = last - t;  // rows past it are none of the request's: the last one is read again, and masked
+        const int kr = l16 < most ? l16 : most;
+        const uint8_t* kp = kt + (uint32_t)kr * (uint32_t)row_bytes + grp * 16;
+#pragma unroll
+        for (int j = 0; j < kKWords / 4; ++j) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + j * 64);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) k[i].w[4 * j + e] = w[e];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int vr = grp * 4 + r < most ? grp * 4 + r : most;
+          v[4 * i + r] = fetch<kVWords>(vt + (uint32_t)vr * (uint32_t)row_bytes + l16 * (kChans * kWidth));
+        }
+        if constexpr (KIND != KVH_CACHE_16) {
+          const float s = a.sk[(int64_t)page * a.s_ps + head], z = a.sv[(int64_t)page * a.s_ps + head];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) ks[4 * i + r] = s, lsv[4 * i + r] = z;
+        }
+      }
+    } else {
+      const int at0 = (int)a.by_block.quotient((uint32_t)t0), tz = t0 + kStep - 1 < last ? t0 + kStep - 1 : last;
+      const int at1 = (int)a.by_block.quotient((uint32_t)tz);
+      if (at0 < run.base || at1 - run.base >= kWave) run.load(a, table, at0, (int)a.by_block.quotient((uint32_t)last), lane);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int t = t0 + 16 * i + l16 < last ? t0 + 16 * i + l16 : last;
+        const int at = (int)a.by_block.quotient((uint32_t)t);
+        const int page = __shfl(run.entry, at - run.base);
+        const int64_t row = (int64_t)(page < 0 ? 0 : page) * a.block_tokens + (t - at * a.block_tokens);
+        const uint8_t* kp = a.ck + head_at + row * row_bytes + grp * 16;
+#pragma unroll
+        for (int j = 0; j < kKWords / 4; ++j) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + j * 64);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) k[i].w[4 * j + e] = w[e];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int tok = t0 + 16 * (i / 4) + grp * 4 + i % 4, t = tok < last ? tok : last;
+        const int at = (int)a.by_block.quotient((uint32_t)t);
+        int page = __shfl(run.entry, at - run.base);
+        if (page < 0) {
+          page = 0;
+          absent |= 1u << i;
+        }
+        const int64_t row = (int64_t)page * a.block_tokens + (t - at * a.block_tokens);
+        v[i] = fetch<kVWords>(a.cv + head_at + row * row_bytes + l16 * (kChans * kWidth));
+        if constexpr (KIND != KVH_CACHE_16) {
+          ks[i] = a.sk[(int64_t)page * a.s_ps + head];
+          lsv[i] = a.sv[(int64_t)page * a.s_ps + head];
+        }
+      }
+    }
+    // Whether some row does not see all of these tokens.
+    hidden_any = t0 + kStep > end || (a.causal && t0 + kStep - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) ||
+                 __any(absent != 0);
+    if constexpr (KIND != KVH_CACHE_16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float z = lsv[i];
+        // a scale of zero (or next to it) keeps its tokens in the sum and takes their values off the weight
+        const float used = z < kLeastScale ? kLeastScale : z;
+        rest[i] = z < kLeastScale ? z * (1.0f / kLeastScale) : 1.0f;
+        lsv[i] = __builtin_amdgcn_logf(used);
+        inv[i] = __builtin_amdgcn_rcpf(used);
+      }
+    }
+
+    u32x4 kop[2][kSums];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int kk = 0; kk < kSums; ++kk) {
+        if constexpr (KIND == KVH_CACHE_16) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kop[i][kk][e] = k[i].w[4 * kk + e];
+        } else {
+          uint32_t w[4];
+          widen4<KIND>(k[i].w[2 * kk], w[0], w[1]);
+          widen4<KIND>(k[i].w[2 * kk + 1], w[2], w[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kop[i][kk][e] = w[e];
+        }
+      }
+
+    u32x4 p[NR];
+    float w[NR][8];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+      f32x4 s[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s[i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int kk = 0; kk < kSums; ++kk) s[i] = mfma<kBf>(kop[i][kk], q[t][kk], s[i]);
+      }
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (KIND == KVH_CACHE_16)
+          x[i] = s[i / 4][i % 4] * coef[t];
+        else
+          x[i] = __builtin_fmaf(s[i / 4][i % 4], ks[i] * coef[t], lsv[i]);
+      }
+      if (hidden_any) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool seen = sees(pos[t], t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
+          bad |= seen && none;
+          if (!seen || none) x[i] = -INFINITY;
+        }
+      }
+      float most = x[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) most = fmaxf(most, x[i]);
+      most = over_groups_max(most);
+      if (__any(most > m[t])) {
+        const float now = fmaxf(m[t], most);
+        const float down = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
+        m[t] = now;
+        l[t] *= down;
+#pragma unroll
+        for (int ct = 0; ct < kChans; ++ct) o[t][ct] *= down;
+      }
+      const float top = m[t] == -INFINITY ? 0.0f : m[t];  // nothing seen yet: the weights below are zeros
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float e = __builtin_amdgcn_exp2f(x[i] - top);
+        if constexpr (KIND == KVH_CACHE_16) {
+          l[t] += e;
+        } else {
+          l[t] = __builtin_fmaf(e, inv[i], l[t]);
+          e *= rest[i];
+        }
+        w[t][i] = e;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[t][e] = narrow2<kBf ? KVH_BF16 : KVH_F16>(w[t][2 * e], w[t][2 * e + 1]);
+    }
+
+    if (hidden_any) {
+      // What no row sees is not multiplied at all; what some rows see and others do not may only meet those that do.
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int tok = t0 + 16 * (i / 4) + grp * 4 + i % 4;
+        const bool none = tok >= end || (absent >> i & 1u);
+#pragma unroll
+        for (int e = 0; e < kVWords; ++e) v[i].w[e] = none ? 0u : v[i].w[e];
+      }
+      if constexpr (KIND != KVH_CACHE_I8) {
+        bool odd = false;  // an infinity or NaN among them
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < kVWords; ++e) odd |= has_odd(v[i].w[e]);
+        if (__any(odd)) {
+          one_by_one(w, table, t0);
+          return;
+        }
+      }
+    }
+#pragma unroll
+    for (int c4 = 0; c4 < kVWords; ++c4) {
+      constexpr int kPer = 4 / kWidth;  // channels of a word
+      uint32_t z[4][kPer];              // pairs of tokens, of each channel
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (KIND == KVH_CACHE_16) {
+          z[e][0] = __builtin_amdgcn_perm(v[2 * e + 1].w[c4], v[2 * e].w[c4], 0x05040100u);
+          z[e][1] = __builtin_amdgcn_perm(v[2 * e + 1].w[c4], v[2 * e].w[c4], 0x07060302u);
+        } else {
+          zip4<KIND>(v[2 * e].w[c4], v[2 * e + 1].w[c4], z[e]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const u32x4 vop = {z[0][j], z[1][j], z[2][j], z[3][j]};
+#pragma unroll
+        for (int t = 0; t < NR; ++t) o[t][c4 * kPer + j] = mfma<kBf>(vop, p[t], o[t][c4 * kPer + j]);
+      }
+    }
+  }
+
+  static __device__ __forceinline__ bool has_odd(uint32_t w) {
+    if constexpr (KIND == KVH_CACHE_E4M3) {
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= (w >> 8 * e & 0x7fu) == 0x7fu;
+      return odd;
+    } else {
+      constexpr uint32_t kExp = DT == KVH_BF16 ? 0x7f80u : 0x7c00u;
+      return (w & kExp) == kExp || (w >> 16 & kExp) == kExp;
+    }
+  }
+
+  // The weighted sum of a step whose tokens hold an infinity or NaN that some rows do not see: token by token in fp32, adding nothing
+  // to a row that does not see it.  Rare, and as slow as it looks: the values are read again, so that nothing has to stay in registers
+  // for it.
+  __device__ __forceinline__ void one_by_one(float (&w)[NR][8], const int32_t* table, int t0) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll 1
+      for (int g = 0; g < 4; ++g) {
+        const int tok = t0 + 16 * (i / 4) + g * 4 + i % 4;
+        if (tok >= end) continue;
+        const int at = (int)a.by_block.quotient((uint32_t)tok), page = table[at];
+        if (page < 0 || page >= a.pages) continue;
+        const int64_t row = (int64_t)page * a.block_tokens + (tok - at * a.block_tokens);
+        const uint8_t* src = a.cv + ((int64_t)head * D + row * a.c_ts + 4 * grp * kChans) * kWidth;
+        float e[NR];
+#pragma unroll
+        for (int t = 0; t < NR; ++t) e[t] = __shfl(w[t][0], g * 16 + l16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {  // the lane holds of its row the channels (4 grp + r) kChans + ct
+          const Words<kVWords> raw = fetch<kVWords>(src + r * kChans * kWidth);
+          float x[kChans];
+#pragma unroll
+          for (int c = 0; c < kVWords; ++c) {
+            if constexpr (KIND == KVH_CACHE_16) {
+              x[2 * c] = t16_to_f32<DT>(raw.w[c] & 0xffffu);
+              x[2 * c + 1] = t16_to_f32<DT>(raw.w[c] >> 16);
+            } else if constexpr (KIND == KVH_CACHE_E4M3) {
+              x[4 * c] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 0);
+              x[4 * c + 1] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 1);
+              x[4 * c + 2] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 2);
+              x[4 * c + 3] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 3);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < NR; ++t)
+            if (sees(pos[t], tok)) {
+#pragma unroll
+              for (int ct = 0; ct < kChans; ++ct) o[t][ct][r] = __builtin_fmaf(e[t], x[ct], o[t][ct][r]);
+            }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NR; ++t)
+#pragma unroll
+        for (int n = 0; n < 7; ++n) w[t][n] = w[t][n + 1];
+    }
+  }
+};
+
+template <int DT, int KIND, int D, int NR, bool PAGE16>
+__global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams a) {
+  using W = Worker<DT, KIND, D, NR, PAGE16>;
+  constexpr int kTile = 16 * NR;
+  constexpr int kPitch = D + 4;  // floats of a row in LDS
+  __shared__ float lds[kWavesPerBlock * 16 * kPitch];
+  __shared__ float lds_ml[kWavesPerBlock][kTile][2];
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  const int head = blockIdx.y;
+  Item it;
+  if (!find_item(a, kTile, blockIdx.x, false, lane, it)) {
+    return;
+  }
+  W w(a);
+  w.lane = lane, w.l16 = lane % 16, w.grp = lane / 16;
+  w.rq = it.rq;
+  w.head = head;
+  w.row0 = it.tile * kTile;
+  const int all = it.rq.n * a.group;
+  w.rows = all - w.row0 < kTile ? all - w.row0 : kTile;
+  w.p_least = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)w.row0);
+  w.p_most = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)(w.row0 + w.rows - 1));
+  w.end = a.causal && w.p_most + 1 < it.rq.len ? w.p_most + 1 : it.rq.len;
+  w.begin();
+  // The tile's steps: those of the first `sink` tokens, then those from the first row's window on.
+  int first = 0, sunk = 0;
+  if (a.window != 0) {
+    const int from = w.p_least - a.window + 1;
+    first = from > 0 ? from / kStep : 0;
+    sunk = (a.sink + kStep - 1) / kStep;
+    if (sunk >= first) first = sunk = 0;
+  }
+  const int steps = w.end > 0 ? sunk + (w.end + kStep - 1) / kStep - first : 0;
+  const int64_t s0 = (int64_t)it.part * it.chunk;
+  const int64_t s1 = it.part + 1 == it.parts ? steps : s0 + it.chunk < steps ? s0 + it.chunk : steps;
+  const int mine = s1 > s0 ? (int)((s1 - s0 + kWavesPerBlock - 1) / kWavesPerBlock) : 0;
+  const int64_t b0 = s0 + (int64_t)wave * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
+  const int32_t* table = a.req.table + (int64_t)it.b * a.req.table_stride;
+  for (int64_t s = b0; s < b1; ++s) w.step(table, (int)(s < sunk ? s : s - sunk + first) * kStep);
+  if (__any(w.bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
+
+  // The four waves' results become one.
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    const float sum = over_groups_sum(w.l[t]);
+    if (w.grp == 0) {
+      lds_ml[wave][t * 16 + w.l16][0] = w.m[t];
+      lds_ml[wave][t * 16 + w.l16][1] = sum;
+    }
+  }
+  const bool split = it.parts > 1;
+  const int64_t slot = (int64_t)blockIdx.x * a.heads + head;
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    if (t * 16 >= w.rows) break;
+    if (t > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int ct = 0; ct < W::kChans; ct += 4) {
+        const f32x4 x = {w.o[t][ct][r], w.o[t][ct + 1][r], w.o[t][ct + 2][r], w.o[t][ct + 3][r]};
+        *reinterpret_cast<f32x4*>(&lds[(wave * 16 + w.l16) * kPitch + (4 * w.grp + r) * W::kChans + ct]) = x;
+      }
+    __syncthreads();
+    // thread: row threadIdx / 16, D / 16 channels
+    const int r = threadIdx.x / 16, ch = (threadIdx.x % 16) * W::kChans, row = t * 16 + r;
+    if (row < w.rows) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < kWavesPerBlock; ++v) m = fmaxf(m, lds_ml[v][row][0]);
+      float l = 0.0f, x[W::kChans];
+#pragma unroll
+      for (int e = 0; e < W::kChans; ++e) x[e] = 0.0f;
+#pragma unroll
+      for (int v = 0; v < kWavesPerBlock; ++v) {
+        const float mv = lds_ml[v][row][0], f = mv == m ? 1.0f : __builtin_amdgcn_exp2f(mv - m);
+        l = __builtin_fmaf(f, lds_ml[v][row][1], l);
+#pragma unroll
+        for (int e = 0; e < W::kChans; ++e) x[e] = __builtin_fmaf(f, lds[(v * 16 + r) * kPitch + ch + e], x[e]);
+      }
+      if (split) {
+        float* to = a.part + (slot * kTile + row) * D + ch;
+#pragma unroll
+        for (int e = 0; e < W::kChans; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        if (ch == 0) {
+          a.part_ml[(slot * kTile + row) * 2] = m;
+          a.part_ml[(slot * kTile + row) * 2 + 1] = l;
+        }
+      } else {
+        const int at = w.row0 + row, token = (int)a.by_group.quotient((uint32_t)at), u = at - token * a.group;
+        const bool blind = it.rq.len == 0 || (a.causal && it.rq.len - it.rq.n + token < 0);
+        const float by = 1.0f / l;
+        const int64_t packed = (int64_t)it.rq.start + token;
+        uint16_t* to = a.out + packed * a.o_ts + ((int64_t)head * a.group + u) * D + ch;
+        uint32_t y[W::kChans / 2];
+#pragma unroll
+        for (int e = 0; e < W::kChans / 2; ++e) y[e] = blind ? 0u : narrow2<DT>(x[2 * e] * by, x[2 * e + 1] * by);
+        if constexpr (W::kChans == 8)
+          *reinterpret_cast<u32x4*>(to) = u32x4{y[0], y[1], y[2], y[3]};
+        else
+          *reinterpret_cast<u32x2*>(to) = u32x2{y[0], y[1]};
+        if (a.lse != nullptr && ch == 0)
+          a.lse[packed * ((int64_t)a.heads * a.group) + (int64_t)head * a.group + u] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+    }
+  }
+}
+
+// Joins the partial results of the requests that were cut: a wave takes one query row.
+template <int DT, int D>
+__global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int tile_rows) {
+  const int lane = threadIdx.x % kWave;
+  const int q_heads = a.heads * a.group;
+  const int64_t unit = (int64_t)blockIdx.x * kWavesPerBlock + uniform((int32_t)(threadIdx.x / kWave));
+  const int64_t packed = unit / q_heads;
+  if (packed >= a.req.n_tokens) return;
+  const int u = (int)(unit - packed * q_heads), head = u / a.group;
+  Item it;
+  if (!find_item(a, tile_rows, packed, true, lane, it) || it.parts == 1) return;
+  const int token = (int)(packed - it.rq.start);
+  const int64_t at = (int64_t)token * a.group + (u - head * a.group);
+  const int tile = (int)(at / tile_rows), row = (int)(at - (int64_t)tile * tile_rows);
+  const int64_t slot0 = it.part + (int64_t)tile * it.parts;
+  if (slot0 + it.parts > a.items) return;  // requests that share rows of the batch: none of the kernel's
+  constexpr int kPer = D / 64;
+  float m = -INFINITY, l = 0.0f, x[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
+  for (int p = 0; p < it.parts; ++p) {
+    const int64_t s = ((slot0 + p) * a.heads + head) * tile_rows + row;
+    const float mp = a.part_ml[2 * s], lp = a.part_ml[2 * s + 1];
+    const float now = fmaxf(m, mp);
+    const float fo = m == now ? 1.0f : __builtin_amdgcn_exp2f(m - now), fp = mp == now ? 1.0f : __builtin_amdgcn_exp2f(mp - now);
+    m = now;
+    l = __builtin_fmaf(l, fo, fp * lp);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x[e] = __builtin_fmaf(x[e], fo, fp * a.part[s * D + lane * kPer + e]);
+  }
+  const bool blind = it.rq.len == 0 || (a.causal && it.rq.len - it.rq.n + token < 0);
+  const float by = 1.0f / l;
+  uint16_t* to = a.out + packed * a.o_ts + (int64_t)u * D + lane * kPer;
+  if constexpr (kPer == 2)
+    *reinterpret_cast<uint32_t*>(to) = blind ? 0u : narrow2<DT>(x[0] * by, x[1] * by);
+  else
+    *to = blind ? 0 : (uint16_t)narrow2<DT>(x[0] * by, 0.0f);
+  if (a.lse != nullptr && lane == 0) a.lse[packed * q_heads + u] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Says which requests are refused; the kernels above pass over them.
+__global__ __launch_bounds__(kBlockThreads) void refuse_kernel(AttnParams a) {
+  const int b = blockIdx.x * kBlockThreads + threadIdx.x;
+  if (b < a.req.n && !read_request(a, b).ok) a.status[b] = KVH_DEV_BAD_REQUEST;
+}
+
+// ---- launch -------------------------------------------------------------------------------------------------------
+constexpr int kTarget = 512;  // blocks of 4 waves that fill the chip: 2 on each compute unit
+
+struct Plan {
+  int nr;          // tiles of 16 rows
+  int64_t tiles;   // row tiles of the batch at most
+  int64_t items;   // items at most, if requests are cut; the grid otherwise
+  int target;      // what the kernel aims at
+  size_t bytes;    // workspace of these items
+};
+
+size_t slot_bytes(int nr, int head_dim) { return (size_t)(16 * nr) * (head_dim + 2) * sizeof(float); }
+
+Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
+  Plan p;
+  const int64_t group = q_heads / heads;
+  const int64_t most = (int64_t)(max_new < n_tokens ? max_new : n_tokens) * group;
+  p.nr = most <= 16 ? 1 : 2;
+  const int rows = 16 * p.nr;
+  p.tiles = (int64_t)n_tokens * group / rows + n_requests;
+  const int64_t aim = (kTarget + heads - 1) / heads;
+  p.target = (int)aim;
+  p.items = p.target + p.tiles;  // each tile's last chunk may be short
+  p.bytes = (size_t)p.items * heads * slot_bytes(p.nr, head_dim);
+  return p;
+}
+
+template <int DT, int KIND, int D, int NR>
+void launch_pages(const AttnParams& a, dim3 grid, hipStream_t stream) {
+  if (a.block_tokens % 16 == 0)
+    launch_kernel(attention_kernel<DT, KIND, D, NR, true>, grid, dim3(kBlockThreads), 0, stream, a);
+  else
+    launch_kernel(attention_kernel<DT, KIND, D, NR, false>, grid, dim3(kBlockThreads), 0, stream, a);
+}
+
+template <int DT, int KIND, int D>
+void launch_rows(const AttnParams& a, int nr, dim3 grid, hipStream_t stream) {
+  if (nr == 1)
+    launch_pages<DT, KIND, D, 1>(a, grid, stream);
+  else
+    launch_pages<DT, KIND, D, 2>(a, grid, stream);
+}
+
+template <int DT, int KIND>
+void launch_dim(const AttnParams& a, int head_dim, int nr, dim3 grid, hipStream_t stream) {
+  if (head_dim == 128)
+    launch_rows<DT, KIND, 128>(a, nr, grid, stream);
+  else
+    launch_rows<DT, KIND, 64>(a, nr, grid, stream);
+}
+
+template <int DT>
+void launch_kind(const AttnParams& a, int kind, int head_dim, int nr, dim3 grid, hipStream_t stream) {
+  switch (kind) {
+    case KVH_CACHE_16: return launch_dim<DT, KVH_CACHE_16>(a, head_dim, nr, grid, stream);
+    case KVH_CACHE_I8: return launch_dim<DT, KVH_CACHE_I8>(a, head_dim, nr, grid, stream);
+    default: return launch_dim<DT, KVH_CACHE_E4M3>(a, head_dim, nr, grid, stream);
+  }
+}
+
+template <int DT>
+void launch_join(const AttnParams& a, int head_dim, int tile_rows, hipStream_t stream) {
+  const int64_t units = (int64_t)a.req.n_tokens * a.heads * a.group;
+  const dim3 grid((unsigned)((units + kWavesPerBlock - 1) / kWavesPerBlock));
+  if (head_dim == 128)
+    hipLaunchKernelGGL((join_kernel<DT, 128>), grid, dim3(kBlockThreads), 0, stream, a, tile_rows);
+  else
+    hipLaunchKernelGGL((join_kernel<DT, 64>), grid, dim3(kBlockThreads), 0, stream, a, tile_rows);
+}
+
+bool heads_fit(int heads, int q_heads) { return heads >= 1 && q_heads >= heads && q_heads % heads == 0 && q_heads <= 65536; }
+
+}  // namespace
+}  // namespace kvh
+
+using namespace kvh;
+
+extern "C" {
+
+size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
+  if (n_requests < 1 || n_requests > kMaxRequests || max_new < 1 || n_tokens < 1 || !heads_fit(heads, q_heads)) return 0;
+  if (head_dim != 64 && head_dim != 128) return 0;
+  return plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim).bytes;
+}
+
+int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q,
+                  const kvh_rows* out, int q_heads, float* lse_dev, float scale, int causal, int sink, int window,
+                  void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream) {
+  if ((dt != KVH_F16 && dt != KVH_BF16) || q == nullptr || out == nullptr) return KVH_E_ARG;
+  if (int rc = check_cache(cache)) return rc;
+  if (int rc = check_requests(requests)) return rc;
+  if (layer < 0 || layer >= cache->layers || !heads_fit(cache->heads, q_heads)) return KVH_E_SHAPE;
+  for (const kvh_rows* r : {q, out})
+    if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim)) return rc;
+  if (!std::isfinite(scale) || sink < 0 || window < 0 || (window > 0 && !causal) || (window == 0 && sink != 0)) return KVH_E_ARG;
+  if (!is_aligned16(workspace_dev) || (reinterpret_cast<uintptr_t>(lse_dev) & 3u) != 0) return KVH_E_ALIGN;
+  if (requests->n_tokens == 0) return KVH_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  AttnParams a{};
+  a.req = Requests(*requests, cache->block_tokens);
+  if (a.req.max_new > a.req.n_tokens) a.req.max_new = a.req.n_tokens;
+  a.q = static_cast<const uint16_t*>(q->p);
+  a.out = static_cast<uint16_t*>(out->p);
+  a.lse = lse_dev;
+  a.q_ts = q->token_stride, a.o_ts = out->token_stride;
+  const int width = cache->kind == KVH_CACHE_16 ? 2 : 1;
+  a.ck = static_cast<const uint8_t*>(cache->k) + layer * cache->layer_stride * width;
+  a.cv = static_cast<const uint8_t*>(cache->v) + layer * cache->layer_stride * width;
+  if (cache->k_scale != nullptr) {
+    a.sk = cache->k_scale + layer * cache->scale_layer_stride;
+    a.sv = cache->v_scale + layer * cache->scale_layer_stride;
+  }
+  a.c_ts = cache->token_stride, a.s_ps = cache->scale_page_stride;
+  a.pages = cache->pages, a.block_tokens = cache->block_tokens, a.heads = cache->heads;
+  a.group = q_heads / cache->heads;
+  a.scale = scale;
+  a.causal = causal != 0, a.sink = sink, a.window = window;
+  a.status = status_dev;
+  a.by_block = Divisor((uint32_t)cache->block_tokens);
+  a.by_group = Divisor((uint32_t)a.group);
+  if ((int64_t)a.req.max_new * a.group >= (int64_t)1 << 31) return KVH_E_SHAPE;
+  Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim);
+  // Requests are cut where the row tiles alone leave the chip idle and there is room for the parts.
+  const size_t one = (size_t)a.heads * slot_bytes(p.nr, cache->head_dim);
+  const size_t room = workspace_dev == nullptr ? 0 : workspace_bytes / one;
+  bool cut = p.tiles * a.heads < 2 * kTarget;
+  if (cut && room < (size_t)p.items) {
+    if (room >= (size_t)p.tiles + 1)
+      p.target = (int)(room - p.tiles), p.items = (int64_t)room;
+    else
+      cut = false;
+  }
+  if (!cut) p.items = p.tiles;
+  if (p.items > 0x7fffffff) return KVH_E_SHAPE;
+  a.target = p.target;
+  a.items = p.items;
+  a.least = 16;
+  if (cut) {
+    a.part = static_cast<float*>(workspace_dev);
+    a.part_ml = a.part + (size_t)p.items * a.heads * 16 * p.nr * cache->head_dim;
+  }
+  if (status_dev != nullptr) {
+    hipLaunchKernelGGL(refuse_kernel, dim3((a.req.n + kBlockThreads - 1) / kBlockThreads), dim3(kBlockThreads), 0, s, a);
+    KVH_HIP_CHECK_LAUNCH();
+  }
+  const dim3 grid((unsigned)p.items, (unsigned)a.heads);
+  if (dt == KVH_F16)
+    launch_kind<KVH_F16>(a, cache->kind, cache->head_dim, p.nr, grid, s);
+  else
+    launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, p.nr, grid, s);
+  KVH_HIP_CHECK_LAUNCH();
+  if (cut) {
+    if (dt == KVH_F16)
+      launch_join<KVH_F16>(a, cache->head_dim, 16 * p.nr, s);
+    else
+      launch_join<KVH_BF16>(a, cache->head_dim, 16 * p.nr, s);
+    KVH_HIP_CHECK_LAUNCH();
+  }
+  return KVH_OK;
+}
+
+}  // extern "C"
