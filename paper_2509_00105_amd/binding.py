@@ -157,7 +157,7 @@ def lib() -> ctypes.CDLL:
         if _fastcall is not None and _raw_stream is not None:
             _fast = _fastcall.Calls(torch.cuda.current_device, _raw_stream, *[
                 ctypes.cast(f, vp).value for f in (L.kvh_encode, L.kvh_encode_batch, L.kvh_decode, L.kvh_decode_batch,
-                                                   L.kvh_encode_kept, L.kvh_decode_kept)])
+                                                   L.kvh_encode_kept, L.kvh_decode_kept, L.kvh_append, L.kvh_attention)])
         _lib = L
     return _lib
 
@@ -591,7 +591,8 @@ def _cache(k_cache, v_cache, k_scale, v_scale, head_dim, dtype):
     if kind is None:
         raise ValueError("the cache must hold the type of the call, int8 or float8_e4m3fn")
     l, pages, block, c = k_cache.shape
-    if k_cache.stride(3) != 1 or (k_cache.stride(1) != k_cache.stride(2) * block and pages > 1):
+    row = k_cache.stride(2) if block > 1 else k_cache.stride(1) if pages > 1 else c
+    if k_cache.stride(3) != 1 or (pages > 1 and k_cache.stride(1) != row * block):
         raise ValueError("channel stride must be 1 and blocks of a paged cache densely packed")
     if head_dim < 1 or c % head_dim:
         raise ValueError("c must be a multiple of head_dim")
@@ -606,7 +607,7 @@ def _cache(k_cache, v_cache, k_scale, v_scale, head_dim, dtype):
         if k_scale.stride(2) != 1 and heads > 1:
             raise ValueError("the heads of a page's scales must be dense")
         ls, ps = k_scale.stride(0), k_scale.stride(1) if pages > 1 else heads
-    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), k_cache.stride(0), k_cache.stride(2) if block > 1 or pages > 1 else c,
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), k_cache.stride(0), row,
                   ls, ps, l, pages, block, heads, head_dim, kind)
 
 
@@ -654,6 +655,11 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     """kvh_append: K/V [l][T][c] of the requests' new tokens -> the pages of [l][P][block][c] caches (16-bit, int8 or float8_e4m3fn
     with scales [l][P][heads]).  K and q [l][T][q_heads * head_dim] are rotated by `rotation`, float32 [positions][rot]: cosines, then sines.
     Returns q_out (made here if none is given; may be q)."""
+    rc = _fast.append(k, v, k_cache, v_cache, starts, lens, page_table, max_new, head_dim, k_scale, v_scale, q, q_out, rotation, positions, pairs, status,
+                      stream) if _fast is not None else None
+    if rc is not None:
+        _check(rc, "kvh_append")
+        return q_out
     view, dt = _view(k, v)
     l, T, c = k.shape
     cache = _cache(k_cache, v_cache, k_scale, v_scale, head_dim, k.dtype)
@@ -679,8 +685,6 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
         rot = _Rotation(rotation.data_ptr(), _ptr(positions), rotation.stride(0), rotation.shape[0], rotation.shape[1], int(pairs))
     elif positions is not None:
         raise ValueError("positions without a rotation")
-    if q is not None and rotation is None:
-        raise ValueError("q is taken to be rotated: without a rotation it is used as it is")
     ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
     _check(lib().kvh_append(ctypes.byref(cache), ctypes.byref(req), dt, ctypes.byref(view), ref(rows), ref(out), q_heads, ref(rot), _ptr(status),
                             _stream_ptr(stream)), "kvh_append")
@@ -700,6 +704,11 @@ def attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lay
     """kvh_attention: queries [T][q_heads * head_dim] of the requests' new tokens over layer `layer` of the cache they were appended to.
     scale: head_dim ** -0.5 if not given.  lse: float32 [T][q_heads] or None.  workspace: uint8, kept by programs that call often (see
     attention_workspace); made here if none is given."""
+    rc = _fast.attention(q, k_cache, v_cache, layer, starts, lens, page_table, max_new, head_dim, k_scale, v_scale, scale, causal, sink, window, out, lse,
+                         workspace, status, stream) if _fast is not None and workspace is not None and out is not None else None
+    if rc is not None:
+        _check(rc, "kvh_attention")
+        return out
     _require_cuda(q, lse, workspace)
     if q.dtype not in _TORCH_DT:
         raise ValueError("q must be float16 or bfloat16")

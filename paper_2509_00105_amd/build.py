@@ -1,6 +1,7 @@
 """Build the HIP library (libkvh.so) in-tree for gfx950 with hipcc, and the binding's call module (_fastcall) with the C++ compiler."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shlex
 import shutil
@@ -14,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvh.so")
 CALLS = os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))  # for the interpreter that builds it alone
 SOURCES = ["kvh_api.hip", "kvh_decode.hip", "kvh_encode.hip", "kvh_transcode.hip", "kvh_loader.hip", "kvh_policy.cpp"]
-CACHE_SOURCES = ["kvh_append.hip", "kvh_attention.hip"]  # what reads a caller's cache as it is: NaN and infinities are values there
+CACHE_SOURCES = ["kvh_append.hip", "kvh_attention.hip", "kvh_attention_many.hip"]  # what reads a caller's cache as it is: NaN and infinities are values there
 
 # -ffp-contract=off: the codec's arithmetic fuses only where the source says fma.
 # -fno-honor-nans (the codec's sources only): inputs are finite by contract; without it every min/max of a value unpacked with
@@ -50,7 +51,9 @@ def _build_calls(verbose: bool) -> None:
     if not os.path.exists(os.path.join(include, "Python.h")) or not cxx or shutil.which(cxx[0]) is None:
         print("no Python.h or no C++ compiler: calls go through ctypes")
         return
-    _compile(CALLS, [*cxx, "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I", include, os.path.join(CSRC, "kvh_fastcall.cpp")], verbose)
+    spec = importlib.util.find_spec("torch")  # for one header, if it is there
+    torch_include = [arg for d in (spec.submodule_search_locations if spec else []) for arg in ("-isystem", os.path.join(d, "include"))]
+    _compile(CALLS, [*cxx, "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-I", include, *torch_include, os.path.join(CSRC, "kvh_fastcall.cpp")], verbose)
 
 
 def build(verbose: bool = False) -> str:

@@ -241,8 +241,8 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
           }
       }
       most = wave_max(most);
-      constexpr float kTop = KIND == KVH_CACHE_I8 ? 127.0f : 448.0f;
-      const float now = fmaxf(old, most < 0x1p-100f ? 0.0f : most / kTop);
+      constexpr float kPart = 1.0f / (KIND == KVH_CACHE_I8 ? 127.0f : 448.0f);
+      const float now = fmaxf(old, most < 0x1p-100f ? 0.0f : most * kPart);
       const float inv = now > 0.0f ? 1.0f / now : 0.0f;
       uint8_t* rows = cache + (int64_t)page * a.block_tokens * a.c_ts + col * 8;
       if (now > old && old > 0.0f) {  // earlier rows of the page under its new scale

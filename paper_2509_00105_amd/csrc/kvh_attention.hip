@@ -10,212 +10,10 @@
 // two of their row's own), the K scale of its page multiplies the finished dot product, and the V scale sv of its page enters the
 // exponent: with s' = s + log2 sv and m' = max s', the weight exp2(s' - m') <= 1 multiplies the code and exp2(s' - m') / sv adds
 // to the sum.  A weight is thus as exact as fp16 is, however the scales of a request's pages differ.
-#include "kvh_cache.hpp"
+#include "kvh_attention.hpp"
 
 namespace kvh {
 namespace {
-
-constexpr int kStep = 32;  // tokens a wave takes at once: two tiles of 16
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kLeastScale = 0x1p-60f;  // V scales below it keep it in the exponent; the rest goes onto the weight
-
-struct AttnParams {
-  Requests req;
-  const uint16_t* q;
-  uint16_t* out;
-  float* lse;
-  int64_t q_ts, o_ts;  // elements
-  const uint8_t *ck, *cv;  // of the layer
-  const float *sk, *sv;
-  int64_t c_ts, s_ps;
-  int pages, block_tokens, heads, group;
-  float scale;
-  int causal, sink, window;
-  int32_t* status;
-  float* part;       // partial outputs [slot][rows][D], then (maximum, sum) [slot][rows][2]; nullptr: nothing is split
-  float* part_ml;
-  int target;        // items that the batch is cut into, about
-  int least;         // steps of an item at least, where a request is cut
-  int64_t items;     // partial results that there is room for, of each head
-  Divisor by_block, by_group;
-};
-
-// ---- items --------------------------------------------------------------------------------------------------------
-// A request's rows come in tiles of `tile_rows`, its tokens in steps of 32, and an item is a tile and a run of `chunk` steps.  All
-// blocks work out the same list from the lengths: no block is idle while another has two requests' worth of tokens, and the host
-// need not know the lengths.
-__device__ __forceinline__ int steps_of(const AttnParams& a, const Request& rq, int tile_rows) {
-  if (!rq.ok || rq.n == 0) return 0;
-  const int all = (rq.len + kStep - 1) / kStep;
-  if (a.window == 0) return all;
-  const int64_t reach = (int64_t)a.window + tile_rows + 2 * kStep;  // of a tile's rows, with a step begun on either side
-  const int64_t some = reach / kStep + (a.sink + kStep - 1) / kStep;
-  return all < some ? all : (int)some;
-}
-
-struct Item {
-  int b, tile, part, parts;  // parts: of the request's tokens
-  int chunk;
-  Request rq;
-};
-
-__device__ __forceinline__ Request read_request(const AttnParams& a, int b) {
-  Request rq{0, 0, 0, false};
-  if (b < a.req.n) {
-    rq.start = a.req.starts[b];
-    const int32_t end = a.req.starts[b + 1];
-    rq.len = a.req.lens[b];
-    rq.n = end - rq.start;
-    rq.ok = request_ok(a.req, rq.start, end, rq.len);
-  }
-  return rq;
-}
-
-// Steps of an item, from the steps of the batch.
-__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows, int lane) {
-  if (a.part == nullptr) return 0x7fffffff;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
-    const Request rq = read_request(a, b0 + lane);
-    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
-    int64_t s = (int64_t)tiles * steps_of(a, rq, tile_rows);
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) s += __shfl_xor((long long)s, d);
-    total += s;
-  }
-  int64_t chunk = (total + a.target - 1) / a.target;
-  if (chunk < a.least) chunk = a.least;
-  chunk = (chunk + 3) & ~(int64_t)3;  // four waves share it
-  return chunk < 0x7fffffff ? (int)chunk : 0x7fffffff;
-}
-
-// The request whose item (or, with by_row, whose packed row) `want` is.  Returns false where there is none.
-__device__ __forceinline__ bool find_item(const AttnParams& a, int tile_rows, int64_t want, bool by_row, int lane, Item& it) {
-  it.chunk = chunk_of(a, tile_rows, lane);
-  int64_t base = 0;
-  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
-    const Request rq = read_request(a, b0 + lane);
-    const int steps = steps_of(a, rq, tile_rows);
-    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
-    int parts = steps == 0 ? 1 : 1 + (steps - 1) / it.chunk;
-    const int64_t mine = (int64_t)tiles * parts;
-    int64_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int64_t o = __shfl_up((long long)upto, d);
-      if (lane >= d) upto += o;
-    }
-    const bool here = by_row ? rq.ok && want >= rq.start && want < (int64_t)rq.start + rq.n
-                             : want >= base + upto - mine && want < base + upto;
-    const uint64_t who = __ballot(here);
-    if (who != 0) {
-      const int l = __builtin_ctzll(who);
-      it.b = b0 + l;
-      it.rq.start = uniform(__shfl(rq.start, l));
-      it.rq.n = uniform(__shfl(rq.n, l));
-      it.rq.len = uniform(__shfl(rq.len, l));
-      it.rq.ok = true;
-      it.parts = uniform(__shfl(parts, l));
-      const int64_t first = base + __shfl((long long)(upto - mine), l);
-      if (by_row) {
-        it.tile = 0;
-        it.part = (int)first;  // the request's first item
-      } else {
-        const int in = uniform((int)(want - first));
-        it.tile = in / it.parts;
-        it.part = in - it.tile * it.parts;
-      }
-      return true;
-    }
-    base += __shfl((long long)upto, kWave - 1);
-  }
-  return false;
-}
-
-// ---- operands -----------------------------------------------------------------------------------------------------
-template <int DT, int KIND>
-constexpr bool kBf16 = KIND == KVH_CACHE_16 && DT == KVH_BF16;  // the products' type; fp16 otherwise
-
-template <bool BF>
-__device__ __forceinline__ f32x4 mfma(const u32x4& x, const u32x4& y, const f32x4& c) {
-  if constexpr (BF)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
-}
-
-// bytes (lo, hi) of offset-binary codes q + 128 in the low byte of each half, 0x64 above: 1024 + 128 + q in fp16
-__device__ __forceinline__ uint32_t less_1152(uint32_t w) {
-  const f16x2 h = __builtin_bit_cast(f16x2, w), o = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-  return __builtin_bit_cast(uint32_t, h + o);
-}
-
-// 4 codes of one word -> 2 words of fp16 pairs, in order.
-template <int KIND>
-__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if constexpr (KIND == KVH_CACHE_I8) {
-    w ^= 0x80808080u;
-    lo = less_1152(__builtin_amdgcn_perm(0x64646464u, w, 0x04010400u));
-    hi = less_1152(__builtin_amdgcn_perm(0x64646464u, w, 0x04030402u));
-  } else {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
-  }
-}
-
-// The same 4 channels of two tokens x, y -> pairs (x, y) of each channel.
-template <int KIND>
-__device__ __forceinline__ void zip4(uint32_t x, uint32_t y, uint32_t (&p)[4]) {
-  widen4<KIND>(__builtin_amdgcn_perm(y, x, 0x05010400u), p[0], p[1]);
-  widen4<KIND>(__builtin_amdgcn_perm(y, x, 0x07030602u), p[2], p[3]);
-}
-
-template <int N>
-struct Words {
-  uint32_t w[N];
-};
-// N words from memory, in the widest accesses (N a power of two; the address is aligned to 4 N bytes, 16 at most).
-template <int N>
-__device__ __forceinline__ Words<N> fetch(const uint8_t* p) {
-  Words<N> r;
-  if constexpr (N == 1) {
-    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
-  } else if constexpr (N == 2) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-    r.w[0] = v[0], r.w[1] = v[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p + 16 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) r.w[4 * i + e] = v[e];
-    }
-  }
-  return r;
-}
-
-__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float over_groups_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
-}
-
-// ---- the page table, 64 entries at a time in the lanes ---------------------------------------------------------------
-struct PageRun {
-  int base, entry;  // entry of page base + lane; -1 where it is none of the cache's
-
-  __device__ __forceinline__ void load(const AttnParams& a, const int32_t* table, int first, int last, int lane) {
-    base = first;
-    entry = -1;
-    if (first + lane <= last) {
-      entry = table[first + lane];
-      if (entry >= a.pages) entry = -1;
-    }
-  }
-};
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------
 // NR tiles of 16 query rows share each K and V tile that is read.  PAGE16: pages hold a multiple of 16 tokens, so a tile lies on
@@ -278,16 +76,14 @@ struct Worker {
           for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
         }
         most = over_groups_max(most);
-        int ex = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
-        if (ex < -100 || ex > 127) ex = 0;  // nothing but zeros (or next to it); infinities stay what they are
-        const float down = __builtin_bit_cast(float, (uint32_t)(127 - (ex > 126 ? 126 : ex)) << 23), up = 1.0f / down;
-        coef[t] *= up;
+        const f32x2 power = row_power(most);
+        coef[t] *= power[1];
 #pragma unroll
         for (int kk = 0; kk < kSums; ++kk) {
           float x[8];
           widen8<DT>(raw[kk], x);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) q[t][kk][e] = narrow2<KVH_F16>(x[2 * e] * down, x[2 * e + 1] * down);
+          for (int e = 0; e < 4; ++e) q[t][kk][e] = narrow2<KVH_F16>(x[2 * e] * power[0], x[2 * e + 1] * power[0]);
         }
       } else {
 #pragma unroll
@@ -300,10 +96,6 @@ struct Worker {
     }
     bad = false;
     run.base = -1000;
-  }
-
-  __device__ __forceinline__ bool sees(int p, int token) const {
-    return token < end && (!a.causal || token <= p) && (a.window == 0 || token > p - a.window || token < a.sink);
   }
 
   // One step: tokens [t0, t0 + 32), t0 < end, a multiple of 32.
@@ -391,12 +183,8 @@ struct Worker {
     if constexpr (KIND != KVH_CACHE_16) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float z = lsv[i];
-        // a scale of zero (or next to it) keeps its tokens in the sum and takes their values off the weight
-        const float used = z < kLeastScale ? kLeastScale : z;
-        rest[i] = z < kLeastScale ? z * (1.0f / kLeastScale) : 1.0f;
-        lsv[i] = __builtin_amdgcn_logf(used);
-        inv[i] = __builtin_amdgcn_rcpf(used);
+        const ValueScale z(lsv[i]);
+        lsv[i] = z.log, inv[i] = z.inv, rest[i] = z.rest;
       }
     }
 
@@ -439,7 +227,7 @@ struct Worker {
       if (hidden_any) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const bool seen = sees(pos[t], t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
+          const bool seen = sees(a, end, pos[t], t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
           bad |= seen && none;
           if (!seen || none) x[i] = -INFINITY;
         }
@@ -486,7 +274,7 @@ struct Worker {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int e = 0; e < kVWords; ++e) odd |= has_odd(v[i].w[e]);
+          for (int e = 0; e < kVWords; ++e) odd |= has_odd<DT, KIND>(v[i].w[e]);
         if (__any(odd)) {
           one_by_one(w, table, t0);
           return;
@@ -512,18 +300,6 @@ struct Worker {
 #pragma unroll
         for (int t = 0; t < NR; ++t) o[t][c4 * kPer + j] = mfma<kBf>(vop, p[t], o[t][c4 * kPer + j]);
       }
-    }
-  }
-
-  static __device__ __forceinline__ bool has_odd(uint32_t w) {
-    if constexpr (KIND == KVH_CACHE_E4M3) {
-      bool odd = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= (w >> 8 * e & 0x7fu) == 0x7fu;
-      return odd;
-    } else {
-      constexpr uint32_t kExp = DT == KVH_BF16 ? 0x7f80u : 0x7c00u;
-      return (w & kExp) == kExp || (w >> 16 & kExp) == kExp;
     }
   }
 
@@ -562,7 +338,7 @@ struct Worker {
           }
 #pragma unroll
           for (int t = 0; t < NR; ++t)
-            if (sees(pos[t], tok)) {
+            if (sees(a, end, pos[t], tok)) {
 #pragma unroll
               for (int ct = 0; ct < kChans; ++ct) o[t][ct][r] = __builtin_fmaf(e[t], x[ct], o[t][ct][r]);
             }
@@ -584,11 +360,10 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
   __shared__ float lds[kWavesPerBlock * 16 * kPitch];
   __shared__ float lds_ml[kWavesPerBlock][kTile][2];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
-  const int head = blockIdx.y;
+  const uint32_t item = a.by_heads.quotient(blockIdx.x);  // the heads of an item run together: they read neighbouring memory
+  const int head = (int)(blockIdx.x - item * (uint32_t)a.heads);
   Item it;
-  if (!find_item(a, kTile, blockIdx.x, false, lane, it)) {
-    return;
-  }
+  if (!find_item(a, kTile, item, false, lane, it)) return;
   W w(a);
   w.lane = lane, w.l16 = lane % 16, w.grp = lane / 16;
   w.rq = it.rq;
@@ -600,21 +375,13 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
   w.p_most = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)(w.row0 + w.rows - 1));
   w.end = a.causal && w.p_most + 1 < it.rq.len ? w.p_most + 1 : it.rq.len;
   w.begin();
-  // The tile's steps: those of the first `sink` tokens, then those from the first row's window on.
-  int first = 0, sunk = 0;
-  if (a.window != 0) {
-    const int from = w.p_least - a.window + 1;
-    first = from > 0 ? from / kStep : 0;
-    sunk = (a.sink + kStep - 1) / kStep;
-    if (sunk >= first) first = sunk = 0;
-  }
-  const int steps = w.end > 0 ? sunk + (w.end + kStep - 1) / kStep - first : 0;
+  const Steps steps(a, w.p_least, w.end);
   const int64_t s0 = (int64_t)it.part * it.chunk;
-  const int64_t s1 = it.part + 1 == it.parts ? steps : s0 + it.chunk < steps ? s0 + it.chunk : steps;
+  const int64_t s1 = it.part + 1 == it.parts || s0 + it.chunk > steps.count ? steps.count : s0 + it.chunk;
   const int mine = s1 > s0 ? (int)((s1 - s0 + kWavesPerBlock - 1) / kWavesPerBlock) : 0;
   const int64_t b0 = s0 + (int64_t)wave * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
   const int32_t* table = a.req.table + (int64_t)it.b * a.req.table_stride;
-  for (int64_t s = b0; s < b1; ++s) w.step(table, (int)(s < sunk ? s : s - sunk + first) * kStep);
+  for (int64_t s = b0; s < b1; ++s) w.step(table, steps.token(s));
   if (__any(w.bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
   // The four waves' results become one.
@@ -627,7 +394,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
     }
   }
   const bool split = it.parts > 1;
-  const int64_t slot = (int64_t)blockIdx.x * a.heads + head;
+  const int64_t slot = blockIdx.x;
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     if (t * 16 >= w.rows) break;
@@ -734,26 +501,27 @@ __global__ __launch_bounds__(kBlockThreads) void refuse_kernel(AttnParams a) {
 constexpr int kTarget = 512;  // blocks of 4 waves that fill the chip: 2 on each compute unit
 
 struct Plan {
-  int nr;          // tiles of 16 rows
+  int nr;          // tiles of 16 rows of the kernel for few rows; 0: the kernel for many
+  int rows;        // of an item
   int64_t tiles;   // row tiles of the batch at most
   int64_t items;   // items at most, if requests are cut; the grid otherwise
   int target;      // what the kernel aims at
   size_t bytes;    // workspace of these items
 };
 
-size_t slot_bytes(int nr, int head_dim) { return (size_t)(16 * nr) * (head_dim + 2) * sizeof(float); }
+size_t slot_bytes(int rows, int head_dim) { return (size_t)rows * (head_dim + 2) * sizeof(float); }
 
 Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
   Plan p;
   const int64_t group = q_heads / heads;
   const int64_t most = (int64_t)(max_new < n_tokens ? max_new : n_tokens) * group;
-  p.nr = most <= 16 ? 1 : 2;
-  const int rows = 16 * p.nr;
-  p.tiles = (int64_t)n_tokens * group / rows + n_requests;
+  p.nr = most <= 16 ? 1 : most <= 32 ? 2 : 0;
+  p.rows = p.nr != 0 ? 16 * p.nr : kManyRows;
+  p.tiles = (int64_t)n_tokens * group / p.rows + n_requests;
   const int64_t aim = (kTarget + heads - 1) / heads;
   p.target = (int)aim;
   p.items = p.target + p.tiles;  // each tile's last chunk may be short
-  p.bytes = (size_t)p.items * heads * slot_bytes(p.nr, head_dim);
+  p.bytes = (size_t)p.items * heads * slot_bytes(p.rows, head_dim);
   return p;
 }
 
@@ -850,10 +618,11 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   a.status = status_dev;
   a.by_block = Divisor((uint32_t)cache->block_tokens);
   a.by_group = Divisor((uint32_t)a.group);
+  a.by_heads = Divisor((uint32_t)a.heads);
   if ((int64_t)a.req.max_new * a.group >= (int64_t)1 << 31) return KVH_E_SHAPE;
   Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim);
   // Requests are cut where the row tiles alone leave the chip idle and there is room for the parts.
-  const size_t one = (size_t)a.heads * slot_bytes(p.nr, cache->head_dim);
+  const size_t one = (size_t)a.heads * slot_bytes(p.rows, cache->head_dim);
   const size_t room = workspace_dev == nullptr ? 0 : workspace_bytes / one;
   bool cut = p.tiles * a.heads < 2 * kTarget;
   if (cut && room < (size_t)p.items) {
@@ -863,29 +632,31 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
       cut = false;
   }
   if (!cut) p.items = p.tiles;
-  if (p.items > 0x7fffffff) return KVH_E_SHAPE;
+  if (p.items * a.heads > 0x7fffffff) return KVH_E_SHAPE;
   a.target = p.target;
   a.items = p.items;
   a.least = 16;
   if (cut) {
     a.part = static_cast<float*>(workspace_dev);
-    a.part_ml = a.part + (size_t)p.items * a.heads * 16 * p.nr * cache->head_dim;
+    a.part_ml = a.part + (size_t)p.items * a.heads * p.rows * cache->head_dim;
   }
   if (status_dev != nullptr) {
     hipLaunchKernelGGL(refuse_kernel, dim3((a.req.n + kBlockThreads - 1) / kBlockThreads), dim3(kBlockThreads), 0, s, a);
     KVH_HIP_CHECK_LAUNCH();
   }
-  const dim3 grid((unsigned)p.items, (unsigned)a.heads);
-  if (dt == KVH_F16)
+  const dim3 grid((unsigned)(p.items * a.heads));
+  if (p.nr == 0)
+    launch_attention_many(a, dt, cache->kind, cache->head_dim, grid.x, s);
+  else if (dt == KVH_F16)
     launch_kind<KVH_F16>(a, cache->kind, cache->head_dim, p.nr, grid, s);
   else
     launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, p.nr, grid, s);
   KVH_HIP_CHECK_LAUNCH();
   if (cut) {
     if (dt == KVH_F16)
-      launch_join<KVH_F16>(a, cache->head_dim, 16 * p.nr, s);
+      launch_join<KVH_F16>(a, cache->head_dim, p.rows, s);
     else
-      launch_join<KVH_BF16>(a, cache->head_dim, 16 * p.nr, s);
+      launch_join<KVH_BF16>(a, cache->head_dim, p.rows, s);
     KVH_HIP_CHECK_LAUNCH();
   }
   return KVH_OK;
