@@ -36,7 +36,7 @@ struct Worker {
 
   u32x4 q[NR][kSums];
   float coef[NR];  // what turns a dot product into an exponent of 2
-  int pos[NR];
+  Sight sight[NR];
   f32x4 o[NR][kChans];
   float m[NR], l[NR];
   PageRun run;
@@ -56,7 +56,7 @@ struct Worker {
       const int r = t * 16 + l16;
       const bool real = r < rows;
       const int at = row0 + (real ? r : 0), token = (int)a.by_group.quotient((uint32_t)at), u = at - token * a.group;
-      pos[t] = rq.len - rq.n + token;
+      sight[t] = Sight(a, end, rq.len - rq.n + token);
       const uint16_t* src = a.q + ((int64_t)rq.start + token) * a.q_ts + ((int64_t)head * a.group + u) * D;
       float most = 0.0f;
       u32x4 raw[kSums];
@@ -95,7 +95,6 @@ struct Worker {
       for (int ct = 0; ct < kChans; ++ct) o[t][ct] = f32x4{0, 0, 0, 0};
     }
     bad = false;
-    run.base = -1000;
   }
 
   // One step: tokens [t0, t0 + 32), t0 < end, a multiple of 32.
@@ -227,7 +226,7 @@ struct Worker {
       if (hidden_any) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const bool seen = sees(a, end, pos[t], t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
+          const bool seen = sight[t].sees(a, t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
           bad |= seen && none;
           if (!seen || none) x[i] = -INFINITY;
         }
@@ -270,16 +269,35 @@ struct Worker {
         for (int e = 0; e < kVWords; ++e) v[i].w[e] = none ? 0u : v[i].w[e];
       }
       if constexpr (KIND != KVH_CACHE_I8) {
-        bool odd = false;  // an infinity or NaN among them
+        bool any = false;  // an infinity or NaN among them
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int e = 0; e < kVWords; ++e) odd |= has_odd<DT, KIND>(v[i].w[e]);
-        if (__any(odd)) {
-          one_by_one(w, table, t0);
+          for (int e = 0; e < kVWords; ++e) any |= has_odd<DT, KIND>(v[i].w[e]);
+        if (__any(any)) {
+          weigh<true>(v, p, t0);
           return;
         }
       }
+    }
+    weigh<false>(v, p, t0);
+  }
+
+  // The second product: ODD where some values are infinities or NaN that some rows do not see.
+  template <bool ODD>
+  __device__ __forceinline__ void weigh(const Words<kVWords> (&v)[8], const u32x4 (&p)[NR], int t0) {
+    using Bad = Odd<kBf>;
+    u32x4 one[ODD ? NR : 1];  // of the tokens that the lane's row sees
+    if constexpr (ODD) {
+#pragma unroll
+      for (int t = 0; t < NR; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          one[t][e] = 0;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+            if (sight[t].sees(a, t0 + 16 * (e / 2) + grp * 4 + 2 * (e % 2) + n)) one[t][e] |= Bad::kOne << 16 * n;
+        }
     }
 #pragma unroll
     for (int c4 = 0; c4 < kVWords; ++c4) {
@@ -298,56 +316,19 @@ struct Worker {
       for (int j = 0; j < kPer; ++j) {
         const u32x4 vop = {z[0][j], z[1][j], z[2][j], z[3][j]};
 #pragma unroll
-        for (int t = 0; t < NR; ++t) o[t][c4 * kPer + j] = mfma<kBf>(vop, p[t], o[t][c4 * kPer + j]);
-      }
-    }
-  }
-
-  // The weighted sum of a step whose tokens hold an infinity or NaN that some rows do not see: token by token in fp32, adding nothing
-  // to a row that does not see it.  Rare, and as slow as it looks: the values are read again, so that nothing has to stay in registers
-  // for it.
-  __device__ __forceinline__ void one_by_one(float (&w)[NR][8], const int32_t* table, int t0) {
+        for (int t = 0; t < NR; ++t) {
+          f32x4& to = o[t][c4 * kPer + j];
+          to = mfma<kBf>(ODD ? Bad::without(vop) : vop, p[t], to);
+          if constexpr (ODD) {
 #pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll 1
-      for (int g = 0; g < 4; ++g) {
-        const int tok = t0 + 16 * (i / 4) + g * 4 + i % 4;
-        if (tok >= end) continue;
-        const int at = (int)a.by_block.quotient((uint32_t)tok), page = table[at];
-        if (page < 0 || page >= a.pages) continue;
-        const int64_t row = (int64_t)page * a.block_tokens + (tok - at * a.block_tokens);
-        const uint8_t* src = a.cv + ((int64_t)head * D + row * a.c_ts + 4 * grp * kChans) * kWidth;
-        float e[NR];
+            for (int which = 0; which < 3; ++which) {
+              const f32x4 hit = mfma<kBf>(Bad::ones(vop, which), one[t], f32x4{0, 0, 0, 0});
 #pragma unroll
-        for (int t = 0; t < NR; ++t) e[t] = __shfl(w[t][0], g * 16 + l16);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {  // the lane holds of its row the channels (4 grp + r) kChans + ct
-          const Words<kVWords> raw = fetch<kVWords>(src + r * kChans * kWidth);
-          float x[kChans];
-#pragma unroll
-          for (int c = 0; c < kVWords; ++c) {
-            if constexpr (KIND == KVH_CACHE_16) {
-              x[2 * c] = t16_to_f32<DT>(raw.w[c] & 0xffffu);
-              x[2 * c + 1] = t16_to_f32<DT>(raw.w[c] >> 16);
-            } else if constexpr (KIND == KVH_CACHE_E4M3) {
-              x[4 * c] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 0);
-              x[4 * c + 1] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 1);
-              x[4 * c + 2] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 2);
-              x[4 * c + 3] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[c], 3);
+              for (int r = 0; r < 4; ++r) to[r] += hit[r] > 0.0f ? Bad::value(which) : 0.0f;
             }
           }
-#pragma unroll
-          for (int t = 0; t < NR; ++t)
-            if (sees(a, end, pos[t], tok)) {
-#pragma unroll
-              for (int ct = 0; ct < kChans; ++ct) o[t][ct][r] = __builtin_fmaf(e[t], x[ct], o[t][ct][r]);
-            }
         }
       }
-#pragma unroll
-      for (int t = 0; t < NR; ++t)
-#pragma unroll
-        for (int n = 0; n < 7; ++n) w[t][n] = w[t][n + 1];
     }
   }
 };
@@ -376,12 +357,12 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
   w.end = a.causal && w.p_most + 1 < it.rq.len ? w.p_most + 1 : it.rq.len;
   w.begin();
   const Steps steps(a, w.p_least, w.end);
-  const int64_t s0 = (int64_t)it.part * it.chunk;
-  const int64_t s1 = it.part + 1 == it.parts || s0 + it.chunk > steps.count ? steps.count : s0 + it.chunk;
-  const int mine = s1 > s0 ? (int)((s1 - s0 + kWavesPerBlock - 1) / kWavesPerBlock) : 0;
-  const int64_t b0 = s0 + (int64_t)wave * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
+  int s0, s1;
+  steps.part_of(it, s0, s1);
+  const int mine = (s1 - s0 + kWavesPerBlock - 1) / kWavesPerBlock;
+  const int b0 = s0 + wave * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
   const int32_t* table = a.req.table + (int64_t)it.b * a.req.table_stride;
-  for (int64_t s = b0; s < b1; ++s) w.step(table, steps.token(s));
+  for (int s = b0; s < b1; ++s) w.step(table, steps.token(s));
   if (__any(w.bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
   // The four waves' results become one.
@@ -465,7 +446,7 @@ __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int t
   const int token = (int)(packed - it.rq.start);
   const int64_t at = (int64_t)token * a.group + (u - head * a.group);
   const int tile = (int)(at / tile_rows), row = (int)(at - (int64_t)tile * tile_rows);
-  const int64_t slot0 = it.part + (int64_t)tile * it.parts;
+  const int64_t slot0 = it.part + (int64_t)(it.tiles - 1 - tile) * it.parts;
   if (slot0 + it.parts > a.items) return;  // requests that share rows of the batch: none of the kernel's
   constexpr int kPer = D / 64;
   float m = -INFINITY, l = 0.0f, x[kPer];

@@ -46,6 +46,7 @@ __device__ __forceinline__ int steps_of(const AttnParams& a, const Request& rq, 
 
 struct Item {
   int b, tile, part, parts;  // parts: of the request's tokens
+  int tiles;                 // of the request's rows; the last one, which sees the most tokens, comes first
   int chunk;
   Request rq;
 };
@@ -82,7 +83,7 @@ __device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows, int 
 
 // The request whose item (or, with by_row, whose packed row) `want` is.  Returns false where there is none.
 __device__ __forceinline__ bool find_item(const AttnParams& a, int tile_rows, int64_t want, bool by_row, int lane, Item& it) {
-  it.chunk = chunk_of(a, tile_rows, lane);
+  it.chunk = uniform(chunk_of(a, tile_rows, lane));
   int64_t base = 0;
   for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
     const Request rq = read_request(a, b0 + lane);
@@ -107,14 +108,15 @@ __device__ __forceinline__ bool find_item(const AttnParams& a, int tile_rows, in
       it.rq.len = uniform(__shfl(rq.len, l));
       it.rq.ok = true;
       it.parts = uniform(__shfl(parts, l));
+      it.tiles = uniform(__shfl(tiles, l));
       const int64_t first = base + __shfl((long long)(upto - mine), l);
       if (by_row) {
         it.tile = 0;
         it.part = (int)first;  // the request's first item
       } else {
         const int in = uniform((int)(want - first));
-        it.tile = in / it.parts;
-        it.part = in - it.tile * it.parts;
+        it.tile = it.tiles - 1 - in / it.parts;
+        it.part = in % it.parts;
       }
       return true;
     }
@@ -197,21 +199,30 @@ __device__ __forceinline__ float over_groups_sum(float v) {
 // ---- the page table, 64 entries at a time in the lanes ---------------------------------------------------------------
 struct PageRun {
   int base, entry;  // entry of page base + lane; -1 where it is none of the cache's
+  int ahead;        // the same of the 64 pages after those
 
+  __device__ __forceinline__ PageRun() : base(-1000), entry(-1), ahead(-1) {}
+  // Makes page `first` the run's first; pages past `last` are not looked at.
   __device__ __forceinline__ void load(const AttnParams& a, const int32_t* table, int first, int last, int lane) {
+    entry = first == base + kWave ? ahead : read(a, table, first + lane, last);
+    ahead = read(a, table, first + kWave + lane, last);
     base = first;
-    entry = -1;
-    if (first + lane <= last) {
-      entry = table[first + lane];
-      if (entry >= a.pages) entry = -1;
-    }
+  }
+  static __device__ __forceinline__ int read(const AttnParams& a, const int32_t* table, int at, int last) {
+    int e = -1;
+    if (at <= last) e = table[at];
+    return e < a.pages ? e : -1;
   }
 };
 
-// Whether a row at logical position p sees a token; `end` is past the last one that any row of the item sees.
-__device__ __forceinline__ bool sees(const AttnParams& a, int end, int p, int token) {
-  return token < end && (!a.causal || token <= p) && (a.window == 0 || token > p - a.window || token < a.sink);
-}
+// What a row at logical position p sees: tokens up to `last`, and of them those past `low` or before the sink's end.
+struct Sight {
+  int last, low;
+  __device__ __forceinline__ Sight() {}
+  // `end` is past the last token that any row of the item sees.
+  __device__ __forceinline__ Sight(const AttnParams& a, int end, int p) : last(a.causal && p < end ? p : end - 1), low(a.window != 0 ? p - a.window : -1) {}
+  __device__ __forceinline__ bool sees(const AttnParams& a, int token) const { return token <= last && (token > low || token < a.sink); }
+};
 
 // An item's steps: those of the first `sink` tokens, then those from its first row's window on.
 struct Steps {
@@ -226,7 +237,13 @@ struct Steps {
     }
     count = end > 0 ? sunk + (end + kStep - 1) / kStep - first : 0;
   }
-  __device__ __forceinline__ int token(int64_t step) const { return (int)(step < sunk ? step : step - sunk + first) * kStep; }
+  __device__ __forceinline__ int token(int step) const { return (step < sunk ? step : step - sunk + first) * kStep; }
+  // The steps [begin, end) of part `part` of `parts`, `chunk` steps each.
+  __device__ __forceinline__ void part_of(const Item& it, int& begin, int& end) const {
+    const int64_t b = (int64_t)it.part * it.chunk, e = b + it.chunk;
+    begin = uniform((int32_t)(b < count ? b : count));
+    end = uniform((int32_t)(it.part + 1 == it.parts || e > count ? count : e));
+  }
 };
 
 // Whether a word of values holds an infinity or NaN.
@@ -244,6 +261,28 @@ __device__ __forceinline__ bool has_odd(uint32_t w) {
     return false;
   }
 }
+
+// Operands of the second product where it holds an infinity or NaN that some rows do not see.  A weight of zero does not keep these from a row,
+// so they are taken out of the product, and what they do to the rows that see them comes from products of ones: where (ones of the tokens
+// that a row sees) x (ones where a value is NaN, or +infinity, or -infinity) is not zero, that value is added to the row's output.
+template <bool BF>
+struct Odd {
+  static constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u, kOne = BF ? 0x3f80u : 0x3c00u;
+  static __device__ __forceinline__ float value(int which) { return which == 0 ? NAN : which == 1 ? INFINITY : -INFINITY; }
+  static __device__ __forceinline__ uint32_t without(uint32_t w) {
+    return ((w & kExp) == kExp ? 0u : w & 0xffffu) | ((w >> 16 & kExp) == kExp ? 0u : w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ bool is(uint32_t h, int which) {
+    return which == 0 ? (h & 0x7fffu) > kExp : h == (which == 1 ? kExp : kExp | 0x8000u);
+  }
+  static __device__ __forceinline__ uint32_t ones(uint32_t w, int which) {
+    return (is(w & 0xffffu, which) ? kOne : 0u) | (is(w >> 16, which) ? kOne << 16 : 0u);
+  }
+  static __device__ __forceinline__ u32x4 without(const u32x4& v) { return u32x4{without(v[0]), without(v[1]), without(v[2]), without(v[3])}; }
+  static __device__ __forceinline__ u32x4 ones(const u32x4& v, int which) {
+    return u32x4{ones(v[0], which), ones(v[1], which), ones(v[2], which), ones(v[3], which)};
+  }
+};
 
 // A V scale as the softmax takes it: its logarithm goes into the exponent, its inverse into the sum; a scale of zero (or next to it) keeps
 // its tokens in the sum and takes their values off the weight.

@@ -35,99 +35,135 @@ template <int DT, int KIND, int D, bool PAGE16>
 struct Tiles {
   static constexpr bool kBf = kBf16<DT, KIND>;
   static constexpr int kWidth = KIND == KVH_CACHE_16 ? 2 : 1;
-  static constexpr int kSums = D / 16;                                         // matrix instructions of a dot product
-  static constexpr int kOuts = D / 32;                                         // channel tiles of the output
-  static constexpr int kKUnits = D * kWidth / 16;                              // 16-byte units of a token's K row in the cache
-  static constexpr int kKEach = kManyTokens * kKUnits / kBlockThreads;         // of them, those a thread moves
-  static constexpr int kVWords = kWidth;                                       // words of V (4 channels) that a thread moves of a token
-  static constexpr int kVThreads = 8 * (D / 4);                                // threads that move V: 8 tokens x 4 channels each
-  static constexpr int kKBytes = kManyTokens * D * 2, kVBytes = D * kManyTokens * 2;
-  static constexpr int kBuffer = kKBytes + kVBytes;
+  static constexpr int kSums = D / 16;                                  // matrix instructions of a dot product
+  static constexpr int kOuts = D / 32;                                  // channel tiles of the output
+  static constexpr int kKUnits = D * kWidth / 16;                       // 16-byte units of a token's K row in the cache
+  static constexpr int kKEach = kManyTokens * kKUnits / kBlockThreads;  // of them, those a thread moves
+  static constexpr int kVChans = D / 32;                                // channels of V that a thread moves, of 8 tokens
+  static constexpr int kVBytes = kVChans * kWidth;                      // 8, 4 or 2
+  static constexpr int kVWords = (kVBytes + 3) / 4;
+  static constexpr int kKTile = kManyTokens * D * 2, kVTile = D * kManyTokens * 2;
+  static constexpr int kBuffer = kKTile + kVTile;
+  static constexpr int kScales = KIND != KVH_CACHE_16 && !PAGE16 ? kManyTokens : 1;
 
   const AttnParams& a;
-  uint8_t* lds;          // two buffers
+  uint8_t* lds;                     // two buffers
   uint32_t (*odd)[kWavesPerBlock];  // of each buffer, by the wave that stored them: an infinity or NaN among its values
-  static constexpr int kScales = KIND != KVH_CACHE_16 && !PAGE16 ? kManyTokens : 1;
-  float (*scales)[3][kScales];  // of each buffer, where a tile's tokens lie on pages of any size: K scales, ValueScale's log and inv
+  float (*scales)[3][kScales];      // of each buffer, where a tile's tokens lie on pages of any size: K scales, ValueScale's log and inv
   const int32_t* table;
-  int head, end, lane;
+  int head, end, lane, wave;
   PageRun run;
+  uint32_t k_from, v_from;  // bytes from a group of 16 tokens' first row to what the thread moves of it (PAGE16)
 
   // what the thread has under way for the next tile
   u32x4 k[kKEach];
   uint32_t v[8][kVWords];
+  uint32_t none;         // of its 8 tokens of V, those past the end or on no page of the cache
   uint64_t absent;       // the tile's tokens on no page of the cache
-  float ks[4], vs[4];    // scales of its groups of 16 tokens (PAGE16), or of token `lane` in [0]
+  float ks[4], vs[4];    // scales of the tile's groups of 16 tokens (PAGE16), or of its token `lane` in [0]
 
   __device__ __forceinline__ Tiles(const AttnParams& a_) : a(a_) {}
 
   static __device__ __forceinline__ int k_place(int token, int unit) { return token * (D * 2) + ((unit ^ token & 7) << 4); }
-  // Rows (channels) are 8 units long.  The store puts rows 4 apart side by side, the operands take neighbouring rows: both differ in all
-  // three bits of this.
+  // Rows (channels) are 8 units long.  The store puts rows kVChans apart side by side, the operands take neighbouring rows: both differ in
+  // all three bits of this.
   static __device__ __forceinline__ int v_place(int ch, int unit) {
-    const int x = (ch >> 2 & 1) | ((ch ^ ch >> 3) & 1) << 1 | ((ch >> 1 ^ ch >> 4) & 1) << 2;
+    const int x = kVChans == 4 ? (ch >> 2 & 1) | ((ch ^ ch >> 3) & 1) << 1 | ((ch >> 1 ^ ch >> 4) & 1) << 2
+                               : (ch >> 1 & 1) | (ch >> 2 & 1) << 1 | ((ch ^ ch >> 3) & 1) << 2;
     return ch * (kManyTokens * 2) + ((unit ^ x) << 4);
   }
+  // Token of element e of unit u = 2 g + h: of the 16 tokens of group g, those whose weights lane half h holds.
+  static __device__ __forceinline__ int v_token(int u, int e) { return 16 * (u / 2) + 4 * (u % 2) + 8 * (e / 4) + e % 4; }
+  // The thread's unit of V and its first channel; a wave's units are those of one group of 16 tokens.
+  __device__ __forceinline__ int v_unit() const { return threadIdx.x / 32; }
+  __device__ __forceinline__ int v_chan() const { return threadIdx.x % 32 * kVChans; }
 
-  // Starts the loads of tokens [t0, t0 + 64), t0 < end.
+  __device__ __forceinline__ void begin() {
+    const uint32_t row_bytes = (uint32_t)a.c_ts * kWidth;
+    k_from = threadIdx.x / kKUnits % 16 * row_bytes + threadIdx.x % kKUnits * 16;
+    v_from = v_unit() % 2 * 4 * row_bytes + v_chan() * kWidth;
+  }
+
+  static __device__ __forceinline__ void fetch_v(uint32_t (&to)[kVWords], const uint8_t* p) {
+    if constexpr (kVBytes == 2) {
+      to[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else {
+      const Words<kVWords> w = fetch<kVWords>(p);
+#pragma unroll
+      for (int c = 0; c < kVWords; ++c) to[c] = w.w[c];
+    }
+  }
+
+  // Starts the loads of tokens [t0, t0 + 64), t0 < end.  Nothing here waits for them.
   __device__ __forceinline__ void fetch_tile(int t0) {
     const int last = end - 1, tid = threadIdx.x;
     const int tz = t0 + kManyTokens - 1 < last ? t0 + kManyTokens - 1 : last;
     const int at0 = (int)a.by_block.quotient((uint32_t)t0), at1 = (int)a.by_block.quotient((uint32_t)tz);
     if (at0 < run.base || at1 - run.base >= kWave) run.load(a, table, at0, (int)a.by_block.quotient((uint32_t)last), lane);
-    // the rows in the cache of tokens t0 + lane, in the lanes; a token past the end stands for the last one, one on no page for row 0
-    const int mine = t0 + lane < last ? t0 + lane : last, at = (int)a.by_block.quotient((uint32_t)mine);
-    const int page = __shfl(run.entry, at - run.base);
-    absent = __ballot(page < 0);
-    const int safe = page < 0 ? 0 : page, in_page = mine - at * a.block_tokens;
-    const int64_t head_at = (int64_t)head * D;
-    auto row_of = [&](int token) {  // of the tile's token (not of its page alone: any token's)
-      return (int64_t)__shfl(safe, token) * a.block_tokens + __shfl(in_page, token);
-    };
+    const int64_t row_bytes = a.c_ts * kWidth, head_at = (int64_t)head * D * kWidth;
+    const int u = v_unit();
+    none = 0;
+    if constexpr (PAGE16) {
+      // Each group of 16 tokens lies on one page: its rows past the end are the page's too, and only have to be kept from the sums.
+      absent = 0;
+      int64_t at[4];  // bytes to the group's first row
 #pragma unroll
-    for (int i = 0; i < kKEach; ++i) {
-      const int idx = tid + kBlockThreads * i, token = idx / kKUnits, unit = idx % kKUnits;
-      k[i] = *reinterpret_cast<const u32x4*>(a.ck + (row_of(token) * a.c_ts + head_at) * kWidth + unit * 16);
+      for (int g = 0; g < 4; ++g) {
+        const int t = t0 + 16 * g <= last ? t0 + 16 * g : last & ~15;  // a group past the end stands for the last one
+        const int in = (int)a.by_block.quotient((uint32_t)t);
+        int page = uniform(__builtin_amdgcn_readlane(run.entry, in - run.base));
+        if (page < 0) {
+          page = 0;
+          absent |= (uint64_t)0xffff << 16 * g;
+        }
+        at[g] = ((int64_t)page * a.block_tokens + (t - in * a.block_tokens)) * row_bytes + head_at;
+        if constexpr (KIND != KVH_CACHE_16) {
+          ks[g] = a.sk[(int64_t)page * a.s_ps + head];
+          vs[g] = a.sv[(int64_t)page * a.s_ps + head];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kKEach; ++i) {
+        constexpr int kWaveTokens = kWave / kKUnits, kStride = kBlockThreads / kKUnits;  // of an access
+        const int g = (wave * kWaveTokens + i * kStride) / 16;
+        const int64_t from = g == 0 ? at[0] : g == 1 ? at[1] : g == 2 ? at[2] : at[3];
+        k[i] = *reinterpret_cast<const u32x4*>(a.ck + from + k_from);
+      }
+      const uint8_t* vg = a.cv + (wave == 0 ? at[0] : wave == 1 ? at[1] : wave == 2 ? at[2] : at[3]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) fetch_v(v[e], vg + (8 * (e / 4) + e % 4) * row_bytes + v_from);
+    } else {
+      // the bytes to the rows of tokens t0 + lane, in the lanes; a token past the end stands for the last one, one on no page for row 0
+      const int mine = t0 + lane < last ? t0 + lane : last, in = (int)a.by_block.quotient((uint32_t)mine);
+      const int page = __shfl(run.entry, in - run.base);
+      absent = __ballot(page < 0);
+      const int64_t at = page < 0 ? head_at : ((int64_t)page * a.block_tokens + (mine - in * a.block_tokens)) * row_bytes + head_at;
+#pragma unroll
+      for (int i = 0; i < kKEach; ++i) {
+        const int idx = tid + kBlockThreads * i;
+        k[i] = *reinterpret_cast<const u32x4*>(a.ck + __shfl((long long)at, idx / kKUnits) + idx % kKUnits * 16);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) fetch_v(v[e], a.cv + __shfl((long long)at, v_token(u, e)) + v_chan() * kWidth);
+      if constexpr (KIND != KVH_CACHE_16) {
+        const int64_t p = page < 0 ? 0 : page;
+        ks[0] = a.sk[p * a.s_ps + head];
+        vs[0] = a.sv[p * a.s_ps + head];
+      }
     }
-    const int u = tid / (D / 4), ch = tid % (D / 4) * 4;  // V: unit of 8 tokens, channels
-    if (kVThreads == kBlockThreads || u < 8) {
+    if (t0 + kManyTokens > end || absent != 0) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int token = v_token(u, e);
-        const uint8_t* src = a.cv + (row_of(token) * a.c_ts + head_at + ch) * kWidth;
-        const Words<kVWords> w = fetch<kVWords>(src);
-        const bool none = t0 + token >= end || (absent >> token & 1) != 0;  // must not reach any row
-#pragma unroll
-        for (int c = 0; c < kVWords; ++c) v[e][c] = none ? 0u : w.w[c];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int c = 0; c < kVWords; ++c) v[e][c] = 0;
-    }
-    if constexpr (KIND != KVH_CACHE_16) {
-      if constexpr (PAGE16) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int64_t p = uniform(__builtin_amdgcn_readlane(safe, 16 * g));
-          ks[g] = a.sk[p * a.s_ps + head];
-          vs[g] = a.sv[p * a.s_ps + head];
-        }
-      } else {
-        ks[0] = a.sk[(int64_t)safe * a.s_ps + head];
-        vs[0] = a.sv[(int64_t)safe * a.s_ps + head];
+        const int t = v_token(u, 0), more = v_token(0, e);  // what differs from thread to thread, and what does not
+        if (t0 + t + more >= end || (absent >> t >> more & 1) != 0) none |= 1u << e;
       }
     }
   }
 
-  // Token of element e of unit u = 2 g + h: of the 16 tokens of group g, those whose weights lane half h holds.
-  static __device__ __forceinline__ int v_token(int u, int e) { return 16 * (u / 2) + 4 * (u % 2) + 8 * (e / 4) + e % 4; }
-
   // Stores what was fetched into a buffer, as operands.
   __device__ __forceinline__ void store_tile(int buffer) {
     uint8_t* kb = lds + buffer * kBuffer;
-    uint8_t* vb = kb + kKBytes;
+    uint8_t* vb = kb + kKTile;
     const int tid = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < kKEach; ++i) {
@@ -144,24 +180,31 @@ struct Tiles {
         }
       }
     }
-    const int u = tid / (D / 4), ch = tid % (D / 4) * 4;
-    if (kVThreads == kBlockThreads || u < 8) {
-      uint32_t z[4][4];  // pairs of tokens, of each channel
+    if (__any(none != 0)) {  // what no row may meet
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (KIND == KVH_CACHE_16) {
+      for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            z[e][2 * c] = __builtin_amdgcn_perm(v[2 * e + 1][c], v[2 * e][c], 0x05040100u);
-            z[e][2 * c + 1] = __builtin_amdgcn_perm(v[2 * e + 1][c], v[2 * e][c], 0x07060302u);
-          }
-        } else {
-          zip4<KIND>(v[2 * e][0], v[2 * e + 1][0], z[e]);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(vb + v_place(ch + j, u)) = u32x4{z[0][j], z[1][j], z[2][j], z[3][j]};
+        for (int c = 0; c < kVWords; ++c) v[e][c] = none >> e & 1 ? 0u : v[e][c];
     }
+    const int u = v_unit(), ch = v_chan();
+    uint32_t z[4][kVChans];  // pairs of tokens, of each channel
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t(&x)[kVWords] = v[2 * e], (&y)[kVWords] = v[2 * e + 1];
+      if constexpr (KIND == KVH_CACHE_16) {
+#pragma unroll
+        for (int c = 0; c < kVWords; ++c) {
+          z[e][2 * c] = __builtin_amdgcn_perm(y[c], x[c], 0x05040100u);
+          z[e][2 * c + 1] = __builtin_amdgcn_perm(y[c], x[c], 0x07060302u);
+        }
+      } else if constexpr (kVChans == 4) {
+        zip4<KIND>(x[0], y[0], z[e]);
+      } else {
+        widen4<KIND>(__builtin_amdgcn_perm(y[0], x[0], 0x05010400u), z[e][0], z[e][1]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kVChans; ++j) *reinterpret_cast<u32x4*>(vb + v_place(ch + j, u)) = u32x4{z[0][j], z[1][j], z[2][j], z[3][j]};
     if constexpr (KIND != KVH_CACHE_I8) {
       bool any = false;
 #pragma unroll
@@ -169,14 +212,14 @@ struct Tiles {
 #pragma unroll
         for (int c = 0; c < kVWords; ++c) any |= has_odd<DT, KIND>(v[e][c]);
       any = __any(any);
-      if (lane == 0) odd[buffer][tid / kWave] = any;
+      if (lane == 0) odd[buffer][wave] = any;
     }
     if constexpr (KIND != KVH_CACHE_16 && !PAGE16) {
       if (tid < kManyTokens) {
-        const ValueScale z(vs[0]);
+        const ValueScale z2(vs[0]);
         scales[buffer][0][tid] = ks[0];
-        scales[buffer][1][tid] = z.log;
-        scales[buffer][2][tid] = z.inv;
+        scales[buffer][1][tid] = z2.log;
+        scales[buffer][2][tid] = z2.inv;
       }
     }
   }
@@ -204,8 +247,8 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   const int p_last = before + (int)a.by_group.quotient((uint32_t)(row0 + block_rows - 1));
   const int end = a.causal && p_last + 1 < rq.len ? p_last + 1 : rq.len;
   const Steps steps(a, p_first, end);
-  const int64_t s0 = (int64_t)it.part * it.chunk;
-  const int64_t s1 = it.part + 1 == it.parts || s0 + it.chunk > steps.count ? steps.count : s0 + it.chunk;
+  int s0, s1;
+  steps.part_of(it, s0, s1);
 
   // The lane's row, and the positions of the wave's rows.
   const int wave_row = row0 + wave * kManyWaveRows;
@@ -213,6 +256,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   const bool works = wave_rows > 0, real = col < wave_rows;
   const int at = real ? wave_row + col : row0, token = (int)a.by_group.quotient((uint32_t)at), u = at - token * a.group;
   const int pos = before + token;
+  const Sight sight(a, end, pos);
   const int p_least = works ? before + (int)a.by_group.quotient((uint32_t)wave_row) : 0;
   const int p_most = works ? before + (int)a.by_group.quotient((uint32_t)(wave_row + wave_rows - 1)) : 0;
 
@@ -258,14 +302,15 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   T t(a);
   t.lds = lds, t.odd = odd, t.scales = scales, t.lane = lane, t.head = head, t.end = end;
   t.table = a.req.table + (int64_t)it.b * a.req.table_stride;
-  t.run.base = -1000;
+  t.wave = wave;
+  t.begin();
   if (s0 < s1) t.fetch_tile(steps.token(s0));
   // Where the lane's operands lie in a buffer: those of a row differ in the unit's low bits, the rest is the same for all lanes.
   int k_at[4], v_at[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) k_at[e] = T::k_place(col, 2 * e + half), v_at[e] = T::v_place(col, 2 * e + half);
   int buffer = 0;
-  for (int64_t s = s0; s < s1; s += 2, buffer ^= 1) {
+  for (int s = s0; s < s1; s += 2, buffer ^= 1) {
     const int t0 = steps.token(s);
     t.store_tile(buffer);
     const uint64_t absent = t.absent;
@@ -288,7 +333,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
     const bool blank = !works || (a.causal && t0 > p_most);  // no row of the wave sees any of it
     if (!blank) {
       const uint8_t* kb = lds + buffer * T::kBuffer;
-      const uint8_t* vb = kb + T::kKBytes;
+      const uint8_t* vb = kb + T::kKTile;
       bool slow = false;
       if constexpr (KIND != KVH_CACHE_I8) slow = hidden && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3]) != 0;
 #pragma unroll
@@ -296,9 +341,23 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
         f32x16 x;
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[j] = 0.0f;
+        u32x4 kf[T::kSums], vf[2 * T::kOuts];
 #pragma unroll
-        for (int kk = 0; kk < T::kSums; ++kk)
-          x = mfma32<T::kBf>(*reinterpret_cast<const u32x4*>(kb + k_at[kk % 4] + i * (32 * D * 2) + kk / 4 * 128), q[kk], x);
+        for (int kk = 0; kk < T::kSums; ++kk) kf[kk] = *reinterpret_cast<const u32x4*>(kb + k_at[kk % 4] + i * (32 * D * 2) + kk / 4 * 128);
+#pragma unroll
+        for (int kk = 0; kk < T::kSums; ++kk) x = mfma32<T::kBf>(kf[kk], q[kk], x);
+        // Operands are read ahead of the instructions that take them: four of K first, then one with each product.
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int kk = 4; kk < T::kSums; ++kk) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        // and the first of V before the softmax
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vf[e] = *reinterpret_cast<const u32x4*>(vb + v_at[2 * i + e % 2] + e / 2 * (32 * kManyTokens * 2));
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (kScaled) {
 #pragma unroll
           for (int j4 = 0; j4 < 4; ++j4) {
@@ -319,8 +378,8 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
         if (hidden) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const int in = 32 * i + 8 * (j / 4) + 4 * half + j % 4;
-            const bool seen = sees(a, end, pos, t0 + in), none = (absent >> in & 1) != 0;
+            const int in = 32 * i + 8 * (j / 4) + j % 4;  // and 4 half more
+            const bool seen = sight.sees(a, t0 + 4 * half + in), none = (absent >> 4 * half >> in & 1) != 0;
             bad |= seen && none;
             x[j] = !seen || none ? -INFINITY : x[j] * unit;
           }
@@ -371,54 +430,47 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
             }
           }
         }
+        u32x4 p[2];  // of each 16 tokens: the lane's 8 weights
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[g][e] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(x[8 * g + 2 * e], x[8 * g + 2 * e + 1]);
+        using Bad = Odd<T::kBf>;
+#pragma unroll
+        for (int e = 4; e < 2 * T::kOuts; ++e) vf[e] = *reinterpret_cast<const u32x4*>(vb + v_at[2 * i + e % 2] + e / 2 * (32 * kManyTokens * 2));
         if (slow) {
-          // An infinity or NaN that some rows do not see: token by token in fp32, nothing added to a row that does not see it.
-#pragma unroll 1
-          for (int n = 0; n < 32; ++n) {
-            const int h = n % 2, j = n / 2, tok = t0 + 32 * i + 8 * (j / 4) + 4 * h + j % 4;
-            const float w = __shfl(x[0], h * 32 + col);
-            if (h == 1) {
 #pragma unroll
-              for (int e = 0; e < 15; ++e) x[e] = x[e + 1];
-            }
-            if (tok >= end) continue;
-            const int in = (int)a.by_block.quotient((uint32_t)tok), page = t.table[in];
-            if (page < 0 || page >= a.pages) continue;
-            const int64_t row = (int64_t)page * a.block_tokens + (tok - in * a.block_tokens);
-            const uint8_t* src = a.cv + (row * a.c_ts + (int64_t)head * D + 4 * half) * T::kWidth;
-            const bool seen = sees(a, end, pos, tok);
+          for (int e = 0; e < 2 * T::kOuts; ++e) vf[e] = Bad::without(vf[e]);
+        }
 #pragma unroll
-            for (int c = 0; c < T::kOuts; ++c)
-#pragma unroll
-              for (int j4 = 0; j4 < 4; ++j4) {
-                const Words<T::kVWords> raw = fetch<T::kVWords>(src + (32 * c + 8 * j4) * T::kWidth);
-                float y[4];
-                if constexpr (KIND == KVH_CACHE_16) {
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) y[e] = t16_to_f32<DT>(raw.w[e / 2] >> 16 * (e % 2) & 0xffffu);
-                } else {
-                  y[0] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[0], 0);
-                  y[1] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[0], 1);
-                  y[2] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[0], 2);
-                  y[3] = __builtin_amdgcn_cvt_f32_fp8((int)raw.w[0], 3);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (seen) o[c][4 * j4 + e] = __builtin_fmaf(w, y[e], o[c][4 * j4 + e]);
-                __builtin_amdgcn_sched_barrier(0);  // one after the other: the registers are the other path's
-              }
-          }
-        } else {
-          u32x4 p[2];  // of each 16 tokens: the lane's 8 weights
+        for (int e = 0; e < 2 * T::kOuts; ++e) o[e / 2] = mfma32<T::kBf>(vf[e], p[e % 2], o[e / 2]);
+        if (slow) {
+          u32x4 one[2];  // of the tokens that the lane's row sees
 #pragma unroll
           for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[g][e] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(x[8 * g + 2 * e], x[8 * g + 2 * e + 1]);
+            for (int e = 0; e < 4; ++e) {
+              one[g][e] = 0;
 #pragma unroll
-          for (int c = 0; c < T::kOuts; ++c)
+              for (int n = 0; n < 2; ++n) {
+                const int j = 8 * g + 2 * e + n;
+                if (sight.sees(a, t0 + 4 * half + 32 * i + 8 * (j / 4) + j % 4)) one[g][e] |= Bad::kOne << 16 * n;
+              }
+            }
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
-              o[c] = mfma32<T::kBf>(*reinterpret_cast<const u32x4*>(vb + v_at[2 * i + g] + c * (32 * kManyTokens * 2)), p[g], o[c]);
+          for (int c = 0; c < T::kOuts; ++c) {
+#pragma unroll 1
+            for (int which = 0; which < 3; ++which) {
+              f32x16 hit;
+#pragma unroll
+              for (int j = 0; j < 16; ++j) hit[j] = 0.0f;
+#pragma unroll
+              for (int g = 0; g < 2; ++g)
+                hit = mfma32<T::kBf>(Bad::ones(*reinterpret_cast<const u32x4*>(vb + v_at[2 * i + g] + c * (32 * kManyTokens * 2)), which), one[g], hit);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[c][j] += hit[j] > 0.0f ? Bad::value(which) : 0.0f;
+            }
+          }
         }
       }
     }
