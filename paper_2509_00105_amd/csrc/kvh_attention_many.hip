@@ -53,13 +53,18 @@ struct Tiles {
   const int32_t* table;
   int head, end, lane, wave;
   PageRun run;
-  uint32_t k_from, v_from;  // bytes from a group of 16 tokens' first row to what the thread moves of it (PAGE16)
+  // PAGE16: bytes from a group of 16 tokens' first row to what the thread moves of it, and where the next group lies: in the
+  // request's page `in`, `past` bytes (and `row` rows) from its start.
+  uint32_t k_from, v_from;
+  int in, row;
+  int64_t past;
 
   // what the thread has under way for the next tile
   u32x4 k[kKEach];
   uint32_t v[8][kVWords];
   uint32_t none;         // of its 8 tokens of V, those past the end or on no page of the cache
   uint64_t absent;       // the tile's tokens on no page of the cache
+  bool edge;             // some row of the block does not see all of the tile
   float ks[4], vs[4];    // scales of the tile's groups of 16 tokens (PAGE16), or of its token `lane` in [0]
 
   __device__ __forceinline__ Tiles(const AttnParams& a_) : a(a_) {}
@@ -94,33 +99,43 @@ struct Tiles {
     }
   }
 
-  // Starts the loads of tokens [t0, t0 + 64), t0 < end.  Nothing here waits for them.
-  __device__ __forceinline__ void fetch_tile(int t0) {
+  // The next tile is that of tokens t0 and on.
+  __device__ __forceinline__ void seek(int t0) {
+    in = (int)a.by_block.quotient((uint32_t)t0);
+    row = t0 - in * a.block_tokens;
+    past = (int64_t)row * (a.c_ts * kWidth);
+  }
+
+  // Starts the loads of tokens [t0, t0 + 64), t0 < end, where seek or the tile before left off.  Nothing here waits for them.
+  __device__ __forceinline__ void fetch_tile(int t0, int p_first) {
     const int last = end - 1, tid = threadIdx.x;
-    const int tz = t0 + kManyTokens - 1 < last ? t0 + kManyTokens - 1 : last;
-    const int at0 = (int)a.by_block.quotient((uint32_t)t0), at1 = (int)a.by_block.quotient((uint32_t)tz);
-    if (at0 < run.base || at1 - run.base >= kWave) run.load(a, table, at0, (int)a.by_block.quotient((uint32_t)last), lane);
     const int64_t row_bytes = a.c_ts * kWidth, head_at = (int64_t)head * D * kWidth;
     const int u = v_unit();
     none = 0;
     if constexpr (PAGE16) {
       // Each group of 16 tokens lies on one page: its rows past the end are the page's too, and only have to be kept from the sums.
       absent = 0;
+      if ((unsigned)(in - run.base) > (unsigned)(kWave - 4)) run.load(a, table, in, (int)a.by_block.quotient((uint32_t)last), lane);
       int64_t at[4];  // bytes to the group's first row
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int t = t0 + 16 * g <= last ? t0 + 16 * g : last & ~15;  // a group past the end stands for the last one
-        const int in = (int)a.by_block.quotient((uint32_t)t);
+        if (g > 0 && t0 + 16 * g > last) {  // a group past the end stands for the one before
+          at[g] = at[g - 1];
+          ks[g] = ks[g - 1], vs[g] = vs[g - 1];
+          continue;
+        }
         int page = uniform(__builtin_amdgcn_readlane(run.entry, in - run.base));
         if (page < 0) {
           page = 0;
           absent |= (uint64_t)0xffff << 16 * g;
         }
-        at[g] = ((int64_t)page * a.block_tokens + (t - in * a.block_tokens)) * row_bytes + head_at;
+        at[g] = (int64_t)page * a.block_tokens * row_bytes + past + head_at;
         if constexpr (KIND != KVH_CACHE_16) {
           ks[g] = a.sk[(int64_t)page * a.s_ps + head];
           vs[g] = a.sv[(int64_t)page * a.s_ps + head];
         }
+        row += 16, past += 16 * row_bytes;
+        if (row == a.block_tokens) row = 0, past = 0, ++in;
       }
 #pragma unroll
       for (int i = 0; i < kKEach; ++i) {
@@ -133,6 +148,9 @@ struct Tiles {
 #pragma unroll
       for (int e = 0; e < 8; ++e) fetch_v(v[e], vg + (8 * (e / 4) + e % 4) * row_bytes + v_from);
     } else {
+      const int tz = t0 + kManyTokens - 1 < last ? t0 + kManyTokens - 1 : last;
+      const int at0 = (int)a.by_block.quotient((uint32_t)t0), at1 = (int)a.by_block.quotient((uint32_t)tz);
+      if (at0 < run.base || at1 - run.base >= kWave) run.load(a, table, at0, (int)a.by_block.quotient((uint32_t)last), lane);
       // the bytes to the rows of tokens t0 + lane, in the lanes; a token past the end stands for the last one, one on no page for row 0
       const int mine = t0 + lane < last ? t0 + lane : last, in = (int)a.by_block.quotient((uint32_t)mine);
       const int page = __shfl(run.entry, in - run.base);
@@ -151,13 +169,51 @@ struct Tiles {
         vs[0] = a.sv[p * a.s_ps + head];
       }
     }
-    if (t0 + kManyTokens > end || absent != 0) {
+    edge = t0 + kManyTokens > end || absent != 0 || (a.causal && t0 + kManyTokens - 1 > p_first) || a.window != 0;
+    if (edge) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int t = v_token(u, 0), more = v_token(0, e);  // what differs from thread to thread, and what does not
         if (t0 + t + more >= end || (absent >> t >> more & 1) != 0) none |= 1u << e;
       }
     }
+  }
+
+  static __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+    if constexpr (KIND == KVH_CACHE_16) {
+      return Odd<kBf>::without(w);
+    } else {  // a code of NaN becomes one of zero
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((w >> 8 * e & 0x7fu) == 0x7fu) w &= ~(0xffu << 8 * e);
+      return w;
+    }
+  }
+
+  // The operand of the second product for channel 32 c + l of lane half h and group g of the tile at t0, again from the cache: ones where a
+  // value is the `which`th odd one.
+  __device__ __forceinline__ u32x4 odd_ones(int t0, int c, int g, int which) const {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = 0;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int tok = t0 + v_token(2 * g + lane / 32, 2 * e + n);
+        if (tok >= end) continue;
+        const int p = (int)a.by_block.quotient((uint32_t)tok), page = table[p];
+        if (page < 0 || page >= a.pages) continue;
+        const int64_t row = (int64_t)page * a.block_tokens + (tok - p * a.block_tokens);
+        const uint8_t* src = a.cv + (row * a.c_ts + (int64_t)head * D + 32 * c + lane % 32) * kWidth;
+        bool is;
+        if constexpr (KIND == KVH_CACHE_16)
+          is = Odd<kBf>::is(*reinterpret_cast<const uint16_t*>(src), which);
+        else
+          is = which == 0 && (*src & 0x7fu) == 0x7fu;
+        if (is) w[e] |= Odd<kBf>::kOne << 16 * n;
+      }
+    }
+    return w;
   }
 
   // Stores what was fetched into a buffer, as operands.
@@ -187,6 +243,24 @@ struct Tiles {
         for (int c = 0; c < kVWords; ++c) v[e][c] = none >> e & 1 ? 0u : v[e][c];
     }
     const int u = v_unit(), ch = v_chan();
+    if constexpr (KIND != KVH_CACHE_I8) {
+      // Where some row does not see all of the tile, its infinities and NaN stay out of the product: see Odd.
+      bool any = false;
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int c = 0; c < kVWords; ++c) any |= has_odd<DT, KIND>(v[e][c]);
+        any = __any(any);
+      }
+      if (lane == 0) odd[buffer][wave] = any;
+      if (any) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int c = 0; c < kVWords; ++c) v[e][c] = without_odd(v[e][c]);
+      }
+    }
     uint32_t z[4][kVChans];  // pairs of tokens, of each channel
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -203,17 +277,28 @@ struct Tiles {
         widen4<KIND>(__builtin_amdgcn_perm(y[0], x[0], 0x05010400u), z[e][0], z[e][1]);
       }
     }
+    if constexpr (KIND != KVH_CACHE_16) {
+      // Scales below the least that the exponent takes: the rest goes onto the values.
+      bool faint = false;
+#pragma unroll
+      for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) faint |= vs[g] < kLeastScale;
+      if (__any(faint)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float r[2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const float s = PAGE16 ? (wave == 0 ? vs[0] : wave == 1 ? vs[1] : wave == 2 ? vs[2] : vs[3]) : __shfl(vs[0], v_token(u, 2 * e + n));
+            r[n] = ValueScale(s).rest;
+          }
+          const f16x2 by = __builtin_bit_cast(f16x2, narrow2<KVH_F16>(r[0], r[1]));
+#pragma unroll
+          for (int j = 0; j < kVChans; ++j) z[e][j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, z[e][j]) * by);
+        }
+      }
+    }
 #pragma unroll
     for (int j = 0; j < kVChans; ++j) *reinterpret_cast<u32x4*>(vb + v_place(ch + j, u)) = u32x4{z[0][j], z[1][j], z[2][j], z[3][j]};
-    if constexpr (KIND != KVH_CACHE_I8) {
-      bool any = false;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int c = 0; c < kVWords; ++c) any |= has_odd<DT, KIND>(v[e][c]);
-      any = __any(any);
-      if (lane == 0) odd[buffer][wave] = any;
-    }
     if constexpr (KIND != KVH_CACHE_16 && !PAGE16) {
       if (tid < kManyTokens) {
         const ValueScale z2(vs[0]);
@@ -261,13 +346,14 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   const int p_most = works ? before + (int)a.by_group.quotient((uint32_t)(wave_row + wave_rows - 1)) : 0;
 
   u32x4 q[T::kSums];
-  float coef = a.scale * kLog2e;
+  float coef = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // positive, also where the scale is 0: see f below
   {
+    const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
     const uint16_t* src = a.q + ((int64_t)rq.start + token) * a.q_ts + ((int64_t)head * a.group + u) * D;
 #pragma unroll
     for (int kk = 0; kk < T::kSums; ++kk) {
       q[kk] = u32x4{0, 0, 0, 0};
-      if (real) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * 16 + half * 8);
+      if (real) q[kk] = *reinterpret_cast<const u32x4*>(src + kk * 16 + half * 8) ^ sign;
     }
     if constexpr (kScaled && DT == KVH_BF16) {
       float most = 0.0f;
@@ -304,7 +390,10 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   t.table = a.req.table + (int64_t)it.b * a.req.table_stride;
   t.wave = wave;
   t.begin();
-  if (s0 < s1) t.fetch_tile(steps.token(s0));
+  if (s0 < s1) {
+    t.seek(steps.token(s0));
+    t.fetch_tile(steps.token(s0), p_first);
+  }
   // Where the lane's operands lie in a buffer: those of a row differ in the unit's low bits, the rest is the same for all lanes.
   int k_at[4], v_at[4];
 #pragma unroll
@@ -314,149 +403,165 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
     const int t0 = steps.token(s);
     t.store_tile(buffer);
     const uint64_t absent = t.absent;
-    float ks[4], lsv[4], inv[4], rest[4];
-    bool faint = false;
-    if constexpr (kScaled && PAGE16) {
+    // An element's exponent of 2 is f x + z, by groups of 16 tokens (one group where there are no scales).
+    constexpr int kGroups = kScaled && PAGE16 ? 4 : 1;
+    float f[kGroups], z[kGroups], inv[kGroups];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const ValueScale z(t.vs[g]);
-        ks[g] = t.ks[g], lsv[g] = z.log, inv[g] = z.inv, rest[g] = z.rest;
-        faint |= z.rest != 1.0f;
+    for (int g = 0; g < kGroups; ++g) {
+      f[g] = coef, z[g] = 0.0f, inv[g] = 1.0f;
+      if constexpr (kScaled && PAGE16) {
+        const ValueScale v(t.vs[g]);
+        f[g] = fmaxf(t.ks[g] * coef, 0x1p-126f);  // never 0: a hidden score is minus infinity, and has to stay it
+        z[g] = v.log, inv[g] = v.inv;
+      } else if constexpr (kScaled) {
+        f[g] = 1.0f;  // its tokens' own scales are applied to the scores at once
       }
-    } else if constexpr (kScaled) {
-      rest[0] = ValueScale(t.vs[0]).rest;  // of the tile's token `lane`
-      faint = __any(rest[0] != 1.0f);
     }
     __syncthreads();
-    if (s + 2 < s1) t.fetch_tile(steps.token(s + 2));
+    if (s + 2 < s1) {
+      const int next = steps.token(s + 2);
+      if (PAGE16 && next != t0 + kManyTokens) t.seek(next);
+      t.fetch_tile(next, p_first);
+    }
     const bool hidden = t0 + kManyTokens > end || (a.causal && t0 + kManyTokens - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) || absent != 0;
     const bool blank = !works || (a.causal && t0 > p_most);  // no row of the wave sees any of it
-    if (!blank) {
-      const uint8_t* kb = lds + buffer * T::kBuffer;
-      const uint8_t* vb = kb + T::kKTile;
-      bool slow = false;
-      if constexpr (KIND != KVH_CACHE_I8) slow = hidden && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3]) != 0;
+    if (blank) continue;
+    const uint8_t* kb = lds + buffer * T::kBuffer;
+    const uint8_t* vb = kb + T::kKTile;
+    f32x16 x[2];  // element j of x[i] is token 32 i + 8 (j / 4) + 4 half + j % 4 of the tile, of its group 2 i + j / 8
+    {
+      u32x4 kf[2 * T::kSums];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {  // 32 tokens at a time: element j of x is token 32 i + 8 (j / 4) + 4 half + j % 4 of the tile
-        f32x16 x;
+      for (int kk = 0; kk < 2 * T::kSums; ++kk)
+        kf[kk] = *reinterpret_cast<const u32x4*>(kb + k_at[kk % 4] + kk / T::kSums * (32 * D * 2) + kk % T::kSums / 4 * 128);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = 0.0f;
-        u32x4 kf[T::kSums], vf[2 * T::kOuts];
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int kk = 0; kk < T::kSums; ++kk) kf[kk] = *reinterpret_cast<const u32x4*>(kb + k_at[kk % 4] + i * (32 * D * 2) + kk / 4 * 128);
+        for (int j = 0; j < 16; ++j) x[i][j] = 0.0f;
 #pragma unroll
-        for (int kk = 0; kk < T::kSums; ++kk) x = mfma32<T::kBf>(kf[kk], q[kk], x);
-        // Operands are read ahead of the instructions that take them: four of K first, then one with each product.
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        for (int kk = 0; kk < T::kSums; ++kk) x[i] = mfma32<T::kBf>(kf[i * T::kSums + kk], q[kk], x[i]);
+      }
+      // Operands are read ahead of the instructions that take them: four first, then one with each product.
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-        for (int kk = 4; kk < T::kSums; ++kk) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-        // and the first of V before the softmax
+      for (int kk = 4; kk < 2 * T::kSums; ++kk) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    }
+    if constexpr (kScaled && !PAGE16) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) vf[e] = *reinterpret_cast<const u32x4*>(vb + v_at[2 * i + e % 2] + e / 2 * (32 * kManyTokens * 2));
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kScaled) {
-#pragma unroll
-          for (int j4 = 0; j4 < 4; ++j4) {
-            if constexpr (PAGE16) {
-              const int g = 2 * i + j4 / 2;
-              const float f = ks[g] * coef;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[4 * j4 + e] = __builtin_fmaf(x[4 * j4 + e], f, lsv[g]);
-            } else {
-              const f32x4 f = *reinterpret_cast<const f32x4*>(&scales[buffer][0][32 * i + 8 * j4 + 4 * half]);
-              const f32x4 z = *reinterpret_cast<const f32x4*>(&scales[buffer][1][32 * i + 8 * j4 + 4 * half]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[4 * j4 + e] = __builtin_fmaf(x[4 * j4 + e], f[e] * coef, z[e]);
-            }
-          }
-        }
-        const float unit = kScaled ? 1.0f : coef;  // what is left to turn x into an exponent of 2
-        if (hidden) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int in = 32 * i + 8 * (j / 4) + j % 4;  // and 4 half more
-            const bool seen = sight.sees(a, t0 + 4 * half + in), none = (absent >> 4 * half >> in & 1) != 0;
-            bad |= seen && none;
-            x[j] = !seen || none ? -INFINITY : x[j] * unit;
-          }
-        } else if constexpr (!kScaled) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] *= unit;
-        }
-        float most = x[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) most = fmaxf(most, x[j]);
-        most = fmaxf(most, __shfl_xor(most, 32));
-        // The maximum may lag behind by 2^8: weights up to 256 are as good, and the outputs are hardly ever rescaled.
-        if (__any(most > m + 8.0f)) {
-          const float now = fmaxf(m, most);
-          const float down = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-          m = now;
-          l *= down;
-#pragma unroll
-          for (int c = 0; c < T::kOuts; ++c)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[c][j] *= down;
-        }
-        const float top = m == -INFINITY ? 0.0f : m;
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j4 = 0; j4 < 4; ++j4) {
-          f32x4 z = {1, 1, 1, 1};
-          if constexpr (kScaled && !PAGE16) z = *reinterpret_cast<const f32x4*>(&scales[buffer][2][32 * i + 8 * j4 + 4 * half]);
+          const f32x4 kz = *reinterpret_cast<const f32x4*>(&scales[buffer][0][32 * i + 8 * j4 + 4 * half]);
+          const f32x4 lz = *reinterpret_cast<const f32x4*>(&scales[buffer][1][32 * i + 8 * j4 + 4 * half]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float w = __builtin_amdgcn_exp2f(x[4 * j4 + e] - top);
-            if constexpr (!kScaled)
-              l += w;
-            else if constexpr (PAGE16)
-              l = __builtin_fmaf(w, inv[2 * i + j4 / 2], l);
-            else
-              l = __builtin_fmaf(w, z[e], l);
-            x[4 * j4 + e] = w;
-          }
+          for (int e = 0; e < 4; ++e) x[i][4 * j4 + e] = __builtin_fmaf(x[i][4 * j4 + e], kz[e] * coef, lz[e]);
         }
-        if constexpr (kScaled) {
-          if (faint) {
+    }
+    if (hidden) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              if constexpr (PAGE16)
-                x[j] *= rest[2 * i + j / 8];
-              else
-                x[j] *= __shfl(rest[0], 32 * i + 8 * (j / 4) + 4 * half + j % 4);
-            }
-          }
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int in = 32 * i + 8 * (j / 4) + j % 4;  // and 4 half more
+          const bool seen = sight.sees(a, t0 + 4 * half + in), none = (absent >> 4 * half >> in & 1) != 0;
+          bad |= seen && none;
+          x[i][j] = !seen || none ? -INFINITY : x[i][j];
         }
-        u32x4 p[2];  // of each 16 tokens: the lane's 8 weights
+    }
+    float most = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < kGroups; ++g) {  // f is positive: the largest score of a group has its largest exponent
+      constexpr int kPer = 32 / kGroups;
+      float top = x[g * kPer / 16][g * kPer % 16];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[g][e] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(x[8 * g + 2 * e], x[8 * g + 2 * e + 1]);
+      for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[(g * kPer + j) / 16][(g * kPer + j) % 16]);
+      most = fmaxf(most, __builtin_fmaf(top, f[g], z[g]));
+    }
+    most = fmaxf(most, __shfl_xor(most, 32));
+    // The maximum may lag behind by 2^8: weights up to 256 are as good, and the outputs are hardly ever rescaled.
+    if (__any(most > m + 8.0f)) {
+      const float now = fmaxf(m, most);
+      const float down = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= down;
+#pragma unroll
+      for (int c = 0; c < T::kOuts; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[c][j] *= down;
+    }
+    const float top = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) z[g] -= top;
+    u32x4 p[4];  // of each 16 tokens: the lane's 8 weights
+    auto weights = [&](int i) {
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4) {
+        f32x4 by = {1, 1, 1, 1};
+        if constexpr (kScaled && !PAGE16) by = *reinterpret_cast<const f32x4*>(&scales[buffer][2][32 * i + 8 * j4 + 4 * half]);
+        const int g = kGroups == 4 ? 2 * i + j4 / 2 : 0;
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][4 * j4 + e], f[g], z[g]));
+          if constexpr (!kScaled)
+            l += w[e];
+          else
+            l = __builtin_fmaf(w[e], PAGE16 ? inv[g] : by[e], l);
+        }
+        p[2 * i + j4 / 2][2 * (j4 % 2)] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(w[0], w[1]);
+        p[2 * i + j4 / 2][2 * (j4 % 2) + 1] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(w[2], w[3]);
+      }
+    };
+    auto operand = [&](int c, int g) { return *reinterpret_cast<const u32x4*>(vb + v_at[g] + c * (32 * kManyTokens * 2)); };
+    weights(0);
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      u32x4 vf[2 * T::kOuts];
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) vf[e] = operand(e / 2, e % 2);
+      weights(1);
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) o[e / 2] = mfma32<T::kBf>(vf[e], p[e % 2], o[e / 2]);
+      // the first half's products run under the second half's exponentials
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        if (e + 4 < 2 * T::kOuts) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * T::kOuts), 1);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      u32x4 vf[2 * T::kOuts];
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) vf[e] = operand(e / 2, 2 + e % 2);
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) o[e / 2] = mfma32<T::kBf>(vf[e], p[2 + e % 2], o[e / 2]);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 2);
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOuts; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+        if (e + 4 < 2 * T::kOuts) __builtin_amdgcn_sched_group_barrier(0x100, 1, 2);
+      }
+    }
+    if constexpr (KIND != KVH_CACHE_I8) {
+      if ((odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3]) != 0) {
         using Bad = Odd<T::kBf>;
 #pragma unroll
-        for (int e = 4; e < 2 * T::kOuts; ++e) vf[e] = *reinterpret_cast<const u32x4*>(vb + v_at[2 * i + e % 2] + e / 2 * (32 * kManyTokens * 2));
-        if (slow) {
+        for (int g = 0; g < 4; ++g) {
+          u32x4 one;  // of the group's tokens that the lane's row sees
 #pragma unroll
-          for (int e = 0; e < 2 * T::kOuts; ++e) vf[e] = Bad::without(vf[e]);
-        }
+          for (int e = 0; e < 4; ++e) {
+            one[e] = 0;
 #pragma unroll
-        for (int e = 0; e < 2 * T::kOuts; ++e) o[e / 2] = mfma32<T::kBf>(vf[e], p[e % 2], o[e / 2]);
-        if (slow) {
-          u32x4 one[2];  // of the tokens that the lane's row sees
-#pragma unroll
-          for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              one[g][e] = 0;
-#pragma unroll
-              for (int n = 0; n < 2; ++n) {
-                const int j = 8 * g + 2 * e + n;
-                if (sight.sees(a, t0 + 4 * half + 32 * i + 8 * (j / 4) + j % 4)) one[g][e] |= Bad::kOne << 16 * n;
-              }
-            }
+            for (int n = 0; n < 2; ++n)
+              if (sight.sees(a, t0 + T::v_token(2 * g + half, 2 * e + n))) one[e] |= Bad::kOne << 16 * n;
+          }
 #pragma unroll
           for (int c = 0; c < T::kOuts; ++c) {
 #pragma unroll 1
@@ -464,9 +569,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
               f32x16 hit;
 #pragma unroll
               for (int j = 0; j < 16; ++j) hit[j] = 0.0f;
-#pragma unroll
-              for (int g = 0; g < 2; ++g)
-                hit = mfma32<T::kBf>(Bad::ones(*reinterpret_cast<const u32x4*>(vb + v_at[2 * i + g] + c * (32 * kManyTokens * 2)), which), one[g], hit);
+              hit = mfma32<T::kBf>(t.odd_ones(t0, c, g, which), one, hit);
 #pragma unroll
               for (int j = 0; j < 16; ++j) o[c][j] += hit[j] > 0.0f ? Bad::value(which) : 0.0f;
             }
