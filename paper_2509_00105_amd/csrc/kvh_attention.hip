@@ -21,14 +21,26 @@ namespace {
 template <int DT, int KIND, int D, int NR, bool PAGE16>
 struct Worker {
   static constexpr bool kBf = kBf16<DT, KIND>;
-  static constexpr int kWidth = KIND == KVH_CACHE_16 ? 2 : 1;
-  static constexpr int kSums = D / 32;           // matrix instructions of a dot product
-  static constexpr int kChans = D / 16;          // channels of V that a lane reads of a token, and channel tiles of the output
-  static constexpr int kKWords = D * kWidth / 16;       // words of K that a lane reads of a tile
-  static constexpr int kVWords = kChans * kWidth / 4;   // words of V that a lane reads of a token
+  static constexpr bool kScaled = KIND != KVH_CACHE_16;
+  static constexpr int kWidth = kScaled ? 1 : 2;
+  static constexpr int kSums = D / 32;                 // matrix instructions of a dot product
+  static constexpr int kChans = D / 16;                // channels of V that a lane reads of a token, and channel tiles of the output
+  static constexpr int kKWords = D * kWidth / 16;      // words of K that a lane reads of a tile
+  static constexpr int kVWords = kChans * kWidth / 4;  // words of V that a lane reads of a token
+  static constexpr int kScales = kScaled ? (PAGE16 ? 2 : 8) : 1;
+  static constexpr bool kAhead = NR == 1 && !(KIND == KVH_CACHE_16 && D == 128);  // where two steps fit the registers
+
+  // A step's tokens as they are in the cache.  Token slot 4 i + r of a lane is token 16 i + 4 grp + r of the step.
+  struct Raw {
+    Words<kKWords> k[2];
+    Words<kVWords> v[8];
+    float ks[kScales], vs[kScales];  // of the step's two tiles (PAGE16), or of the lane's token slots
+    uint32_t absent;                 // token slots on no page of the cache
+  };
 
   const AttnParams& a;
   Request rq;
+  const int32_t* table;
   int head, row0, rows;  // of the tile: its first row, rows it has
   int lane, l16, grp;
   int end;               // tokens at and past it are seen by no row
@@ -40,6 +52,8 @@ struct Worker {
   f32x4 o[NR][kChans];
   float m[NR], l[NR];
   PageRun run;
+  int in, row;           // PAGE16: where the next tile of 16 tokens lies: in the request's page `in`, `row` rows from its start
+  uint32_t k_from, v_from;  // PAGE16: bytes from a tile's first row to what the lane reads of it
   bool bad;  // a token that a row should see lies on no page of the cache
 
   __device__ __forceinline__ Worker(const AttnParams& a_) : a(a_) {}
@@ -95,50 +109,50 @@ struct Worker {
       for (int ct = 0; ct < kChans; ++ct) o[t][ct] = f32x4{0, 0, 0, 0};
     }
     bad = false;
+    const uint32_t row_bytes = (uint32_t)a.c_ts * kWidth;
+    k_from = l16 * row_bytes + grp * 16;
+    v_from = grp * 4 * row_bytes + l16 * (kChans * kWidth);
   }
 
-  // One step: tokens [t0, t0 + 32), t0 < end, a multiple of 32.
-  __device__ __forceinline__ void step(const int32_t* table, int t0) {
+  // The next step fetched is that of tokens t0 and on.
+  __device__ __forceinline__ void seek(int t0) {
+    in = (int)a.by_block.quotient((uint32_t)t0);
+    row = t0 - in * a.block_tokens;
+  }
+
+  // Starts the loads of tokens [t0, t0 + 32), t0 < end, where seek or the step before left off.  Nothing here waits for them.
+  __device__ __forceinline__ void fetch_step(Raw& x, int t0) {
     const int last = end - 1;
-    Words<kKWords> k[2];
-    Words<kVWords> v[8];
-    float ks[8], lsv[8], inv[8], rest[8];  // by token slot: 4 i + r is token 16 i + 4 grp + r
-    bool hidden_any = false;
-    uint32_t absent = 0;  // token slots on no page of the cache
-    const int64_t row_bytes = a.c_ts * kWidth;
-    const int64_t head_at = (int64_t)head * D * kWidth;
+    const int64_t row_bytes = a.c_ts * kWidth, head_at = (int64_t)head * D * kWidth;
+    x.absent = 0;
     if constexpr (PAGE16) {
+      // A tile lies on one page: its rows past the end are the page's too, and only have to be kept from the sums.
+      if ((unsigned)(in - run.base) > (unsigned)(kWave - 2)) run.load(a, table, in, (int)a.by_block.quotient((uint32_t)last), lane);
+      int64_t at = 0;
+      int page = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        int t = t0 + 16 * i;
-        if (t > last) t = last & ~15;  // a tile past the end reads the last one again, and is masked
-        const int at = (int)a.by_block.quotient((uint32_t)t);
-        if ((unsigned)(at - run.base) >= (unsigned)kWave) run.load(a, table, at, (int)a.by_block.quotient((uint32_t)last), lane);
-        int page = uniform(__builtin_amdgcn_readlane(run.entry, at - run.base));
-        if (page < 0) {
-          page = 0;
-          absent |= 15u << 4 * i;
+        if (i == 0 || t0 + 16 <= last) {  // a tile past the end stands for the one before
+          page = uniform(__builtin_amdgcn_readlane(run.entry, in - run.base));
+          if (page < 0) {
+            page = 0;
+            x.absent |= 15u << 4 * i;
+          }
+          at = ((int64_t)page * a.block_tokens + row) * row_bytes + head_at;
+          row += 16;
+          if (row == a.block_tokens) row = 0, ++in;
         }
-        const int64_t row = (int64_t)page * a.block_tokens + (t - at * a.block_tokens);
-        const uint8_t *kt = a.ck + head_at + row * row_bytes, *vt = a.cv + head_at + row * row_bytes;
-        const int most = last - t;  // rows past it are none of the request's: the last one is read again, and masked
-        const int kr = l16 < most ? l16 : most;
-        const uint8_t* kp = kt + (uint32_t)kr * (uint32_t)row_bytes + grp * 16;
 #pragma unroll
         for (int j = 0; j < kKWords / 4; ++j) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kp + j * 64);
+          const u32x4 w = *reinterpret_cast<const u32x4*>(a.ck + at + k_from + j * 64);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) k[i].w[4 * j + e] = w[e];
+          for (int e = 0; e < 4; ++e) x.k[i].w[4 * j + e] = w[e];
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int vr = grp * 4 + r < most ? grp * 4 + r : most;
-          v[4 * i + r] = fetch<kVWords>(vt + (uint32_t)vr * (uint32_t)row_bytes + l16 * (kChans * kWidth));
-        }
-        if constexpr (KIND != KVH_CACHE_16) {
-          const float s = a.sk[(int64_t)page * a.s_ps + head], z = a.sv[(int64_t)page * a.s_ps + head];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) ks[4 * i + r] = s, lsv[4 * i + r] = z;
+        for (int r = 0; r < 4; ++r) x.v[4 * i + r] = fetch<kVWords>(a.cv + at + r * row_bytes + v_from);
+        if constexpr (kScaled) {
+          x.ks[i] = a.sk[(int64_t)page * a.s_ps + head];
+          x.vs[i] = a.sv[(int64_t)page * a.s_ps + head];
         }
       }
     } else {
@@ -147,16 +161,16 @@ struct Worker {
       if (at0 < run.base || at1 - run.base >= kWave) run.load(a, table, at0, (int)a.by_block.quotient((uint32_t)last), lane);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int t = t0 + 16 * i + l16 < last ? t0 + 16 * i + l16 : last;
+        const int t = t0 + 16 * i + l16 < last ? t0 + 16 * i + l16 : last;  // a token past the end stands for the last one
         const int at = (int)a.by_block.quotient((uint32_t)t);
         const int page = __shfl(run.entry, at - run.base);
-        const int64_t row = (int64_t)(page < 0 ? 0 : page) * a.block_tokens + (t - at * a.block_tokens);
-        const uint8_t* kp = a.ck + head_at + row * row_bytes + grp * 16;
+        const int64_t r = (int64_t)(page < 0 ? 0 : page) * a.block_tokens + (t - at * a.block_tokens);
+        const uint8_t* kp = a.ck + head_at + r * row_bytes + grp * 16;
 #pragma unroll
         for (int j = 0; j < kKWords / 4; ++j) {
           const u32x4 w = *reinterpret_cast<const u32x4*>(kp + j * 64);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) k[i].w[4 * j + e] = w[e];
+          for (int e = 0; e < 4; ++e) x.k[i].w[4 * j + e] = w[e];
         }
       }
 #pragma unroll
@@ -166,76 +180,84 @@ struct Worker {
         int page = __shfl(run.entry, at - run.base);
         if (page < 0) {
           page = 0;
-          absent |= 1u << i;
+          x.absent |= 1u << i;
         }
-        const int64_t row = (int64_t)page * a.block_tokens + (t - at * a.block_tokens);
-        v[i] = fetch<kVWords>(a.cv + head_at + row * row_bytes + l16 * (kChans * kWidth));
-        if constexpr (KIND != KVH_CACHE_16) {
-          ks[i] = a.sk[(int64_t)page * a.s_ps + head];
-          lsv[i] = a.sv[(int64_t)page * a.s_ps + head];
+        const int64_t r = (int64_t)page * a.block_tokens + (t - at * a.block_tokens);
+        x.v[i] = fetch<kVWords>(a.cv + head_at + r * row_bytes + l16 * (kChans * kWidth));
+        if constexpr (kScaled) {
+          x.ks[i] = a.sk[(int64_t)page * a.s_ps + head];
+          x.vs[i] = a.sv[(int64_t)page * a.s_ps + head];
         }
       }
     }
-    // Whether some row does not see all of these tokens.
-    hidden_any = t0 + kStep > end || (a.causal && t0 + kStep - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) ||
-                 __any(absent != 0);
-    if constexpr (KIND != KVH_CACHE_16) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const ValueScale z(lsv[i]);
-        lsv[i] = z.log, inv[i] = z.inv, rest[i] = z.rest;
-      }
-    }
+  }
 
-    u32x4 kop[2][kSums];
+  // Takes the tokens [t0, t0 + 32) into the sums.
+  __device__ __forceinline__ void take(Raw& x, int t0) {
+    // Whether some row does not see all of these tokens.
+    const bool hidden_any = t0 + kStep > end || (a.causal && t0 + kStep - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) ||
+                            (PAGE16 ? x.absent != 0 : __any(x.absent != 0));
+    float lsv[kScales], inv[kScales], rest[kScales];
+    bool faint = false;
+    if constexpr (kScaled) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kScales; ++i) {
+        const ValueScale z(x.vs[i]);
+        lsv[i] = z.log, inv[i] = z.inv, rest[i] = z.rest;
+        faint |= z.rest != 1.0f;
+      }
+      faint = __any(faint);
+    }
+    auto of = [](int i) { return PAGE16 ? i / 4 : i; };  // token slot -> its scale
+
+    f32x4 s[NR][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int t = 0; t < NR; ++t) s[t][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int kk = 0; kk < kSums; ++kk) {
-        if constexpr (KIND == KVH_CACHE_16) {
+        u32x4 kop;
+        if constexpr (!kScaled) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kop[i][kk][e] = k[i].w[4 * kk + e];
+          for (int e = 0; e < 4; ++e) kop[e] = x.k[i].w[4 * kk + e];
         } else {
           uint32_t w[4];
-          widen4<KIND>(k[i].w[2 * kk], w[0], w[1]);
-          widen4<KIND>(k[i].w[2 * kk + 1], w[2], w[3]);
+          widen4<KIND>(x.k[i].w[2 * kk], w[0], w[1]);
+          widen4<KIND>(x.k[i].w[2 * kk + 1], w[2], w[3]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kop[i][kk][e] = w[e];
+          for (int e = 0; e < 4; ++e) kop[e] = w[e];
         }
+#pragma unroll
+        for (int t = 0; t < NR; ++t) s[t][i] = mfma<kBf>(kop, q[t][kk], s[t][i]);
       }
+    }
 
     u32x4 p[NR];
-    float w[NR][8];
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
-      f32x4 s[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        s[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int kk = 0; kk < kSums; ++kk) s[i] = mfma<kBf>(kop[i][kk], q[t][kk], s[i]);
-      }
-      float x[8];
+      float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if constexpr (KIND == KVH_CACHE_16)
-          x[i] = s[i / 4][i % 4] * coef[t];
+        if constexpr (!kScaled)
+          y[i] = s[t][i / 4][i % 4] * coef[t];
         else
-          x[i] = __builtin_fmaf(s[i / 4][i % 4], ks[i] * coef[t], lsv[i]);
+          y[i] = __builtin_fmaf(s[t][i / 4][i % 4], x.ks[of(i)] * coef[t], lsv[of(i)]);
       }
       if (hidden_any) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const bool seen = sight[t].sees(a, t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (absent >> i & 1u) != 0;
+          const bool seen = sight[t].sees(a, t0 + 16 * (i / 4) + grp * 4 + i % 4), none = (x.absent >> i & 1u) != 0;
           bad |= seen && none;
-          if (!seen || none) x[i] = -INFINITY;
+          if (!seen || none) y[i] = -INFINITY;
         }
       }
-      float most = x[0];
+      float most = y[0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) most = fmaxf(most, x[i]);
+      for (int i = 1; i < 8; ++i) most = fmaxf(most, y[i]);
       most = over_groups_max(most);
-      if (__any(most > m[t])) {
+      // The maximum may lag behind by 2^8: weights up to 256 are as good, and the outputs are hardly ever rescaled.
+      if (__any(most > m[t] + 8.0f)) {
         const float now = fmaxf(m[t], most);
         const float down = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
         m[t] = now;
@@ -246,17 +268,20 @@ struct Worker {
       const float top = m[t] == -INFINITY ? 0.0f : m[t];  // nothing seen yet: the weights below are zeros
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float e = __builtin_amdgcn_exp2f(x[i] - top);
-        if constexpr (KIND == KVH_CACHE_16) {
-          l[t] += e;
-        } else {
-          l[t] = __builtin_fmaf(e, inv[i], l[t]);
-          e *= rest[i];
+        y[i] = __builtin_amdgcn_exp2f(y[i] - top);
+        if constexpr (!kScaled)
+          l[t] += y[i];
+        else
+          l[t] = __builtin_fmaf(y[i], inv[of(i)], l[t]);
+      }
+      if constexpr (kScaled) {
+        if (faint) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] *= rest[of(i)];
         }
-        w[t][i] = e;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[t][e] = narrow2<kBf ? KVH_BF16 : KVH_F16>(w[t][2 * e], w[t][2 * e + 1]);
+      for (int e = 0; e < 4; ++e) p[t][e] = narrow2<kBf ? KVH_BF16 : KVH_F16>(y[2 * e], y[2 * e + 1]);
     }
 
     if (hidden_any) {
@@ -264,23 +289,23 @@ struct Worker {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int tok = t0 + 16 * (i / 4) + grp * 4 + i % 4;
-        const bool none = tok >= end || (absent >> i & 1u);
+        const bool none = tok >= end || (x.absent >> i & 1u);
 #pragma unroll
-        for (int e = 0; e < kVWords; ++e) v[i].w[e] = none ? 0u : v[i].w[e];
+        for (int e = 0; e < kVWords; ++e) x.v[i].w[e] = none ? 0u : x.v[i].w[e];
       }
       if constexpr (KIND != KVH_CACHE_I8) {
         bool any = false;  // an infinity or NaN among them
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int e = 0; e < kVWords; ++e) any |= has_odd<DT, KIND>(v[i].w[e]);
+          for (int e = 0; e < kVWords; ++e) any |= has_odd<DT, KIND>(x.v[i].w[e]);
         if (__any(any)) {
-          weigh<true>(v, p, t0);
+          weigh<true>(x.v, p, t0);
           return;
         }
       }
     }
-    weigh<false>(v, p, t0);
+    weigh<false>(x.v, p, t0);
   }
 
   // The second product: ODD where some values are infinities or NaN that some rows do not see.
@@ -331,41 +356,76 @@ struct Worker {
       }
     }
   }
+
+  // Steps [s0, s1).  kAhead: a step's loads are under way while the one before it is worked on.
+  __device__ __forceinline__ void walk(const Steps& steps, int s0, int s1) {
+    if (s0 >= s1) return;
+    int t = steps.token(s0);
+    seek(t);
+    if constexpr (!kAhead) {
+      for (int s = s0; s < s1; ++s) {
+        const int t1 = steps.token(s);
+        if (s > s0 && t1 != t + kStep) seek(t1);
+        t = t1;
+        Raw x;
+        fetch_step(x, t);
+        take(x, t);
+      }
+    } else {
+      Raw x[2];
+      fetch_step(x[0], t);
+      auto next = [&](int s, Raw& to) {  // the step after s
+        if (s + 1 >= s1) return t;
+        const int t1 = steps.token(s + 1);
+        if (t1 != t + kStep) seek(t1);
+        fetch_step(to, t1);
+        return t1;
+      };
+      for (int s = s0;;) {
+        int t1 = next(s, x[1]);
+        take(x[0], t);
+        t = t1;
+        if (++s >= s1) break;
+        t1 = next(s, x[0]);
+        take(x[1], t);
+        t = t1;
+        if (++s >= s1) break;
+      }
+    }
+  }
 };
 
+constexpr int kLogFewWaves = 2, kFewWaves = 1 << kLogFewWaves, kFewThreads = kFewWaves * kWave;
+
+constexpr int few_log_rows(int nr) { return nr == 1 ? 4 : 5; }
+
 template <int DT, int KIND, int D, int NR, bool PAGE16>
-__global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams a) {
+__device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int head0, int wave, int lane, float* lds, float (*lds_ml)[16 * NR][2]) {
   using W = Worker<DT, KIND, D, NR, PAGE16>;
   constexpr int kTile = 16 * NR;
   constexpr int kPitch = D + 4;  // floats of a row in LDS
-  __shared__ float lds[kWavesPerBlock * 16 * kPitch];
-  __shared__ float lds_ml[kWavesPerBlock][kTile][2];
-  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
-  const uint32_t item = a.by_heads.quotient(blockIdx.x);  // the heads of an item run together: they read neighbouring memory
-  const int head = (int)(blockIdx.x - item * (uint32_t)a.heads);
-  Item it;
-  if (!find_item(a, kTile, item, false, lane, it)) return;
   W w(a);
   w.lane = lane, w.l16 = lane % 16, w.grp = lane / 16;
   w.rq = it.rq;
-  w.head = head;
+  w.head = head0 + (wave & (1 << a.log_hw) - 1);
   w.row0 = it.tile * kTile;
   const int all = it.rq.n * a.group;
   w.rows = all - w.row0 < kTile ? all - w.row0 : kTile;
   w.p_least = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)w.row0);
   w.p_most = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)(w.row0 + w.rows - 1));
   w.end = a.causal && w.p_most + 1 < it.rq.len ? w.p_most + 1 : it.rq.len;
+  w.table = a.req.table + (int64_t)it.b * a.req.table_stride;
   w.begin();
   const Steps steps(a, w.p_least, w.end);
   int s0, s1;
   steps.part_of(it, s0, s1);
-  const int mine = (s1 - s0 + kWavesPerBlock - 1) / kWavesPerBlock;
-  const int b0 = s0 + wave * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
-  const int32_t* table = a.req.table + (int64_t)it.b * a.req.table_stride;
-  for (int s = b0; s < b1; ++s) w.step(table, steps.token(s));
+  const int log_tw = kLogFewWaves - a.log_hw, tw = 1 << log_tw;  // the waves of a head share its steps
+  const int mine = (s1 - s0 + tw - 1) >> log_tw;
+  const int b0 = s0 + (wave >> a.log_hw) * mine, b1 = b0 + mine < s1 ? b0 + mine : s1;
+  w.walk(steps, b0, b1);
   if (__any(w.bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
-  // The four waves' results become one.
+  // The results of a head's waves become one.
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     const float sum = over_groups_sum(w.l[t]);
@@ -374,8 +434,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
       lds_ml[wave][t * 16 + w.l16][1] = sum;
     }
   }
-  const bool split = it.parts > 1;
-  const int64_t slot = blockIdx.x;
+  const int log_hw = a.log_hw, hw = 1 << log_hw;
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     if (t * 16 >= w.rows) break;
@@ -388,30 +447,27 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
         *reinterpret_cast<f32x4*>(&lds[(wave * 16 + w.l16) * kPitch + (4 * w.grp + r) * W::kChans + ct]) = x;
       }
     __syncthreads();
-    // thread: row threadIdx / 16, D / 16 channels
-    const int r = threadIdx.x / 16, ch = (threadIdx.x % 16) * W::kChans, row = t * 16 + r;
-    if (row < w.rows) {
+    // a thread: D / 16 channels of one row of every (kFewWaves / 4)-th head
+    const int r = threadIdx.x % 256 / 16, ch = (threadIdx.x % 16) * W::kChans, row = t * 16 + r;
+    for (int h = threadIdx.x / 256; h < hw && row < w.rows; h += kFewWaves / 4) {
+      const int head = head0 + h;
       float m = -INFINITY;
-#pragma unroll
-      for (int v = 0; v < kWavesPerBlock; ++v) m = fmaxf(m, lds_ml[v][row][0]);
+      for (int v = h; v < kFewWaves; v += hw) m = fmaxf(m, lds_ml[v][row][0]);
       float l = 0.0f, x[W::kChans];
 #pragma unroll
       for (int e = 0; e < W::kChans; ++e) x[e] = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kWavesPerBlock; ++v) {
+      for (int v = h; v < kFewWaves; v += hw) {
         const float mv = lds_ml[v][row][0], f = mv == m ? 1.0f : __builtin_amdgcn_exp2f(mv - m);
         l = __builtin_fmaf(f, lds_ml[v][row][1], l);
 #pragma unroll
         for (int e = 0; e < W::kChans; ++e) x[e] = __builtin_fmaf(f, lds[(v * 16 + r) * kPitch + ch + e], x[e]);
       }
-      if (split) {
-        float* to = a.part + (slot * kTile + row) * D + ch;
+      if (it.split) {
+        const int64_t at = (it.slot * a.heads + head) * kTile + row;
+        float* to = a.part + at * D + ch;
 #pragma unroll
         for (int e = 0; e < W::kChans; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-        if (ch == 0) {
-          a.part_ml[(slot * kTile + row) * 2] = m;
-          a.part_ml[(slot * kTile + row) * 2 + 1] = l;
-        }
+        if (ch == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m, l};
       } else {
         const int at = w.row0 + row, token = (int)a.by_group.quotient((uint32_t)at), u = at - token * a.group;
         const bool blind = it.rq.len == 0 || (a.causal && it.rq.len - it.rq.n + token < 0);
@@ -432,37 +488,103 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_kernel(AttnParams 
   }
 }
 
-// Joins the partial results of the requests that were cut: a wave takes one query row.
-template <int DT, int D>
-__global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int tile_rows) {
-  const int lane = threadIdx.x % kWave;
-  const int q_heads = a.heads * a.group;
-  const int64_t unit = (int64_t)blockIdx.x * kWavesPerBlock + uniform((int32_t)(threadIdx.x / kWave));
-  const int64_t packed = unit / q_heads;
-  if (packed >= a.req.n_tokens) return;
-  const int u = (int)(unit - packed * q_heads), head = u / a.group;
+template <int DT, int KIND, int D, int NR, bool PAGE16>
+__global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void attention_kernel(AttnParams a) {
+  __shared__ float lds[kFewWaves * 16 * (D + 4)];
+  __shared__ float lds_ml[kFewWaves][16 * NR][2];
+  int lane = threadIdx.x % kWave;
+  const int wave = uniform((int32_t)(threadIdx.x / kWave));
+  // The head groups of an item run on one XCD (consecutive blocks go to the 8 of them in turn), one after the other: they read neighbouring memory.
+  const uint32_t g = blockIdx.x / 8, hi = a.by_heads.quotient(g), k = hi * 8 + blockIdx.x % 8;
+  const int head = (int)(g - hi * a.by_heads.d) << a.log_hw;
+  tell_refused(a);
   Item it;
-  if (!find_item(a, tile_rows, packed, true, lane, it) || it.parts == 1) return;
-  const int token = (int)(packed - it.rq.start);
-  const int64_t at = (int64_t)token * a.group + (u - head * a.group);
-  const int tile = (int)(at / tile_rows), row = (int)(at - (int64_t)tile * tile_rows);
-  const int64_t slot0 = it.part + (int64_t)(it.tiles - 1 - tile) * it.parts;
-  if (slot0 + it.parts > a.items) return;  // requests that share rows of the batch: none of the kernel's
-  constexpr int kPer = D / 64;
+  for (Items items; items.next(a, few_log_rows(NR), k, head == 0 && wave == 0, lane, it);) {
+    if (it.split && it.slot >= a.slots) continue;  // requests that share rows of the batch
+    attend<DT, KIND, D, NR, PAGE16>(a, it, head, wave, lane, lds, lds_ml);
+    __syncthreads();
+  }
+}
+
+// Joins the partial results of the tiles that were cut: WAVES waves take one row, all of a block's where there are few rows, whose parts are
+// then many, and one where there are many.
+// The parts' factors come first, 64 in the lanes, so that the sums are loads that wait for nothing but each other.
+template <int DT, int D, int WAVES>
+__global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int log_rows) {
+  constexpr int kPer = D / 64, kAtOnce = 8, kLogRows = WAVES == 1 ? 2 : 0;  // of a block
+  __shared__ float lds[WAVES > 1 ? WAVES : 1][D];
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  const uint32_t unit = blockIdx.x >> (log_rows - kLogRows), tile = a.by_heads.quotient(unit);
+  const int head = (int)(unit - tile * (uint32_t)a.heads);
+  const int share = WAVES == 1 ? 0 : wave;  // the wave's parts of 64: those, and every WAVES-th after them
+  const int row = ((int)(blockIdx.x & ((1u << (log_rows - kLogRows)) - 1)) << kLogRows) + (WAVES == 1 ? wave : 0);
+  const u32x4* from_joint = reinterpret_cast<const u32x4*>(a.joints + tile);
+  const u32x4 j0 = from_joint[0], j1 = from_joint[1];
+  if (tile >= (uint32_t)uniform(*a.joints_n)) return;  // (the room is there; what it holds is of no account)
+  const int start = uniform((int32_t)j0[0]), n = uniform((int32_t)j0[1]), len = uniform((int32_t)j0[2]), parts = uniform((int32_t)j1[0]);
+  const int64_t slot = uniform((int64_t)((uint64_t)j1[3] << 32 | j1[2]));
+  if (parts == 1 || slot + parts > a.slots) return;  // (past them: requests that share rows of the batch)
+  const int64_t row0 = (int64_t)uniform((int32_t)j0[3]) << log_rows, all = (int64_t)n * a.group;
+  const int64_t next = (int64_t)a.heads << log_rows;  // rows of partial results from one part to the next
+  const int q_heads = a.heads * a.group;
+  if (row0 + row >= all) return;
+  const int64_t first = ((slot * a.heads + head) << log_rows) + row;
   float m = -INFINITY, l = 0.0f, x[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
-  for (int p = 0; p < it.parts; ++p) {
-    const int64_t s = ((slot0 + p) * a.heads + head) * tile_rows + row;
-    const float mp = a.part_ml[2 * s], lp = a.part_ml[2 * s + 1];
-    const float now = fmaxf(m, mp);
-    const float fo = m == now ? 1.0f : __builtin_amdgcn_exp2f(m - now), fp = mp == now ? 1.0f : __builtin_amdgcn_exp2f(mp - now);
-    m = now;
-    l = __builtin_fmaf(l, fo, fp * lp);
+  for (int p0 = 0; p0 < parts; p0 += kWave) {
+    const int here = parts - p0 < kWave ? parts - p0 : kWave;
+    const float* from = a.part + (first + p0 * next) * D + lane * kPer;
+    float y[kAtOnce][kPer];
+    auto fetch_parts = [&](int i) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = __builtin_fmaf(x[e], fo, fp * a.part[s * D + lane * kPer + e]);
+      for (int e = 0; e < kAtOnce; ++e)
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+          const int p = (i + e) * WAVES + share;
+          y[e][c] = p < here ? from[(int64_t)p * next * D + c] : 0.0f;
+        }
+    };
+    fetch_parts(0);
+    f32x2 ml = {-INFINITY, 0.0f};
+    if (lane < here) ml = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * (first + (p0 + lane) * next));
+    float most = ml[0];
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float now = fmaxf(m, most), down = m == now ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+    m = now;
+    const float f = lane < here ? (ml[0] == now ? 1.0f : __builtin_amdgcn_exp2f(ml[0] - now)) : 0.0f;
+    float sum = f * ml[1];
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    l = __builtin_fmaf(l, down, sum);
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) x[c] *= down;
+    for (int i = 0; i * WAVES < here; i += kAtOnce) {
+      if (i > 0) fetch_parts(i);
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const int p = (i + e) * WAVES + share;
+        const float by = p < here ? __shfl(f, p & (kWave - 1)) : 0.0f;
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) x[c] = __builtin_fmaf(by, y[e][c], x[c]);
+      }
+    }
   }
-  const bool blind = it.rq.len == 0 || (a.causal && it.rq.len - it.rq.n + token < 0);
+  if constexpr (WAVES > 1) {
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) lds[wave][lane * kPer + c] = x[c];
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c)
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) x[c] += lds[w][lane * kPer + c];
+  }
+  const int64_t at = row0 + row;
+  const int token = (int)a.by_group.quotient((uint32_t)at), u = head * a.group + (int)(at - (int64_t)token * a.group);
+  const int64_t packed = (int64_t)start + token;
+  const bool blind = len == 0 || (a.causal && len - n + token < 0);
   const float by = 1.0f / l;
   uint16_t* to = a.out + packed * a.o_ts + (int64_t)u * D + lane * kPer;
   if constexpr (kPer == 2)
@@ -472,46 +594,44 @@ __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int t
   if (a.lse != nullptr && lane == 0) a.lse[packed * q_heads + u] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Says which requests are refused; the kernels above pass over them.
-__global__ __launch_bounds__(kBlockThreads) void refuse_kernel(AttnParams a) {
-  const int b = blockIdx.x * kBlockThreads + threadIdx.x;
-  if (b < a.req.n && !read_request(a, b).ok) a.status[b] = KVH_DEV_BAD_REQUEST;
-}
-
 // ---- launch -------------------------------------------------------------------------------------------------------
-constexpr int kTarget = 512;  // blocks of 4 waves that fill the chip: 2 on each compute unit
+constexpr int kFill = 512;            // blocks of 4 waves that fill the chip: their registers leave room for 2 on a compute unit
+constexpr int kLeastSteps = 16;       // of a chunk, few rows: shorter ones cost more in joining than they save
+constexpr int kLeastStepsMany = 4;    // and many rows
+constexpr int64_t kWideTokens = 2048; // from this capacity on a block's waves take heads and not tokens
 
 struct Plan {
   int nr;          // tiles of 16 rows of the kernel for few rows; 0: the kernel for many
-  int rows;        // of an item
+  int log_rows;    // of a tile
+  int log_hw;      // heads that a block takes where it takes several
   int64_t tiles;   // row tiles of the batch at most
-  int64_t items;   // items at most, if requests are cut; the grid otherwise
-  int target;      // what the kernel aims at
-  size_t bytes;    // workspace of these items
+  int64_t target;  // chunks, where the batch is cut
+  size_t slot;     // bytes of a partial result, of all heads
+  int64_t slots() const { return target + tiles; }
+  size_t joints() const { return (size_t)(tiles + 1) * sizeof(Joint); }  // bytes: what the joining kernel reads
 };
-
-size_t slot_bytes(int rows, int head_dim) { return (size_t)rows * (head_dim + 2) * sizeof(float); }
 
 Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
   Plan p;
   const int64_t group = q_heads / heads;
   const int64_t most = (int64_t)(max_new < n_tokens ? max_new : n_tokens) * group;
   p.nr = most <= 16 ? 1 : most <= 32 ? 2 : 0;
-  p.rows = p.nr != 0 ? 16 * p.nr : kManyRows;
-  p.tiles = (int64_t)n_tokens * group / p.rows + n_requests;
-  const int64_t aim = (kTarget + heads - 1) / heads;
-  p.target = (int)aim;
-  p.items = p.target + p.tiles;  // each tile's last chunk may be short
-  p.bytes = (size_t)p.items * heads * slot_bytes(p.rows, head_dim);
+  p.log_rows = p.nr != 0 ? few_log_rows(p.nr) : kLogManyRows;
+  p.log_hw = 0;
+  if (p.nr != 0)
+    while (p.log_hw < kLogFewWaves && (heads >> p.log_hw & 1) == 0) ++p.log_hw;
+  p.tiles = ((int64_t)n_tokens * group >> p.log_rows) + n_requests;
+  p.target = (int64_t)((kFill + heads - 1) / heads) << p.log_hw;
+  p.slot = (size_t)heads * (head_dim + 2) * sizeof(float) << p.log_rows;
   return p;
 }
 
 template <int DT, int KIND, int D, int NR>
 void launch_pages(const AttnParams& a, dim3 grid, hipStream_t stream) {
   if (a.block_tokens % 16 == 0)
-    launch_kernel(attention_kernel<DT, KIND, D, NR, true>, grid, dim3(kBlockThreads), 0, stream, a);
+    launch_kernel(attention_kernel<DT, KIND, D, NR, true>, grid, dim3(kFewThreads), 0, stream, a);
   else
-    launch_kernel(attention_kernel<DT, KIND, D, NR, false>, grid, dim3(kBlockThreads), 0, stream, a);
+    launch_kernel(attention_kernel<DT, KIND, D, NR, false>, grid, dim3(kFewThreads), 0, stream, a);
 }
 
 template <int DT, int KIND, int D>
@@ -539,14 +659,21 @@ void launch_kind(const AttnParams& a, int kind, int head_dim, int nr, dim3 grid,
   }
 }
 
-template <int DT>
-void launch_join(const AttnParams& a, int head_dim, int tile_rows, hipStream_t stream) {
-  const int64_t units = (int64_t)a.req.n_tokens * a.heads * a.group;
-  const dim3 grid((unsigned)((units + kWavesPerBlock - 1) / kWavesPerBlock));
-  if (head_dim == 128)
-    hipLaunchKernelGGL((join_kernel<DT, 128>), grid, dim3(kBlockThreads), 0, stream, a, tile_rows);
+template <int DT, int D>
+void launch_join(const AttnParams& a, int64_t tiles, int log_rows, hipStream_t stream) {
+  const int64_t rows = tiles * a.heads << log_rows;
+  if (tiles * a.heads <= 256)
+    hipLaunchKernelGGL((join_kernel<DT, D, kWavesPerBlock>), dim3((unsigned)rows), dim3(kBlockThreads), 0, stream, a, log_rows);
   else
-    hipLaunchKernelGGL((join_kernel<DT, 64>), grid, dim3(kBlockThreads), 0, stream, a, tile_rows);
+    hipLaunchKernelGGL((join_kernel<DT, D, 1>), dim3((unsigned)(rows / kWavesPerBlock)), dim3(kBlockThreads), 0, stream, a, log_rows);
+}
+
+template <int DT>
+void launch_join(const AttnParams& a, int64_t tiles, int head_dim, int log_rows, hipStream_t stream) {
+  if (head_dim == 128)
+    launch_join<DT, 128>(a, tiles, log_rows, stream);
+  else
+    launch_join<DT, 64>(a, tiles, log_rows, stream);
 }
 
 bool heads_fit(int heads, int q_heads) { return heads >= 1 && q_heads >= heads && q_heads % heads == 0 && q_heads <= 65536; }
@@ -561,7 +688,8 @@ extern "C" {
 size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
   if (n_requests < 1 || n_requests > kMaxRequests || max_new < 1 || n_tokens < 1 || !heads_fit(heads, q_heads)) return 0;
   if (head_dim != 64 && head_dim != 128) return 0;
-  return plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim).bytes;
+  const Plan p = plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim);
+  return p.joints() + (size_t)p.slots() * p.slot;
 }
 
 int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q,
@@ -602,30 +730,31 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   a.by_heads = Divisor((uint32_t)a.heads);
   if ((int64_t)a.req.max_new * a.group >= (int64_t)1 << 31) return KVH_E_SHAPE;
   Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim);
-  // Requests are cut where the row tiles alone leave the chip idle and there is room for the parts.
-  const size_t one = (size_t)a.heads * slot_bytes(p.rows, cache->head_dim);
-  const size_t room = workspace_dev == nullptr ? 0 : workspace_bytes / one;
-  bool cut = p.tiles * a.heads < 2 * kTarget;
-  if (cut && room < (size_t)p.items) {
-    if (room >= (size_t)p.tiles + 1)
-      p.target = (int)(room - p.tiles), p.items = (int64_t)room;
-    else
-      cut = false;
-  }
-  if (!cut) p.items = p.tiles;
-  if (p.items * a.heads > 0x7fffffff) return KVH_E_SHAPE;
-  a.target = p.target;
-  a.items = p.items;
-  a.least = 16;
+  // Few rows of short requests: a block's waves share the tokens of one head, and a step's latency.
+  if (a.req.capacity < kWideTokens) p.target >>= p.log_hw, p.log_hw = 0;
+  // The batch is cut where its row tiles alone leave the chip idle, some request can be longer than the shortest part, and there is room
+  // for the parts.
+  const int least = p.nr == 0 ? kLeastStepsMany : kLeastSteps;
+  const int64_t room = workspace_dev == nullptr || workspace_bytes < p.joints() ? 0 : (int64_t)((workspace_bytes - p.joints()) / p.slot);
+  const bool cut = p.tiles * a.heads < 2 * kFill && a.req.capacity > least * kStep && room > p.tiles;
+  if (cut && room < p.slots()) p.target = room - p.tiles;
+  a.log_hw = p.log_hw;
+  a.by_heads = Divisor((uint32_t)(a.heads >> a.log_hw));
+  int64_t blocks = cut ? p.target : p.tiles;
+  if (p.nr != 0) blocks = (blocks + 7) & ~(int64_t)7;  // see attention_kernel's order
+  blocks *= a.by_heads.d;
+  if (blocks > 0x7fffffff) return KVH_E_SHAPE;
+  a.target = (int)p.target;
+  a.least = least;
   if (cut) {
-    a.part = static_cast<float*>(workspace_dev);
-    a.part_ml = a.part + (size_t)p.items * a.heads * p.rows * cache->head_dim;
+    a.slots = p.slots();
+    a.tiles = p.tiles;
+    a.joints_n = static_cast<int32_t*>(workspace_dev);
+    a.joints = static_cast<Joint*>(workspace_dev) + 1;
+    a.part = reinterpret_cast<float*>(a.joints + p.tiles);
+    a.part_ml = a.part + ((size_t)a.slots * a.heads * cache->head_dim << p.log_rows);
   }
-  if (status_dev != nullptr) {
-    hipLaunchKernelGGL(refuse_kernel, dim3((a.req.n + kBlockThreads - 1) / kBlockThreads), dim3(kBlockThreads), 0, s, a);
-    KVH_HIP_CHECK_LAUNCH();
-  }
-  const dim3 grid((unsigned)(p.items * a.heads));
+  const dim3 grid((unsigned)blocks);
   if (p.nr == 0)
     launch_attention_many(a, dt, cache->kind, cache->head_dim, grid.x, s);
   else if (dt == KVH_F16)
@@ -634,10 +763,11 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
     launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, p.nr, grid, s);
   KVH_HIP_CHECK_LAUNCH();
   if (cut) {
+    a.by_heads = Divisor((uint32_t)a.heads);
     if (dt == KVH_F16)
-      launch_join<KVH_F16>(a, cache->head_dim, p.rows, s);
+      launch_join<KVH_F16>(a, p.tiles, cache->head_dim, p.log_rows, s);
     else
-      launch_join<KVH_BF16>(a, cache->head_dim, p.rows, s);
+      launch_join<KVH_BF16>(a, p.tiles, cache->head_dim, p.log_rows, s);
     KVH_HIP_CHECK_LAUNCH();
   }
   return KVH_OK;

@@ -6,7 +6,7 @@
 namespace kvh {
 
 constexpr int kStep = 32;  // tokens a wave takes at once: two tiles of 16
-constexpr int kManyRows = 128;  // a tile of the kernel for many rows (kvh_attention_many.hip)
+constexpr int kLogManyRows = 7, kManyRows = 1 << kLogManyRows;  // a tile of the kernel for many rows (kvh_attention_many.hip)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLeastScale = 0x1p-60f;  // V scales below it keep it in the exponent; the rest goes onto the weight
 
@@ -25,104 +25,203 @@ struct AttnParams {
   int32_t* status;
   float* part;       // partial outputs [slot][rows][D], then (maximum, sum) [slot][rows][2]; nullptr: nothing is split
   float* part_ml;
-  int target;        // items that the batch is cut into, about
-  int least;         // steps of an item at least, where a request is cut
-  int64_t items;     // partial results that there is room for, of each head
-  Divisor by_block, by_group, by_heads;
+  struct Joint* joints;  // of the tiles, for the joining kernel, and how many they are
+  int32_t* joints_n;
+  int target;        // chunks that the batch is cut into
+  int least;         // steps of a chunk at least
+  int64_t slots;     // partial results that there is room for, of each head
+  int64_t tiles;     // tiles of the batch at most
+  int log_hw;        // few rows: a block's waves take 2^log_hw heads
+  Divisor by_block, by_group, by_heads;  // by_heads: heads, or groups of them that a block takes
 };
 
 // ---- items --------------------------------------------------------------------------------------------------------
-// A request's rows come in tiles of `tile_rows`, its tokens in steps of 32, and an item is a tile and a run of `chunk` steps.  All
-// blocks work out the same list from the lengths: no block is idle while another has two requests' worth of tokens, and the host
-// need not know the lengths.
-__device__ __forceinline__ int steps_of(const AttnParams& a, const Request& rq, int tile_rows) {
-  if (!rq.ok || rq.n == 0) return 0;
+// A request's rows come in tiles, its tokens in steps of 32; the tiles of a batch, each with its steps, make one long row of steps.  Where
+// the batch is cut, that row is cut every `chunk` steps and block k of the grid takes chunk k, one tile after the other: no block has more to do
+// than another.  All blocks work out the same cuts from the lengths, which the host need not know.  The partial result of tile r (counted
+// over the batch) in chunk k has place k + r: a tile's last chunk is the next one's first, or lies before it.  Where nothing is cut, block r
+// takes tile r.
+__device__ __forceinline__ int steps_of(const AttnParams& a, const Request& rq, int log_rows) {
   const int all = (rq.len + kStep - 1) / kStep;
-  if (a.window == 0) return all;
-  const int64_t reach = (int64_t)a.window + tile_rows + 4 * kStep;  // of a tile's rows, with two steps begun on either side
-  const int64_t some = reach / kStep + (a.sink + kStep - 1) / kStep + 1;
-  return all < some ? all : (int)some;
+  int64_t some = all;
+  if (a.window != 0) {
+    const int64_t reach = (int64_t)a.window + (1 << log_rows) + 4 * kStep;  // of a tile's rows, with two steps begun on either side
+    some = reach / kStep + (a.sink + kStep - 1) / kStep + 1;
+  }
+  const int steps = all < some ? all : (int)some;
+  return steps < 2 ? 2 : steps + 1 & ~1;  // some, also where there is no token: its rows have to be written
 }
 
 struct Item {
-  int b, tile, part, parts;  // parts: of the request's tokens
-  int tiles;                 // of the request's rows; the last one, which sees the most tokens, comes first
-  int chunk;
+  int b, tile, tiles;  // request; tile of its rows, and how many they are
+  int from, count;     // steps of the tile
+  bool last, split;    // its last ones; some of them are another item's
+  int64_t slot;        // of its partial result
   Request rq;
 };
 
-__device__ __forceinline__ Request read_request(const AttnParams& a, int b) {
-  Request rq{0, 0, 0, false};
-  if (b < a.req.n) {
-    rq.start = a.req.starts[b];
-    const int32_t end = a.req.starts[b + 1];
-    rq.len = a.req.lens[b];
-    rq.n = end - rq.start;
-    rq.ok = request_ok(a.req, rq.start, end, rq.len);
-  }
-  return rq;
-}
+// What the joining kernel has to know of a tile, written by the block that has its first part.
+struct Joint {
+  int32_t start, n, len, tile;  // of the request; the tile of its rows
+  int32_t parts, spare;
+  int64_t slot;                 // of the first one
+};
+static_assert(sizeof(Joint) == 32, "two 16-byte accesses");
 
-// Steps of an item, from the steps of the batch.
-__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows, int lane) {
-  if (a.part == nullptr) return 0x7fffffff;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
-    const Request rq = read_request(a, b0 + lane);
-    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
-    int64_t s = (int64_t)tiles * steps_of(a, rq, tile_rows);
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) s += __shfl_xor((long long)s, d);
-    total += s;
+// Quotients by a number of the launch that only the device knows; both below 2^50.
+struct WideDivisor {
+  int64_t d;
+  double inv;
+  __device__ __forceinline__ explicit WideDivisor(int64_t d_) : d(d_), inv(1.0 / (double)d_) {}
+  __device__ __forceinline__ int64_t quotient(int64_t x) const {
+    int64_t q = (int64_t)((double)x * inv);  // within one of it
+    const int64_t r = x - q * d;
+    if (r < 0) --q;
+    if (r >= d) ++q;
+    return q;
   }
-  int64_t chunk = (total + a.target - 1) / a.target;
-  if (chunk < a.least) chunk = a.least;
-  chunk = (chunk + 3) & ~(int64_t)3;  // four waves share it
-  return chunk < 0x7fffffff ? (int)chunk : 0x7fffffff;
-}
+};
 
-// The request whose item (or, with by_row, whose packed row) `want` is.  Returns false where there is none.
-__device__ __forceinline__ bool find_item(const AttnParams& a, int tile_rows, int64_t want, bool by_row, int lane, Item& it) {
-  it.chunk = uniform(chunk_of(a, tile_rows, lane));
-  int64_t base = 0;
-  for (int b0 = 0; b0 < a.req.n; b0 += kWave) {
-    const Request rq = read_request(a, b0 + lane);
-    const int steps = steps_of(a, rq, tile_rows);
-    const int tiles = (int)(((int64_t)(rq.ok ? rq.n : 0) * a.group + tile_rows - 1) / tile_rows);
-    int parts = steps == 0 ? 1 : 1 + (steps - 1) / it.chunk;
-    const int64_t mine = (int64_t)tiles * parts;
-    int64_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int64_t o = __shfl_up((long long)upto, d);
-      if (lane >= d) upto += o;
-    }
-    const bool here = by_row ? rq.ok && want >= rq.start && want < (int64_t)rq.start + rq.n
-                             : want >= base + upto - mine && want < base + upto;
-    const uint64_t who = __ballot(here);
-    if (who != 0) {
-      const int l = __builtin_ctzll(who);
-      it.b = b0 + l;
-      it.rq.start = uniform(__shfl(rq.start, l));
-      it.rq.n = uniform(__shfl(rq.n, l));
-      it.rq.len = uniform(__shfl(rq.len, l));
-      it.rq.ok = true;
-      it.parts = uniform(__shfl(parts, l));
-      it.tiles = uniform(__shfl(tiles, l));
-      const int64_t first = base + __shfl((long long)(upto - mine), l);
-      if (by_row) {
-        it.tile = 0;
-        it.part = (int)first;  // the request's first item
-      } else {
-        const int in = uniform((int)(want - first));
-        it.tile = it.tiles - 1 - in / it.parts;
-        it.part = in % it.parts;
+struct Schedule {
+  const AttnParams& a;
+  const int log_rows, lane;
+  // of request b0 + lane: its tiles and the steps of each, and the tiles and steps up to its end
+  int b0, tiles, steps;
+  Request rq;
+  int64_t tile_end, step_end;
+
+  __device__ __forceinline__ Schedule(const AttnParams& a_, int log_rows_, int lane_) : a(a_), log_rows(log_rows_), lane(lane_) { group(0, 0, 0); }
+
+  __device__ __forceinline__ void group(int first, int64_t tile_base, int64_t step_base) {
+    b0 = first;
+    rq = Request{0, 0, 0, false};
+    tiles = steps = 0;
+    const int b = first + lane;
+    if (b < a.req.n) {
+      rq.start = a.req.starts[b];
+      const int32_t end = a.req.starts[b + 1];
+      rq.len = a.req.lens[b];
+      rq.n = end - rq.start;
+      rq.ok = request_ok(a.req, rq.start, end, rq.len);
+      if (rq.ok && rq.n > 0) {
+        tiles = (int)(((int64_t)rq.n * a.group + (1 << log_rows) - 1) >> log_rows);
+        steps = steps_of(a, rq, log_rows);
       }
-      return true;
     }
-    base += __shfl((long long)upto, kWave - 1);
+    tile_end = tiles, step_end = (int64_t)tiles * steps;
+    const int many = a.req.n - first;
+    for (int d = 1; d < kWave && d < many; d *= 2) {
+      const int64_t t = __shfl_up((long long)tile_end, d), s = __shfl_up((long long)step_end, d);
+      if (lane >= d) tile_end += t, step_end += s;
+    }
+    // lanes past the last request stand at its end
+    if (many < kWave) {
+      const int64_t t = __shfl((long long)tile_end, many - 1), s = __shfl((long long)step_end, many - 1);
+      if (lane >= many) tile_end = t, step_end = s;
+    }
+    tile_end += tile_base, step_end += step_base;
   }
-  return false;
+  __device__ __forceinline__ bool next_group() {
+    if (b0 + kWave >= a.req.n) return false;
+    group(b0 + kWave, __shfl((long long)tile_end, kWave - 1), __shfl((long long)step_end, kWave - 1));
+    return true;
+  }
+
+  // The lane of the request for which `here` holds, with its group in the lanes; -1 where there is none.
+  template <typename F>
+  __device__ __forceinline__ int find(F&& here) {
+    do {
+      const uint64_t who = __ballot(rq.ok && here());
+      if (who != 0) return __builtin_ctzll(who);
+    } while (next_group());
+    return -1;
+  }
+
+  __device__ __forceinline__ void take(int l, Item& it) const {
+    it.b = b0 + l;
+    it.rq.start = uniform(__shfl(rq.start, l));
+    it.rq.n = uniform(__shfl(rq.n, l));
+    it.rq.len = uniform(__shfl(rq.len, l));
+    it.rq.ok = true;
+    it.tiles = uniform(__shfl(tiles, l));
+  }
+
+  // Item `k` of a batch that is not cut.  A request's last tile, which sees the most tokens, comes first.
+  __device__ __forceinline__ bool whole(int64_t k, Item& it) {
+    const int l = find([&] { return k < tile_end && k >= tile_end - tiles; });
+    if (l < 0) return false;
+    take(l, it);
+    it.tile = uniform((int32_t)(__shfl((long long)tile_end, l) - k)) - 1;
+    it.from = 0, it.count = uniform(__shfl(steps, l));
+    it.last = true, it.split = false;
+    it.slot = 0;
+    return true;
+  }
+
+  // Of a batch that is cut: what chunk k holds from step `at` on (its first, if `at` is negative) that is of one tile; `at` becomes the step
+  // after.  `tells`: this block writes what the joining kernel has to know.
+  __device__ __forceinline__ bool part(int64_t k, int64_t& at, int64_t& past, Item& it, bool tells) {
+    while (next_group()) {}
+    const int64_t total = uniform((int64_t)__shfl((long long)step_end, kWave - 1));
+    if (tells && k == 0) {
+      const int64_t n = __shfl((long long)tile_end, kWave - 1);
+      if (lane == 0) *a.joints_n = (int32_t)(n < a.tiles ? n : a.tiles);
+    }
+    int64_t size = (total + a.target - 1) / a.target;
+    if (size < a.least) size = a.least;
+    const WideDivisor chunk(uniform((size + 3) & ~(int64_t)3));  // four waves may share it
+    if (at < 0) at = k * chunk.d;
+    const int64_t mine = (k + 1) * chunk.d < total ? (k + 1) * chunk.d : total;
+    past = mine;
+    if (at >= mine) return false;
+    if (a.req.n > kWave) group(0, 0, 0);
+    const int l = find([&] { return at < step_end && at >= step_end - (int64_t)tiles * steps; });
+    if (l < 0) return false;
+    take(l, it);
+    const int each = uniform(__shfl(steps, l));
+    const int64_t step0 = uniform((int64_t)__shfl((long long)(step_end - (int64_t)tiles * steps), l));
+    const int64_t tile0 = uniform((int64_t)__shfl((long long)(tile_end - tiles), l));
+    it.tile = it.tiles > 1 ? uniform((int32_t)((at - step0) / each)) : 0;
+    const int64_t begin = step0 + (int64_t)it.tile * each, end = begin + each, rank = tile0 + it.tile;
+    it.from = (int)(at - begin);
+    it.last = end <= mine;
+    it.count = (int)((it.last ? end : mine) - at);
+    it.split = at > begin || !it.last;
+    it.slot = k + rank;
+    if (tells && at == begin && lane == 0 && rank < a.tiles) {
+      Joint j;
+      j.start = it.rq.start, j.n = it.rq.n, j.len = it.rq.len, j.tile = it.tile;
+      j.parts = (int32_t)(uniform(chunk.quotient(end - 1)) - k) + 1;
+      j.spare = 0;
+      j.slot = it.slot;
+      const u32x4* w = reinterpret_cast<const u32x4*>(&j);
+      u32x4* p = reinterpret_cast<u32x4*>(a.joints + rank);
+      p[0] = w[0], p[1] = w[1];
+    }
+    at += it.count;
+    return true;
+  }
+};
+
+// The items of block k, one after the other.  (lane is made opaque: what follows from it is worked out anew for each item, and does not take
+// registers from one to the next.)
+struct Items {
+  int64_t at = -1, past = 0;  // steps of a batch that is cut: the next one, and the end of the block's
+  __device__ __forceinline__ bool next(const AttnParams& a, int log_rows, int64_t k, bool tells, int& lane, Item& it) {
+    if (at >= past) return false;
+    asm volatile("" : "+v"(lane));
+    Schedule schedule(a, log_rows, lane);
+    if (a.part != nullptr) return schedule.part(k, at, past, it, tells);
+    at = past = 0;
+    return schedule.whole(k, it);
+  }
+};
+
+// Says which requests are refused; the kernels pass over them.
+__device__ __forceinline__ void tell_refused(const AttnParams& a) {
+  if (blockIdx.x != 0 || a.status == nullptr) return;
+  for (int b = threadIdx.x; b < a.req.n; b += kBlockThreads)
+    if (!request_ok(a.req, a.req.starts[b], a.req.starts[b + 1], a.req.lens[b])) a.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
 // ---- operands -----------------------------------------------------------------------------------------------------
@@ -238,11 +337,10 @@ struct Steps {
     count = end > 0 ? sunk + (end + kStep - 1) / kStep - first : 0;
   }
   __device__ __forceinline__ int token(int step) const { return (step < sunk ? step : step - sunk + first) * kStep; }
-  // The steps [begin, end) of part `part` of `parts`, `chunk` steps each.
+  // Of an item's, those there are.
   __device__ __forceinline__ void part_of(const Item& it, int& begin, int& end) const {
-    const int64_t b = (int64_t)it.part * it.chunk, e = b + it.chunk;
-    begin = uniform((int32_t)(b < count ? b : count));
-    end = uniform((int32_t)(it.part + 1 == it.parts || e > count ? count : e));
+    begin = it.from < count ? it.from : count;
+    end = it.last || it.from + it.count > count ? count : it.from + it.count;
   }
 };
 

@@ -19,7 +19,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kManyTokens = 64;             // of a tile
+constexpr int kManyTokens = 64;  // of a tile
 constexpr int kManyWaveRows = 32;
 static_assert(kManyRows == kManyWaveRows * kWavesPerBlock, "rows of a block");
 
@@ -311,18 +311,21 @@ struct Tiles {
 };
 
 template <int DT, int KIND, int D, bool PAGE16>
-__global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnParams a) {
+struct Shared {
+  using T = Tiles<DT, KIND, D, PAGE16>;
+  __attribute__((aligned(16))) uint8_t buffers[2 * T::kBuffer];
+  __attribute__((aligned(16))) float scales[2][3][T::kScales];
+  uint32_t odd[2][kWavesPerBlock];
+};
+
+template <int DT, int KIND, int D, bool PAGE16>
+__device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int head, int wave, int lane, Shared<DT, KIND, D, PAGE16>& shared) {
   using T = Tiles<DT, KIND, D, PAGE16>;
   constexpr bool kScaled = KIND != KVH_CACHE_16;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * T::kBuffer];
-  __shared__ uint32_t odd[2][kWavesPerBlock];
-  __shared__ __attribute__((aligned(16))) float scales[2][3][T::kScales];
-  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  uint8_t* lds = shared.buffers;
+  auto& odd = shared.odd;
+  auto& scales = shared.scales;
   const int col = lane % 32, half = lane / 32;
-  const uint32_t item = a.by_heads.quotient(blockIdx.x);
-  const int head = (int)(blockIdx.x - item * (uint32_t)a.heads);
-  Item it;
-  if (!find_item(a, kManyRows, item, false, lane, it)) return;
   const Request rq = it.rq;
   const int all = rq.n * a.group;
   const int row0 = it.tile * kManyRows;
@@ -581,9 +584,9 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
   const float sum = l + __shfl_xor(l, 32);
-  if (it.parts > 1) {
+  if (it.split) {
     if (real) {
-      const int64_t row = (int64_t)blockIdx.x * kManyRows + wave * kManyWaveRows + col;
+      const int64_t row = (it.slot * a.heads + head) * kManyRows + wave * kManyWaveRows + col;
       float* to = a.part + row * D + 4 * half;
 #pragma unroll
       for (int c = 0; c < T::kOuts; ++c)
@@ -625,12 +628,40 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
     a.lse[((int64_t)rq.start + token) * ((int64_t)a.heads * a.group) + (int64_t)head * a.group + u] = blind ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
+template <int DT, int KIND, int D, bool PAGE16, bool CUT>
+__global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnParams a) {
+  __shared__ Shared<DT, KIND, D, PAGE16> shared;
+  int lane = threadIdx.x % kWave;
+  const int wave = uniform((int32_t)(threadIdx.x / kWave));
+  const uint32_t k = a.by_heads.quotient(blockIdx.x);
+  const int head = (int)(blockIdx.x - k * (uint32_t)a.heads);
+  tell_refused(a);
+  Item it;
+  if constexpr (!CUT) {
+    if (Schedule(a, kLogManyRows, lane).whole(k, it)) attend<DT, KIND, D, PAGE16>(a, it, head, wave, lane, shared);
+  } else {
+    for (Items items; items.next(a, kLogManyRows, k, head == 0 && wave == 0, lane, it);) {
+      if (it.split && it.slot >= a.slots) continue;  // requests that share rows of the batch
+      attend<DT, KIND, D, PAGE16>(a, it, head, wave, lane, shared);
+      __syncthreads();
+    }
+  }
+}
+
+template <int DT, int KIND, int D, bool PAGE16>
+void launch_cut(const AttnParams& a, unsigned blocks, hipStream_t stream) {
+  if (a.part != nullptr)
+    launch_kernel(attention_many_kernel<DT, KIND, D, PAGE16, true>, dim3(blocks), dim3(kBlockThreads), 0, stream, a);
+  else
+    launch_kernel(attention_many_kernel<DT, KIND, D, PAGE16, false>, dim3(blocks), dim3(kBlockThreads), 0, stream, a);
+}
+
 template <int DT, int KIND, int D>
 void launch_pages(const AttnParams& a, unsigned blocks, hipStream_t stream) {
   if (a.block_tokens % 16 == 0)
-    launch_kernel(attention_many_kernel<DT, KIND, D, true>, dim3(blocks), dim3(kBlockThreads), 0, stream, a);
+    launch_cut<DT, KIND, D, true>(a, blocks, stream);
   else
-    launch_kernel(attention_many_kernel<DT, KIND, D, false>, dim3(blocks), dim3(kBlockThreads), 0, stream, a);
+    launch_cut<DT, KIND, D, false>(a, blocks, stream);
 }
 
 template <int DT, int KIND>
