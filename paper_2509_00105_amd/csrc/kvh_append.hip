@@ -1,16 +1,17 @@
 // kvh_append: keys and values of new tokens go into the pages of the serving cache, keys and queries rotated on the way.
 //
-// A wave takes a unit: one head of K, of V or of q, and some rows of one request.  The rows of a 16-bit cache are independent
-// and come in tiles of 16; an 8-bit page is described by one scale a head, so there the unit is a page: its new rows are read
-// and rotated, their largest magnitude is found across the wave, and they are stored as codes.  A lane holds 8 neighbouring
-// channels (one 16-byte load, one 16- or 8-byte store), D / 8 lanes a row; the other half of a rotated pair is 0 lanes away or
-// rot / 16 lanes, and comes by a lane exchange, which also makes q_out == q safe.
+// A lane holds 8 neighbouring channels (one 16-byte load, one 16- or 8-byte store), D / 8 lanes a head.  A wave takes a unit of one
+// request.  Queries, and keys and values of a 16-bit cache: some rows of 512 / D neighbouring heads, so that an access is 1 KiB of one token and
+// its lanes share the row's cosines and sines.  An 8-bit page is described by one scale a head, so there the unit is a page
+// and a head: its new rows are read and rotated, their largest magnitude is found across the wave, and they are stored as codes.  The
+// other half of a rotated pair is 0 lanes away or rot / 16 lanes, and comes by a lane exchange, which also makes q_out == q safe.
 #include "kvh_cache.hpp"
 
 namespace kvh {
 namespace {
 
-constexpr int kTileRows = 16;
+constexpr int kPageRows = 16;  // rows of an 8-bit page that are taken at once
+constexpr int kTileRows = 4;   // and of a unit of queries or of a 16-bit cache (8K prompt, e4m3: 41.4 us; 8 rows 44.0, 16 rows 51)
 
 struct AppendParams {
   Requests req;
@@ -28,24 +29,91 @@ struct AppendParams {
   int n_positions, rot, pairs;  // rot 0: nothing is rotated
   int32_t* status;
   uint32_t kv_units, units;  // of a request and layer
-  Divisor by_block, by_kv, by_q;  // block_tokens; 2 heads; q_heads
+  Divisor by_block, by_kv;  // block_tokens; 2 heads
 };
+
+// Rows that are read once and written once pass by the caches (PAST), unless they are so few that what reads them next finds them there.
+template <bool PAST, typename V>
+__device__ __forceinline__ V get(const void* p) {
+  if constexpr (PAST)
+    return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else
+    return *reinterpret_cast<const V*>(p);
+}
+template <bool PAST, typename V>
+__device__ __forceinline__ void put(void* p, const V& v) {
+  if constexpr (PAST)
+    __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+  else
+    *reinterpret_cast<V*>(p) = v;
+}
+
+// The 8 values of a lane, rotated by row `pos` of the table; cb is its first channel in the head.  All lanes of a head take part.
+template <int DT>
+__device__ __forceinline__ void turn8(const AppendParams& a, const u32x4& raw, int pos, int cb, int lane, float (&x)[8]) {
+  widen8<DT>(raw, x);
+  const float* row = a.table + (int64_t)pos * a.table_stride;
+  if (a.pairs) {
+    if (cb < a.rot) {
+      const f32x4 c = *reinterpret_cast<const f32x4*>(row + cb / 2), n = *reinterpret_cast<const f32x4*>(row + (a.rot + cb) / 2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x1 = x[2 * e], x2 = x[2 * e + 1];
+        x[2 * e] = x1 * c[e] - x2 * n[e];
+        x[2 * e + 1] = x2 * c[e] + x1 * n[e];
+      }
+    }
+    return;
+  }
+  const int half = a.rot / 2, far = half / 8;
+  const bool low = cb < half;
+  const int other = cb < a.rot ? (low ? lane + far : lane - far) : lane;
+  u32x4 ow;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ow[e] = (uint32_t)__shfl((int)raw[e], other);
+  if (cb < a.rot) {
+    float y[8];
+    widen8<DT>(ow, y);
+    const float* t = row + (low ? cb : cb - half);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const f32x4 c = *reinterpret_cast<const f32x4*>(t + 4 * p), n = *reinterpret_cast<const f32x4*>(t + half + 4 * p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float& v = x[4 * p + e];
+        const float part = y[4 * p + e] * n[e];
+        v = low ? v * c[e] - part : v * c[e] + part;
+      }
+    }
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 packed8(const float (&x)[8]) {
+  return u32x4{narrow2<DT>(x[0], x[1]), narrow2<DT>(x[2], x[3]), narrow2<DT>(x[4], x[5]), narrow2<DT>(x[6], x[7])};
+}
+
+// The position of a request's new token i; -1 where the table has none for it.
+__device__ __forceinline__ int position(const AppendParams& a, const Request& rq, int i) {
+  const int pos = a.positions != nullptr ? a.positions[rq.start + i] : rq.len - rq.n + i;
+  return pos < a.n_positions ? pos : -1;
+}
 
 // One head's rows [i0, i0 + 16) of a request (i < i_end) in registers: D / 8 lanes a row.
 template <int DT, int D>
 struct Tile {
   static constexpr int kLanes = D / 8;
   static constexpr int kRows = kWave / kLanes;  // of one access of the wave
-  static constexpr int kSteps = kTileRows / kRows;
-  u32x4 raw[kSteps];
+  static constexpr int kSteps = kPageRows / kRows;
   float x[kSteps][8];
   bool valid[kSteps];
 
-  // `turn`: rotate into x; otherwise x is the value itself.  Returns whether a token had no position in the table.
+  // `turn`: rotate.  Returns whether a token had no position in the table.
   __device__ __forceinline__ bool load(const AppendParams& a, const uint16_t* src, int64_t ts, const Request& rq, int i0, int i_end,
                                        bool turn, int lane) {
     const int col = lane % kLanes, sub = lane / kLanes;
     bool bad = false;
+    u32x4 raw[kSteps];
     int pos[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -56,8 +124,8 @@ struct Tile {
       if (valid[s]) {
         raw[s] = *reinterpret_cast<const u32x4*>(src + ((int64_t)rq.start + i) * ts + col * 8);
         if (turn) {
-          pos[s] = a.positions != nullptr ? a.positions[rq.start + i] : rq.len - rq.n + i;
-          if (pos[s] < 0 || pos[s] >= a.n_positions) {
+          pos[s] = position(a, rq, i);
+          if (pos[s] < 0) {
             bad = true;
             valid[s] = false;
             pos[s] = 0;
@@ -66,55 +134,13 @@ struct Tile {
       }
     }
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) widen8<DT>(raw[s], x[s]);
-    if (!turn) return false;
-    const int cb = col * 8;
-    if (a.pairs) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        if (valid[s] && cb < a.rot) {
-          const float* t = a.table + (int64_t)pos[s] * a.table_stride + cb / 2;
-          const f32x4 c = *reinterpret_cast<const f32x4*>(t), n = *reinterpret_cast<const f32x4*>(t + a.rot / 2);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x1 = x[s][2 * e], x2 = x[s][2 * e + 1];
-            x[s][2 * e] = x1 * c[e] - x2 * n[e];
-            x[s][2 * e + 1] = x2 * c[e] + x1 * n[e];
-          }
-        }
-    } else {
-      const int half = a.rot / 2, far = half / 8;
-      const bool low = cb < half;
-      const int other = cb < a.rot ? (low ? lane + far : lane - far) : lane;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        u32x4 ow;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ow[e] = (uint32_t)__shfl((int)raw[s][e], other);
-        if (valid[s] && cb < a.rot) {
-          float y[8];
-          widen8<DT>(ow, y);
-          const float* t = a.table + (int64_t)pos[s] * a.table_stride + (low ? cb : cb - half);
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const f32x4 c = *reinterpret_cast<const f32x4*>(t + 4 * p), n = *reinterpret_cast<const f32x4*>(t + half + 4 * p);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float& v = x[s][4 * p + e];
-              const float far_part = y[4 * p + e] * n[e];
-              v = low ? v * c[e] - far_part : v * c[e] + far_part;
-            }
-          }
-        }
-      }
+    for (int s = 0; s < kSteps; ++s) {
+      if (turn)
+        turn8<DT>(a, raw[s], pos[s], col * 8, lane, x[s]);
+      else
+        widen8<DT>(raw[s], x[s]);
     }
     return bad;
-  }
-
-  __device__ __forceinline__ u32x4 packed(int s, bool turned) const {
-    if (!turned) return raw[s];
-    return u32x4{narrow2<DT>(x[s][0], x[s][1]), narrow2<DT>(x[s][2], x[s][3]), narrow2<DT>(x[s][4], x[s][5]),
-                 narrow2<DT>(x[s][6], x[s][7])};
   }
 };
 
@@ -158,7 +184,7 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-template <int DT, int KIND, int D>
+template <int DT, int KIND, int D, bool PAST>
 __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
   using T = Tile<DT, D>;
   const int lane = threadIdx.x % kWave;
@@ -179,43 +205,64 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
   const int before = rq.len - rq.n, col = lane % T::kLanes, sub = lane / T::kLanes;
   const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
   bool bad = false;
-  T t;
-  if (u >= a.kv_units) {  // queries
-    const uint32_t w = u - a.kv_units, tile = a.by_q.quotient(w), head = w - tile * (uint32_t)a.q_heads;
-    const int i0 = (int)tile * kTileRows;
-    if (i0 >= rq.n) return;
-    bad = t.load(a, a.q + layer * a.q_ls + head * D, a.q_ts, rq, i0, rq.n, a.rot != 0, lane);
+  // Rows [i0, i0 + 4) of heads [head0, head0 + 512 / D), from src; `page_of` looks up what `to` needs to say where a row goes
+  // (nullptr: nowhere), in time.
+  auto move_rows = [&](const uint16_t* src, int64_t ts, int heads, uint32_t unit, bool turn, auto&& page_of, auto&& to) {
+    constexpr int kHeads = kWave / T::kLanes, kAtOnce = kTileRows;
+    const uint32_t groups = (uint32_t)(heads + kHeads - 1) / kHeads, tile = unit / groups;
+    const int head = (int)(unit - tile * groups) * kHeads + sub, i0 = (int)tile * kTileRows;
+    const bool mine = head < heads;
+    const int64_t at = (int64_t)(mine ? head : 0) * D + col * 8;
+    if (i0 < rq.n) {
+      u32x4 raw[kAtOnce];
+      int pos[kAtOnce], page[kAtOnce];
 #pragma unroll
-    for (int s = 0; s < T::kSteps; ++s)
-      if (t.valid[s]) {
-        const int64_t row = (int64_t)rq.start + i0 + s * T::kRows + sub;
-        *reinterpret_cast<u32x4*>(a.q_out + layer * a.o_ls + row * a.o_ts + head * D + col * 8) = t.packed(s, a.rot != 0);
+      for (int s = 0; s < kAtOnce; ++s) {
+        const int i = i0 + s < rq.n ? i0 + s : rq.n - 1;
+        page[s] = page_of(i);
+        raw[s] = get<PAST, u32x4>(src + ((int64_t)rq.start + i) * ts + at);
+        pos[s] = turn ? position(a, rq, i) : 0;
       }
-  } else {
-    const uint32_t part = a.by_kv.quotient(u);
-    uint32_t head = u - part * 2u * (uint32_t)a.heads;
-    const bool is_v = head >= (uint32_t)a.heads;
-    if (is_v) head -= a.heads;
-    const uint16_t* src = (is_v ? a.v : a.k) + layer * a.kv_ls + head * D;
-    const bool turn = !is_v && a.rot != 0;
-    uint8_t* cache = (is_v ? a.cv : a.ck) + (layer * a.c_ls + head * D) * (KIND == KVH_CACHE_16 ? 2 : 1);
-    if constexpr (KIND == KVH_CACHE_16) {
-      const int i0 = (int)part * kTileRows;
-      if (i0 >= rq.n) return;
-      bad = t.load(a, src, a.kv_ts, rq, i0, rq.n, turn, lane);
 #pragma unroll
-      for (int s = 0; s < T::kSteps; ++s) {
-        const int slot = before + i0 + s * T::kRows + sub;
-        if (!t.valid[s]) continue;
-        const int at = (int)a.by_block.quotient((uint32_t)slot), page = table[at];
-        if (page < 0 || page >= a.pages) {
-          bad = true;
-          continue;
+      for (int s = 0; s < kAtOnce; ++s) {
+        if (turn) {
+          float x[8];
+          turn8<DT>(a, raw[s], pos[s] < 0 ? 0 : pos[s], col * 8, lane, x);
+          raw[s] = packed8<DT>(x);
         }
-        const int64_t row = (int64_t)page * a.block_tokens + (slot - at * a.block_tokens);
-        *reinterpret_cast<u32x4*>(cache + (row * a.c_ts + col * 8) * 2) = t.packed(s, turn);
+        if (i0 + s >= rq.n) continue;
+        uint16_t* row = pos[s] < 0 ? nullptr : to(i0 + s, page[s]);
+        if (row == nullptr)
+          bad = true;
+        else if (mine)
+          put<PAST>(row + at, raw[s]);
       }
+    }
+  };
+  if (u >= a.kv_units) {  // queries
+    uint16_t* out = a.q_out + layer * a.o_ls;
+    move_rows(a.q + layer * a.q_ls, a.q_ts, a.q_heads, u - a.kv_units, a.rot != 0, [](int) { return 0; },
+              [&](int i, int) { return out + ((int64_t)rq.start + i) * a.o_ts; });
+  } else {
+    if constexpr (KIND == KVH_CACHE_16) {
+      const bool is_v = u >= a.kv_units / 2;
+      uint16_t* cache = reinterpret_cast<uint16_t*>(is_v ? a.cv : a.ck) + layer * a.c_ls;
+      move_rows((is_v ? a.v : a.k) + layer * a.kv_ls, a.kv_ts, a.heads, is_v ? u - a.kv_units / 2 : u, !is_v && a.rot != 0,
+                [&](int i) { return table[a.by_block.quotient((uint32_t)(before + i))]; },
+                [&](int i, int page) -> uint16_t* {
+                  if (page < 0 || page >= a.pages) return nullptr;
+                  const int slot = before + i, at = (int)a.by_block.quotient((uint32_t)slot);
+                  return cache + ((int64_t)page * a.block_tokens + (slot - at * a.block_tokens)) * a.c_ts;
+                });
     } else {
+      const uint32_t part = a.by_kv.quotient(u);
+      uint32_t head = u - part * 2u * (uint32_t)a.heads;
+      const bool is_v = head >= (uint32_t)a.heads;
+      if (is_v) head -= a.heads;
+      const uint16_t* src = (is_v ? a.v : a.k) + layer * a.kv_ls + head * D;
+      const bool turn = !is_v && a.rot != 0;
+      uint8_t* cache = (is_v ? a.cv : a.ck) + layer * a.c_ls + head * D;
+      T t;
       const int at = (int)a.by_block.quotient((uint32_t)before) + (int)part;  // the page's place in the request
       const int64_t page_slot = (int64_t)at * a.block_tokens;
       const int i0 = page_slot > before ? (int)(page_slot - before) : 0;
@@ -223,6 +270,7 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
       const int64_t past = page_slot + a.block_tokens - before;
       const int i_end = past < rq.n ? (int)past : rq.n;
       const int page = table[at];
+      bad = t.load(a, src, a.kv_ts, rq, i0, i_end, turn, lane);  // on the way while the page is looked up
       if (page < 0 || page >= a.pages) {
         if (tells) a.status[b] = KVH_DEV_BAD_REQUEST;
         return;
@@ -231,8 +279,8 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
       float* scale_at = (is_v ? a.sv : a.sk) + layer * a.s_ls + (int64_t)page * a.s_ps + head;
       const float old = row0 > 0 ? *scale_at : 0.0f;
       float most = 0.0f;
-      for (int i = i0; i < i_end; i += kTileRows) {
-        bad |= t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);
+      for (int i = i0; i < i_end; i += kPageRows) {
+        if (i > i0) bad |= t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);
 #pragma unroll
         for (int s = 0; s < T::kSteps; ++s)
           if (t.valid[s]) {
@@ -256,8 +304,8 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
           *p = codes8<KIND>(y);
         }
       }
-      for (int i = i0; i < i_end; i += kTileRows) {
-        if (i_end - i0 > kTileRows) t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);  // otherwise the rows are still here
+      for (int i = i0; i < i_end; i += kPageRows) {
+        if (i_end - i0 > kPageRows) t.load(a, src, a.kv_ts, rq, i, i_end, turn, lane);  // otherwise the rows are still here
 #pragma unroll
         for (int s = 0; s < T::kSteps; ++s)
           if (t.valid[s]) {
@@ -265,7 +313,7 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = t.x[s][e] * inv;
             const int r = row0 + (i - i0) + s * T::kRows + sub;
-            *reinterpret_cast<u32x2*>(rows + (int64_t)r * a.c_ts) = codes8<KIND>(y);
+            put<PAST>(rows + (int64_t)r * a.c_ts, codes8<KIND>(y));
           }
       }
       if (lane == 0) *scale_at = now;
@@ -274,20 +322,28 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
   if (__any(bad) && tells) a.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
-template <int DT, int KIND>
-void launch_dim(const AppendParams& a, int head_dim, dim3 grid, hipStream_t stream) {
-  if (head_dim == 128)
-    launch_kernel(append_kernel<DT, KIND, 128>, grid, dim3(kBlockThreads), 0, stream, a);
+template <int DT, int KIND, int D>
+void launch_past(const AppendParams& a, bool past, dim3 grid, hipStream_t stream) {
+  if (past)
+    launch_kernel(append_kernel<DT, KIND, D, true>, grid, dim3(kBlockThreads), 0, stream, a);
   else
-    launch_kernel(append_kernel<DT, KIND, 64>, grid, dim3(kBlockThreads), 0, stream, a);
+    launch_kernel(append_kernel<DT, KIND, D, false>, grid, dim3(kBlockThreads), 0, stream, a);
+}
+
+template <int DT, int KIND>
+void launch_dim(const AppendParams& a, int head_dim, bool past, dim3 grid, hipStream_t stream) {
+  if (head_dim == 128)
+    launch_past<DT, KIND, 128>(a, past, grid, stream);
+  else
+    launch_past<DT, KIND, 64>(a, past, grid, stream);
 }
 
 template <int DT>
-void launch_kind(const AppendParams& a, int kind, int head_dim, dim3 grid, hipStream_t stream) {
+void launch_kind(const AppendParams& a, int kind, int head_dim, bool past, dim3 grid, hipStream_t stream) {
   switch (kind) {
-    case KVH_CACHE_16: return launch_dim<DT, KVH_CACHE_16>(a, head_dim, grid, stream);
-    case KVH_CACHE_I8: return launch_dim<DT, KVH_CACHE_I8>(a, head_dim, grid, stream);
-    default: return launch_dim<DT, KVH_CACHE_E4M3>(a, head_dim, grid, stream);
+    case KVH_CACHE_16: return launch_dim<DT, KVH_CACHE_16>(a, head_dim, past, grid, stream);
+    case KVH_CACHE_I8: return launch_dim<DT, KVH_CACHE_I8>(a, head_dim, past, grid, stream);
+    default: return launch_dim<DT, KVH_CACHE_E4M3>(a, head_dim, past, grid, stream);
   }
 }
 
@@ -342,20 +398,22 @@ extern "C" int kvh_append(const kvh_cache* cache, const kvh_requests* requests, 
   a.status = status_dev;
   a.by_block = Divisor((uint32_t)cache->block_tokens);
   a.by_kv = Divisor(2u * (uint32_t)cache->heads);
-  a.by_q = Divisor((uint32_t)(a.q_heads > 0 ? a.q_heads : 1));
   const int most = requests->max_new < requests->n_tokens ? requests->max_new : requests->n_tokens;
   a.req.max_new = most;
-  const int64_t tiles = (most + kTileRows - 1) / kTileRows;
+  const int64_t tiles = (most + kTileRows - 1) / kTileRows, together = 512 / cache->head_dim;  // heads of a unit
   const int64_t spread = ((int64_t)most + cache->block_tokens - 2) / cache->block_tokens + 1;  // pages that `most` tokens touch at most
-  const int64_t parts = cache->kind == KVH_CACHE_16 ? tiles : spread < most ? spread : most;
-  const int64_t kv_units = parts * 2 * cache->heads, units = kv_units + tiles * a.q_heads;
+  const int64_t parts = spread < most ? spread : most;
+  const int64_t kv_units = 2 * (cache->kind == KVH_CACHE_16 ? tiles * ((cache->heads + together - 1) / together) : parts * cache->heads);
+  const int64_t units = kv_units + tiles * ((a.q_heads + together - 1) / together);
+  // Measured at 8K tokens of 8 + 32 heads, e4m3: 39.6 us by the caches, 46.2 through them; at 64 single tokens the two are alike.
+  const bool past = (int64_t)requests->n_tokens * cache->layers * (2 * cache->heads + a.q_heads) * cache->head_dim >= (int64_t)4 << 20;
   if (units >= (int64_t)1 << 31) return KVH_E_SHAPE;
   a.kv_units = (uint32_t)kv_units, a.units = (uint32_t)units;
   const dim3 grid((unsigned)((units + kWavesPerBlock - 1) / kWavesPerBlock), (unsigned)requests->n_requests, (unsigned)cache->layers);
   if (dt == KVH_F16)
-    launch_kind<KVH_F16>(a, cache->kind, cache->head_dim, grid, static_cast<hipStream_t>(stream));
+    launch_kind<KVH_F16>(a, cache->kind, cache->head_dim, past, grid, static_cast<hipStream_t>(stream));
   else
-    launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, grid, static_cast<hipStream_t>(stream));
+    launch_kind<KVH_BF16>(a, cache->kind, cache->head_dim, past, grid, static_cast<hipStream_t>(stream));
   KVH_HIP_CHECK_LAUNCH();
   return KVH_OK;
 }

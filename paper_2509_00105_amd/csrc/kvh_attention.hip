@@ -662,7 +662,7 @@ void launch_kind(const AttnParams& a, int kind, int head_dim, int nr, dim3 grid,
 template <int DT, int D>
 void launch_join(const AttnParams& a, int64_t tiles, int log_rows, hipStream_t stream) {
   const int64_t rows = tiles * a.heads << log_rows;
-  if (tiles * a.heads <= 256)
+  if (rows <= 4096)  // one of 128K tokens (128 rows, 256 parts): 10 us, 23 with a wave a row; 512 after 32K (17408 rows, 4 parts): 11 us, 33 with four
     hipLaunchKernelGGL((join_kernel<DT, D, kWavesPerBlock>), dim3((unsigned)rows), dim3(kBlockThreads), 0, stream, a, log_rows);
   else
     hipLaunchKernelGGL((join_kernel<DT, D, 1>), dim3((unsigned)(rows / kWavesPerBlock)), dim3(kBlockThreads), 0, stream, a, log_rows);
