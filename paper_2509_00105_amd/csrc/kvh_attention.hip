@@ -511,7 +511,7 @@ __global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void attention_kernel(A
 // The parts' factors come first, 64 in the lanes, so that the sums are loads that wait for nothing but each other.
 template <int DT, int D, int WAVES>
 __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int log_rows) {
-  constexpr int kPer = D / 64, kAtOnce = 8, kLogRows = WAVES == 1 ? 2 : 0;  // of a block
+  constexpr int kPer = D / 64, kAtOnce = WAVES == 1 ? 8 : 16, kLogRows = WAVES == 1 ? 2 : 0;  // of a block
   __shared__ float lds[WAVES > 1 ? WAVES : 1][D];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   const uint32_t unit = blockIdx.x >> (log_rows - kLogRows), tile = a.by_heads.quotient(unit);

@@ -82,6 +82,12 @@ struct WideDivisor {
   }
 };
 
+// The value of lane l, which is the same for the whole wave.
+__device__ __forceinline__ int32_t of_lane(int32_t v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ int64_t of_lane(int64_t v, int l) {
+  return (int64_t)((uint64_t)(uint32_t)of_lane((int32_t)((uint64_t)v >> 32), l) << 32 | (uint32_t)of_lane((int32_t)(uint64_t)v, l));
+}
+
 struct Schedule {
   const AttnParams& a;
   const int log_rows, lane;
@@ -116,14 +122,14 @@ struct Schedule {
     }
     // lanes past the last request stand at its end
     if (many < kWave) {
-      const int64_t t = __shfl((long long)tile_end, many - 1), s = __shfl((long long)step_end, many - 1);
+      const int64_t t = of_lane(tile_end, many - 1), s = of_lane(step_end, many - 1);
       if (lane >= many) tile_end = t, step_end = s;
     }
     tile_end += tile_base, step_end += step_base;
   }
   __device__ __forceinline__ bool next_group() {
     if (b0 + kWave >= a.req.n) return false;
-    group(b0 + kWave, __shfl((long long)tile_end, kWave - 1), __shfl((long long)step_end, kWave - 1));
+    group(b0 + kWave, of_lane(tile_end, kWave - 1), of_lane(step_end, kWave - 1));
     return true;
   }
 
@@ -139,11 +145,11 @@ struct Schedule {
 
   __device__ __forceinline__ void take(int l, Item& it) const {
     it.b = b0 + l;
-    it.rq.start = uniform(__shfl(rq.start, l));
-    it.rq.n = uniform(__shfl(rq.n, l));
-    it.rq.len = uniform(__shfl(rq.len, l));
+    it.rq.start = of_lane(rq.start, l);
+    it.rq.n = of_lane(rq.n, l);
+    it.rq.len = of_lane(rq.len, l);
     it.rq.ok = true;
-    it.tiles = uniform(__shfl(tiles, l));
+    it.tiles = of_lane(tiles, l);
   }
 
   // Item `k` of a batch that is not cut.  A request's last tile, which sees the most tokens, comes first.
@@ -151,8 +157,8 @@ struct Schedule {
     const int l = find([&] { return k < tile_end && k >= tile_end - tiles; });
     if (l < 0) return false;
     take(l, it);
-    it.tile = uniform((int32_t)(__shfl((long long)tile_end, l) - k)) - 1;
-    it.from = 0, it.count = uniform(__shfl(steps, l));
+    it.tile = (int32_t)(of_lane(tile_end, l) - k) - 1;
+    it.from = 0, it.count = of_lane(steps, l);
     it.last = true, it.split = false;
     it.slot = 0;
     return true;
@@ -162,9 +168,9 @@ struct Schedule {
   // after.  `tells`: this block writes what the joining kernel has to know.
   __device__ __forceinline__ bool part(int64_t k, int64_t& at, int64_t& past, Item& it, bool tells) {
     while (next_group()) {}
-    const int64_t total = uniform((int64_t)__shfl((long long)step_end, kWave - 1));
+    const int64_t total = of_lane(step_end, kWave - 1);
     if (tells && k == 0) {
-      const int64_t n = __shfl((long long)tile_end, kWave - 1);
+      const int64_t n = of_lane(tile_end, kWave - 1);
       if (lane == 0) *a.joints_n = (int32_t)(n < a.tiles ? n : a.tiles);
     }
     int64_t size = (total + a.target - 1) / a.target;
@@ -178,9 +184,9 @@ struct Schedule {
     const int l = find([&] { return at < step_end && at >= step_end - (int64_t)tiles * steps; });
     if (l < 0) return false;
     take(l, it);
-    const int each = uniform(__shfl(steps, l));
-    const int64_t step0 = uniform((int64_t)__shfl((long long)(step_end - (int64_t)tiles * steps), l));
-    const int64_t tile0 = uniform((int64_t)__shfl((long long)(tile_end - tiles), l));
+    const int each = of_lane(steps, l);
+    const int64_t step0 = of_lane((step_end - (int64_t)tiles * steps), l);
+    const int64_t tile0 = of_lane((tile_end - tiles), l);
     it.tile = it.tiles > 1 ? uniform((int32_t)((at - step0) / each)) : 0;
     const int64_t begin = step0 + (int64_t)it.tile * each, end = begin + each, rank = tile0 + it.tile;
     it.from = (int)(at - begin);
@@ -286,13 +292,30 @@ __device__ __forceinline__ Words<N> fetch(const uint8_t* p) {
   return r;
 }
 
-__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+// The two values of lanes 32 apart, and of lanes 16 apart, in both: moves between lanes without LDS.
+__device__ __forceinline__ f32x2 apart32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
+}
+__device__ __forceinline__ f32x2 apart16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
+}
+__device__ __forceinline__ float over_halves_max(float v) {  // of the 2 lanes that hold a row of the kernel for many rows
+  const f32x2 x = apart32(v);
+  return fmaxf(x[0], x[1]);
+}
+__device__ __forceinline__ float over_halves_sum(float v) {
+  const f32x2 x = apart32(v);
+  return x[0] + x[1];
+}
+__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row of the kernel for few
+  const f32x2 x = apart16(v);
+  return over_halves_max(fmaxf(x[0], x[1]));
 }
 __device__ __forceinline__ float over_groups_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  const f32x2 x = apart16(v);
+  return over_halves_sum(x[0] + x[1]);
 }
 
 // ---- the page table, 64 entries at a time in the lanes ---------------------------------------------------------------

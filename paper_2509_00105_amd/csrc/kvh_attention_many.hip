@@ -367,7 +367,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
       }
-      most = fmaxf(most, __shfl_xor(most, 32));
+      most = over_halves_max(most);
       const f32x2 power = row_power(most);
       coef *= power[1];
 #pragma unroll
@@ -484,7 +484,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
       for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[(g * kPer + j) / 16][(g * kPer + j) % 16]);
       most = fmaxf(most, __builtin_fmaf(top, f[g], z[g]));
     }
-    most = fmaxf(most, __shfl_xor(most, 32));
+    most = over_halves_max(most);
     // The maximum may lag behind by 2^8: weights up to 256 are as good, and the outputs are hardly ever rescaled.
     if (__any(most > m + 8.0f)) {
       const float now = fmaxf(m, most);
@@ -583,7 +583,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   }
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
-  const float sum = l + __shfl_xor(l, 32);
+  const float sum = over_halves_sum(l);
   if (it.split) {
     if (real) {
       const int64_t row = (it.slot * a.heads + head) * kManyRows + wave * kManyWaveRows + col;
