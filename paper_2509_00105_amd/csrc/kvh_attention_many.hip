@@ -56,6 +56,7 @@ struct Tiles {
   // PAGE16: bytes from a group of 16 tokens' first row to what the thread moves of it, and where the next group lies: in the
   // request's page `in`, `past` bytes (and `row` rows) from its start.
   uint32_t k_from, v_from;
+  uint32_t k_to, v_to;  // and where it goes in a buffer
   int in, row;
   int64_t past;
 
@@ -87,6 +88,8 @@ struct Tiles {
     const uint32_t row_bytes = (uint32_t)a.c_ts * kWidth;
     k_from = threadIdx.x / kKUnits % 16 * row_bytes + threadIdx.x % kKUnits * 16;
     v_from = v_unit() % 2 * 4 * row_bytes + v_chan() * kWidth;
+    k_to = (uint32_t)k_place(threadIdx.x / kKUnits, threadIdx.x % kKUnits * (KIND == KVH_CACHE_16 ? 1 : 2));
+    v_to = kKTile + (uint32_t)v_place(v_chan(), v_unit());
   }
 
   static __device__ __forceinline__ void fetch_v(uint32_t (&to)[kVWords], const uint8_t* p) {
@@ -218,21 +221,21 @@ struct Tiles {
 
   // Stores what was fetched into a buffer, as operands.
   __device__ __forceinline__ void store_tile(int buffer) {
-    uint8_t* kb = lds + buffer * kBuffer;
-    uint8_t* vb = kb + kKTile;
+    const uint32_t kb = k_to + buffer * kBuffer, vb = v_to + buffer * kBuffer;
     const int tid = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kKEach; ++i) {
-      const int idx = tid + kBlockThreads * i, token = idx / kKUnits, unit = idx % kKUnits;
+    for (int i = 0; i < kKEach; ++i) {  // the thread's tokens are a multiple of 8 apart
+      constexpr int kApart = kBlockThreads / kKUnits * (D * 2);
+      static_assert(kBlockThreads / kKUnits % 8 == 0, "units keep their places");
       if constexpr (KIND == KVH_CACHE_16) {
-        *reinterpret_cast<u32x4*>(kb + k_place(token, unit)) = k[i];
+        *reinterpret_cast<u32x4*>(lds + kb + i * kApart) = k[i];
       } else {
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
           uint32_t w[4];
           widen4<KIND>(k[i][2 * p], w[0], w[1]);
           widen4<KIND>(k[i][2 * p + 1], w[2], w[3]);
-          *reinterpret_cast<u32x4*>(kb + k_place(token, 2 * unit + p)) = u32x4{w[0], w[1], w[2], w[3]};
+          *reinterpret_cast<u32x4*>(lds + (kb ^ p * 16) + i * kApart) = u32x4{w[0], w[1], w[2], w[3]};
         }
       }
     }
@@ -242,7 +245,7 @@ struct Tiles {
 #pragma unroll
         for (int c = 0; c < kVWords; ++c) v[e][c] = none >> e & 1 ? 0u : v[e][c];
     }
-    const int u = v_unit(), ch = v_chan();
+    const int u = v_unit();
     if constexpr (KIND != KVH_CACHE_I8) {
       // Where some row does not see all of the tile, its infinities and NaN stay out of the product: see Odd.
       bool any = false;
@@ -298,7 +301,10 @@ struct Tiles {
       }
     }
 #pragma unroll
-    for (int j = 0; j < kVChans; ++j) *reinterpret_cast<u32x4*>(vb + v_place(ch + j, u)) = u32x4{z[0][j], z[1][j], z[2][j], z[3][j]};
+    for (int j = 0; j < kVChans; ++j) {  // channel ch + j: j rows on, with j's bits in the unit's place (see v_place)
+      constexpr int kOne = kVChans == 4 ? 32 : 64, kTwo = 64;
+      *reinterpret_cast<u32x4*>(lds + (vb ^ (j % 2 * kOne | j / 2 * kTwo)) + j * (kManyTokens * 2)) = u32x4{z[0][j], z[1][j], z[2][j], z[3][j]};
+    }
     if constexpr (KIND != KVH_CACHE_16 && !PAGE16) {
       if (tid < kManyTokens) {
         const ValueScale z2(vs[0]);
@@ -397,10 +403,8 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     t.seek(steps.token(s0));
     t.fetch_tile(steps.token(s0), p_first);
   }
-  // Where the lane's operands lie in a buffer: those of a row differ in the unit's low bits, the rest is the same for all lanes.
-  int k_at[4], v_at[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) k_at[e] = T::k_place(col, 2 * e + half), v_at[e] = T::v_place(col, 2 * e + half);
+  // Where the lane's operands lie in a buffer: unit 2 e + half of its row, whose place differs from unit half's by an exclusive or with 32 e.
+  const uint32_t k_at = (uint32_t)T::k_place(col, half), v_at = T::kKTile + (uint32_t)T::v_place(col, half);
   int buffer = 0;
   for (int s = s0; s < s1; s += 2, buffer ^= 1) {
     const int t0 = steps.token(s);
@@ -429,14 +433,13 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     const bool hidden = t0 + kManyTokens > end || (a.causal && t0 + kManyTokens - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) || absent != 0;
     const bool blank = !works || (a.causal && t0 > p_most);  // no row of the wave sees any of it
     if (blank) continue;
-    const uint8_t* kb = lds + buffer * T::kBuffer;
-    const uint8_t* vb = kb + T::kKTile;
+    const uint32_t kb = k_at + buffer * T::kBuffer, vb = v_at + buffer * T::kBuffer;
     f32x16 x[2];  // element j of x[i] is token 32 i + 8 (j / 4) + 4 half + j % 4 of the tile, of its group 2 i + j / 8
     {
       u32x4 kf[2 * T::kSums];
 #pragma unroll
       for (int kk = 0; kk < 2 * T::kSums; ++kk)
-        kf[kk] = *reinterpret_cast<const u32x4*>(kb + k_at[kk % 4] + kk / T::kSums * (32 * D * 2) + kk % T::kSums / 4 * 128);
+        kf[kk] = *reinterpret_cast<const u32x4*>(lds + (kb ^ kk % 4 * 32) + kk / T::kSums * (32 * D * 2) + kk % T::kSums / 4 * 128);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -519,7 +522,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
         p[2 * i + j4 / 2][2 * (j4 % 2) + 1] = narrow2<T::kBf ? KVH_BF16 : KVH_F16>(w[2], w[3]);
       }
     };
-    auto operand = [&](int c, int g) { return *reinterpret_cast<const u32x4*>(vb + v_at[g] + c * (32 * kManyTokens * 2)); };
+    auto operand = [&](int c, int g) { return *reinterpret_cast<const u32x4*>(lds + (vb ^ g * 32) + c * (32 * kManyTokens * 2)); };
     weights(0);
     __builtin_amdgcn_sched_barrier(0);
     {
@@ -555,7 +558,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     if constexpr (KIND != KVH_CACHE_I8) {
       if ((odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3]) != 0) {
         using Bad = Odd<T::kBf>;
-#pragma unroll
+#pragma unroll 1
         for (int g = 0; g < 4; ++g) {
           u32x4 one;  // of the group's tokens that the lane's row sees
 #pragma unroll
