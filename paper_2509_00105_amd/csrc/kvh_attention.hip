@@ -10,7 +10,16 @@
 // two of their row's own), the K scale of its page multiplies the finished dot product, and the V scale sv of its page enters the
 // exponent: with s' = s + log2 sv and m' = max s', the weight exp2(s' - m') <= 1 multiplies the code and exp2(s' - m') / sv adds
 // to the sum.  A weight is thus as exact as fp16 is, however the scales of a request's pages differ.
+//
+// This kernel is the one for few rows (single tokens, short questions): each byte of the cache is read once and used by 16 rows at most, so it is bound
+// by memory, and where little is read by the chain table -> page -> scores -> values of a step.  Keys and values go from memory to the
+// registers that the matrix instructions take them from, without LDS: no other wave wants them.
+// Measured: 64 requests of 4096 tokens (lognormal), 8 KV heads of 128, 32 query heads: bf16 185 us = 5.2 TB/s (a plain read reaches 6.5), int8 109 us =
+// 4.5 TB/s (a head's rows are 128 bytes there; without any arithmetic it takes as long); one of 131072, e4m3: 67 us = 4.0 TB/s, 10 of them
+// joining; one of 300: 8.7 us.
 #include "kvh_attention.hpp"
+
+#include <algorithm>
 
 namespace kvh {
 namespace {
@@ -28,7 +37,9 @@ struct Worker {
   static constexpr int kKWords = D * kWidth / 16;      // words of K that a lane reads of a tile
   static constexpr int kVWords = kChans * kWidth / 4;  // words of V that a lane reads of a token
   static constexpr int kScales = kScaled ? (PAGE16 ? 2 : 8) : 1;
-  static constexpr bool kAhead = NR == 1 && !(KIND == KVH_CACHE_16 && D == 128);  // where two steps fit the registers
+  // Loads of the next step under way while this one is worked on: where lanes look pages up before they load and registers allow it (40 requests
+  // of 4000, e4m3, D 64, pages of 24: 61 us, 76 without; D 128: 84 and 83; pages of 16, 64 requests of 4096, int8, D 128: 113 and 109).
+  static constexpr bool kAhead = NR == 1 && kScaled && !PAGE16 && D == 64;
 
   // A step's tokens as they are in the cache.  Token slot 4 i + r of a lane is token 16 i + 4 grp + r of the step.
   struct Raw {
@@ -358,7 +369,7 @@ struct Worker {
     }
   }
 
-  // Steps [s0, s1).  kAhead: a step's loads are under way while the one before it is worked on.
+  // Steps [s0, s1).
   __device__ __forceinline__ void walk(const Steps& steps, int s0, int s1) {
     if (s0 >= s1) return;
     int t = steps.token(s0);
@@ -596,10 +607,26 @@ __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int l
 }
 
 // ---- launch -------------------------------------------------------------------------------------------------------
-constexpr int kFill = 512;            // blocks of 4 waves that fill the chip: their registers leave room for 2 on a compute unit
-constexpr int kLeastSteps = 16;       // of a chunk, few rows: shorter ones cost more in joining than they save
-constexpr int kLeastStepsMany = 4;    // and many rows
-constexpr int64_t kWideTokens = 2048; // from this capacity on a block's waves take heads and not tokens
+// Rules with both sides measured (us, 8 KV heads of 128, 32 query heads unless said; "after": new tokens after cached ones).
+// Blocks of 4 waves that fill the chip: their registers leave room for 2 on a compute unit.  Chunks for 512 / 256 / 1024 blocks: 512 after 32768,
+// int8: 391 / 590 / 419; one of 131072, e4m3: 67 / 62 / 67; 64 of 4096, int8: 113 / - / 119.
+constexpr int kFill = 512;
+// Steps of a chunk at least: 4, one for each wave (one request of 2100: 12; 16 steps: 15), but 16 where a wave takes all of a chunk by itself
+// (8 of 6000, bf16: 50; 4 steps: 53).
+constexpr int kLeastSteps = 4, kLeastWide = 16;
+// Steps that cutting has to take from the longest tile to be worth the partial results and the second launch.  Few rows: one of 700 cut 11, whole
+// 13; 16 of 500 cut 18, whole 12.  Many: 128 after 1000 cut 25, whole 45; a prompt of 1024 cut 53, whole 42; 8 of 300 after 500 cut 98, whole 70.
+constexpr int kGainFew = 16, kGainMany = 24;
+// Steps of all heads from which on a block's waves take neighbouring heads, whose rows of a token lie together, and not parts of one head's tokens, which
+// shorten what a step waits for: 64 of 4096, int8: 113, 126 by tokens; 4 of 10000, int8: 28 by tokens, 35 by heads; one of 8000: 16 and 32.
+constexpr int kWideSteps = 40 * kFill;
+
+// 17 to 32 rows: two tiles of 16 share what is read where both tiles' outputs fit the registers beside it, which is not so for 128 channels of 16
+// bits; the kernel for many rows takes those.  16 requests, 8 after 4000: int8 62, with the other kernel 68; bf16 95 and 82; bf16 with heads of 64: 46 and 52.
+// More rows are the other kernel's (9 after 8000: 25; with pairs of tiles 44).
+template <int KIND, int D>
+constexpr bool kTwoTiles = KIND != KVH_CACHE_16 || D == 64;
+bool two_tiles(int kind, int head_dim) { return kind != KVH_CACHE_16 || head_dim == 64; }
 
 struct Plan {
   int nr;          // tiles of 16 rows of the kernel for few rows; 0: the kernel for many
@@ -612,11 +639,11 @@ struct Plan {
   size_t joints() const { return (size_t)(tiles + 1) * sizeof(Joint); }  // bytes: what the joining kernel reads
 };
 
-Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
+Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim, bool two_tiles) {
   Plan p;
   const int64_t group = q_heads / heads;
   const int64_t most = (int64_t)(max_new < n_tokens ? max_new : n_tokens) * group;
-  p.nr = most <= 16 ? 1 : most <= 32 ? 2 : 0;
+  p.nr = most <= 16 ? 1 : most <= 32 && two_tiles ? 2 : 0;
   p.log_rows = p.nr != 0 ? few_log_rows(p.nr) : kLogManyRows;
   p.log_hw = 0;
   if (p.nr != 0)
@@ -629,7 +656,7 @@ Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, 
 
 template <int DT, int KIND, int D, int NR>
 void launch_pages(const AttnParams& a, dim3 grid, hipStream_t stream) {
-  if (a.block_tokens % 16 == 0)
+  if (a.block_tokens % 16 == 0)  // 64 requests of 4096, int8: 109 us, 122 by looking every token up; one of 300: 9 and 11
     launch_kernel(attention_kernel<DT, KIND, D, NR, true>, grid, dim3(kFewThreads), 0, stream, a);
   else
     launch_kernel(attention_kernel<DT, KIND, D, NR, false>, grid, dim3(kFewThreads), 0, stream, a);
@@ -637,10 +664,10 @@ void launch_pages(const AttnParams& a, dim3 grid, hipStream_t stream) {
 
 template <int DT, int KIND, int D>
 void launch_rows(const AttnParams& a, int nr, dim3 grid, hipStream_t stream) {
-  if (nr == 1)
-    launch_pages<DT, KIND, D, 1>(a, grid, stream);
-  else
-    launch_pages<DT, KIND, D, 2>(a, grid, stream);
+  if constexpr (kTwoTiles<KIND, D>) {
+    if (nr == 2) return launch_pages<DT, KIND, D, 2>(a, grid, stream);
+  }
+  launch_pages<DT, KIND, D, 1>(a, grid, stream);
 }
 
 template <int DT, int KIND>
@@ -689,8 +716,12 @@ extern "C" {
 size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim) {
   if (n_requests < 1 || n_requests > kMaxRequests || max_new < 1 || n_tokens < 1 || !heads_fit(heads, q_heads)) return 0;
   if (head_dim != 64 && head_dim != 128) return 0;
-  const Plan p = plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim);
-  return p.joints() + (size_t)p.slots() * p.slot;
+  size_t most = 0;
+  for (bool two : {false, true}) {
+    const Plan p = plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim, two);
+    most = std::max(most, p.joints() + (size_t)p.slots() * p.slot);
+  }
+  return most;
 }
 
 int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q,
@@ -730,14 +761,15 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   a.by_group = Divisor((uint32_t)a.group);
   a.by_heads = Divisor((uint32_t)a.heads);
   if ((int64_t)a.req.max_new * a.group >= (int64_t)1 << 31) return KVH_E_SHAPE;
-  Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim);
-  // Few rows of short requests: a block's waves share the tokens of one head, and a step's latency.
-  if (a.req.capacity < kWideTokens) p.target >>= p.log_hw, p.log_hw = 0;
-  // The batch is cut where its row tiles alone leave the chip idle, some request can be longer than the shortest part, and there is room
-  // for the parts.
-  const int least = p.nr == 0 ? kLeastStepsMany : kLeastSteps;
+  Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim, two_tiles(cache->kind, cache->head_dim));
+  // The steps of the longest tile, and what all tiles come to at most.  The lengths are the device's; the host knows what the table has room for.
+  int64_t longest = std::min<int64_t>((a.req.capacity + kStep - 1) / kStep, 1 << 26);
+  if (window != 0) longest = std::min(longest, ((int64_t)window + sink + (1 << p.log_rows)) / kStep + 5);
+  const int64_t most = std::min<int64_t>(p.tiles * a.heads, 2 * kFill) * longest;
+  if (most < kWideSteps) p.target >>= p.log_hw, p.log_hw = 0;
+  const int64_t even = a.req.n == 1 ? std::max<int64_t>(most / kFill, kLeastSteps) : kLeastSteps;
   const int64_t room = workspace_dev == nullptr || workspace_bytes < p.joints() ? 0 : (int64_t)((workspace_bytes - p.joints()) / p.slot);
-  const bool cut = p.tiles * a.heads < 2 * kFill && a.req.capacity > least * kStep && room > p.tiles;
+  const bool cut = p.tiles * a.heads < 2 * kFill && longest - even >= (p.nr == 0 ? kGainMany : kGainFew) && room > p.tiles;
   if (cut && room < p.slots()) p.target = room - p.tiles;
   a.log_hw = p.log_hw;
   a.by_heads = Divisor((uint32_t)(a.heads >> a.log_hw));
@@ -746,7 +778,7 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   blocks *= a.by_heads.d;
   if (blocks > 0x7fffffff) return KVH_E_SHAPE;
   a.target = (int)p.target;
-  a.least = least;
+  a.least = p.log_hw != 0 ? kLeastWide : kLeastSteps;
   if (cut) {
     a.slots = p.slots();
     a.tiles = p.tiles;
