@@ -5,13 +5,17 @@
 // its lanes share the row's cosines and sines.  An 8-bit page is described by one scale a head, so there the unit is a page
 // and a head: its new rows are read and rotated, their largest magnitude is found across the wave, and they are stored as codes.  The
 // other half of a rotated pair is 0 lanes away or rot / 16 lanes, and comes by a lane exchange, which also makes q_out == q safe.
+//
+// Memory bounds it (some 6 operations an element), or for a step of single tokens the launch.  Measured, 8 KV heads of 128, 32 query heads: a
+// prompt of 8192 into e4m3, rotated: 38.7 us = 4.9 TB/s, what a plain copy reaches; 16 prompts of 1500 in 16 bits (10 KV heads of 64): 48.6 us = 5.0
+// TB/s; 32 layers of 256 tokens into int8: 11.5 us = 4.4 TB/s; 64 single tokens into int8: 5.3 us, one: 4.7 us, a kernel of 3.6.
 #include "kvh_cache.hpp"
 
 namespace kvh {
 namespace {
 
 constexpr int kPageRows = 16;  // rows of an 8-bit page that are taken at once
-constexpr int kTileRows = 4;   // and of a unit of queries or of a 16-bit cache (8K prompt, e4m3: 41.4 us; 8 rows 44.0, 16 rows 51)
+constexpr int kTileRows = 4;   // and of a unit of queries or of a 16-bit cache (8K prompt, e4m3, one head a unit: 41.4 us; 8 rows 44.0, 16 rows 51)
 
 struct AppendParams {
   Requests req;
