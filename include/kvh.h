@@ -30,6 +30,9 @@
  *   pattern is kept, non-finite values included).  Encode, decode, the token-dropping calls and the loader take
  *   it like any other level (token dropping at this level is dropping alone, without quantisation).
  *
+ * Beside the codec stand the two operators of a serving program on the paged cache that entries are decoded into: kvh_append and
+ * kvh_attention ("Serving cache" below).
+ *
  * Conventions
  *   - Pointers named *_dev are DEVICE pointers owned by the caller; everything else is host
  *     memory.  A blob pointer may also be pinned host memory that the device can address (the
