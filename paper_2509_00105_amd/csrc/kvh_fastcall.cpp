@@ -394,6 +394,7 @@ kvh_rows rows_of(Reader& r, const Fields& f, Type type, int64_t layers, int64_t 
 // append(k, v, k_cache, v_cache, starts, lens, page_table, max_new, head_dim, k_scale, v_scale, q, q_out, rotation, positions, pairs, status, stream)
 PyObject* append(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
   KVH_ARGS(18);
+  if (self->append == nullptr) Py_RETURN_NONE;
   const Fields k = read_fields(r, a[0], 3), v = read_fields(r, a[1], 3), q = read_fields(r, a[11], 3, true), o = read_fields(r, a[12], 3, true),
                t = read_fields(r, a[13], 2, true);
   const int head_dim = r.narrow(a[8]);
@@ -441,6 +442,7 @@ PyObject* append(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
 // workspace, status, stream)
 PyObject* attention(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
   KVH_ARGS(20);
+  if (self->attention == nullptr) Py_RETURN_NONE;
   const Fields q = read_fields(r, a[0], 2), o = read_fields(r, a[15], 2), lse = read_fields(r, a[16], 2, true), ws = read_fields(r, a[17], 1);
   const int layer = r.narrow(a[3]), head_dim = r.narrow(a[8]), sink = r.narrow(a[13]), window = r.narrow(a[14]);
   if ((a[12] != Py_True && a[12] != Py_False) || (a[11] != Py_None && !PyFloat_CheckExact(a[11]))) r.ok = false;
@@ -486,11 +488,12 @@ PyObject* attention(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
 void find_exchange() {}
 #endif
 
-// Calls(current_device, raw_stream, addresses of the eight functions in the order of the struct)
+// Calls(current_device, raw_stream, addresses of the functions in the order of the struct; those of the serving cache may be left out, and its
+// calls then go the ctypes way)
 PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
   PyObject *dev, *raw;
-  unsigned long long p[8];
-  if (!PyArg_ParseTuple(args, "OOKKKKKKKK", &dev, &raw, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7])) return nullptr;
+  unsigned long long p[8] = {};
+  if (!PyArg_ParseTuple(args, "OOKKKKKK|KK", &dev, &raw, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7])) return nullptr;
   Calls* c = reinterpret_cast<Calls*>(type->tp_alloc(type, 0));
   if (c == nullptr) return nullptr;
   c->encode = reinterpret_cast<decltype(c->encode)>((uintptr_t)p[0]);
