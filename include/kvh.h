@@ -65,7 +65,7 @@ typedef enum {
   KVH_OK = 0,
   KVH_E_ARG = -1,   /* null pointer, bad dtype, negative offset, bad block_tokens, too many items */
   KVH_E_LEVEL = -2, /* level outside 0..3, or the raw level passed to a call that only takes quantised levels */
-  KVH_E_SHAPE = -3, /* l < 1, n < 1, c not a positive multiple of 128, chunk not a multiple of 128 */
+  KVH_E_SHAPE = -3, /* l < 1, n < 1, c not a positive multiple of 128, chunk not a multiple of 128; see also the calls of the serving cache */
   KVH_E_SIZE = -4,  /* blob capacity too small */
   KVH_E_ALIGN = -5, /* a base pointer or stride breaks the 16-byte rule */
   KVH_E_HIP = -6    /* the kernel launch itself failed */

@@ -516,7 +516,7 @@ const char* kvh_strerror(int status) {
     case KVH_OK: return "ok";
     case KVH_E_ARG: return "bad argument (null pointer, dtype, offset, block size or item count)";
     case KVH_E_LEVEL: return "level outside 0..3 (or the raw level where only quantised levels are allowed)";
-    case KVH_E_SHAPE: return "bad shape (l, n >= 1; c and chunk multiples of 128)";
+    case KVH_E_SHAPE: return "bad shape (l, n >= 1; c and chunk multiples of 128; serving cache: head_dim 64 or 128, layer, heads, pages and rot in range)";
     case KVH_E_SIZE: return "blob capacity too small";
     case KVH_E_ALIGN: return "pointer or stride breaks the 16-byte alignment rule";
     case KVH_E_HIP: return "kernel launch failed";
