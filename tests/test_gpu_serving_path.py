@@ -100,3 +100,22 @@ def test_launch_events(kvh):
     b.run(kvh)
     torch.cuda.synchronize()
     assert 0 < start.elapsed_time(stop) < 100
+
+
+@pytest.mark.parametrize("heads,kind,dt,dim,bt", [(2, "i8", "bf16", 128, 16), (4, "16", "fp16", 64, 16), (8, "e4m3", "bf16", 64, 24), (12, "i8", "fp16", 64, 16)])
+@pytest.mark.parametrize("mask", [dict(), dict(sink=40, window=7900)])
+def test_blocks_of_neighbouring_heads(kvh, heads, kind, dt, dim, bt, mask):
+    """So many steps that a block's waves take heads of their own: one long request among short ones."""
+    n = 80 // heads + 1
+    b = Batch([1] * n, [8300] + [1 + 37 * i % 400 for i in range(1, n)], heads=heads, group=2, dim=dim, bt=bt, kind=kind, dt=dt, seed=61, layers=1)
+    b.check(b.run(kvh, **mask), **mask)
+    assert not b.status.any()
+
+
+@pytest.mark.parametrize("kind", ["16", "i8", "e4m3"])
+@pytest.mark.parametrize("new,length,mask", [(1, 640, {}), (1, 4001, {}), (8, 3000, {}), (16, 3000, {}), (100, 2500, dict(sink=70, window=1200)), (300, 1500, {})])
+def test_one_request_cut(kvh, kind, new, length, mask):
+    """A request alone, in a few rows, in pairs of row tiles and in many."""
+    b = Batch([new], [length], heads=2, group=2, dim=128, kind=kind, dt="bf16", seed=67, layers=1)
+    b.check(b.run(kvh, **mask), **mask)
+    assert not b.status.any()
