@@ -338,7 +338,8 @@ int kvh_load_static(const kvh_load_item* items, int n_items, kvh_dtype dt, int l
  * appended to it, and queries attend over it.  The cache is the paged view of kvh_decode, [layers][pages][block_tokens][c]
  * with c = heads * head_dim channels, and holds either the 16-bit type of the call (KVH_CACHE_16: the very tensors kvh_decode
  * writes) or 8-bit codes with one fp32 scale per page and KV head, for K and V apart: the value of a code is code * scale,
- * the code an int8 (KVH_CACHE_I8, -127 .. 127) or an OCP e4m3 float (KVH_CACHE_E4M3, up to 448).
+ * the code an int8 (KVH_CACHE_I8, -127 .. 127) or an OCP e4m3 float (KVH_CACHE_E4M3, up to 448).  Scales are not negative; a page and head
+ * whose scale is no finite number (what non-finite inputs may leave) holds NaN.
  *
  * A batch holds n_requests requests; the new tokens of request b are the rows starts[b] .. starts[b + 1] - 1 of the packed
  * tensors, lens[b] counts its tokens in the cache WITH the new ones, and its new token i therefore has the logical position

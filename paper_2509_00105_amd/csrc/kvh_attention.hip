@@ -209,15 +209,21 @@ struct Worker {
     const bool hidden_any = t0 + kStep > end || (a.causal && t0 + kStep - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) ||
                             (PAGE16 ? x.absent != 0 : __any(x.absent != 0));
     float lsv[kScales], inv[kScales], rest[kScales];
-    bool faint = false;
+    bool rare = false;  // some scale leaves a rest
     if constexpr (kScaled) {
+      uint32_t rank = 0;
 #pragma unroll
-      for (int i = 0; i < kScales; ++i) {
-        const ValueScale z(x.vs[i]);
-        lsv[i] = z.log, inv[i] = z.inv, rest[i] = z.rest;
-        faint |= z.rest != 1.0f;
+      for (int i = 0; i < kScales; ++i) rank = rank > scale_rank(x.vs[i]) ? rank : scale_rank(x.vs[i]);
+      rare = __any(rank >= kRareRank);
+      if (rare) {
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) {
+          const ValueScale z(x.vs[i]);
+          x.vs[i] = z.used, rest[i] = z.rest;
+        }
       }
-      faint = __any(faint);
+#pragma unroll
+      for (int i = 0; i < kScales; ++i) lsv[i] = __builtin_amdgcn_logf(x.vs[i]), inv[i] = __builtin_amdgcn_rcpf(x.vs[i]);
     }
     auto of = [](int i) { return PAGE16 ? i / 4 : i; };  // token slot -> its scale
 
@@ -287,9 +293,12 @@ struct Worker {
           l[t] = __builtin_fmaf(y[i], inv[of(i)], l[t]);
       }
       if constexpr (kScaled) {
-        if (faint) {
+        if (rare) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] *= rest[of(i)];
+          for (int i = 0; i < 8; ++i) {
+            const bool none = hidden_any && (!sight[t].sees(a, t0 + 16 * (i / 4) + grp * 4 + i % 4) || (x.absent >> i & 1u) != 0);
+            y[i] = none ? 0.0f : y[i] * rest[of(i)];  // the rest may be NaN
+          }
         }
       }
 #pragma unroll

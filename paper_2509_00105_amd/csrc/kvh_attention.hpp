@@ -344,6 +344,16 @@ struct Sight {
   // `end` is past the last token that any row of the item sees.
   __device__ __forceinline__ Sight(const AttnParams& a, int end, int p) : last(a.causal && p < end ? p : end - 1), low(a.window != 0 ? p - a.window : -1) {}
   __device__ __forceinline__ bool sees(const AttnParams& a, int token) const { return token <= last && (token > low || token < a.sink); }
+  // Of tokens [t0, t0 + 64), those it sees.
+  __device__ __forceinline__ uint64_t seen(const AttnParams& a, int t0) const {
+    int last = this->last, low = this->low;
+    asm volatile("" : "+v"(last), "+v"(low));  // rarely asked: nothing of it is worked out ahead of a loop
+    auto below = [&](int token) {  // those before it
+      const int n = token - t0;
+      return n <= 0 ? (uint64_t)0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
+    };
+    return below(last + 1) & (~below(low < 0 ? 0 : low + 1) | below(a.sink));
+  }
 };
 
 // An item's steps: those of the first `sink` tokens, then those from its first row's window on.
@@ -405,17 +415,21 @@ struct Odd {
   }
 };
 
-// A V scale as the softmax takes it: its logarithm goes into the exponent, its inverse into the sum; a scale of zero (or next to it) keeps
-// its tokens in the sum and takes their values off the weight.
+// A V scale as the softmax takes it: its logarithm goes into the exponent, its inverse into the sum.  Two sorts of scales are not taken as they are.  One of
+// zero (or next to it) keeps its tokens in the sum and takes their values off the weight: kLeastScale, with the rest of it as a factor.  The
+// page of one that is no finite number holds NaN: rows that see the page become that, and the scale is taken as 1, since neither a weight of zero nor a
+// hidden score would keep NaN and infinities from the other rows.
+__device__ __forceinline__ bool odd_scale(float z) { return !(__builtin_fabsf(z) < INFINITY); }
 struct ValueScale {
-  float log, inv, rest;
+  float used, rest;
   __device__ __forceinline__ explicit ValueScale(float z) {
-    const float used = z < kLeastScale ? kLeastScale : z;
-    rest = z < kLeastScale ? z * (1.0f / kLeastScale) : 1.0f;
-    log = __builtin_amdgcn_logf(used);
-    inv = __builtin_amdgcn_rcpf(used);
+    used = odd_scale(z) ? 1.0f : z < kLeastScale ? kLeastScale : z;
+    rest = odd_scale(z) ? NAN : z < kLeastScale ? z * (1.0f / kLeastScale) : 1.0f;
   }
 };
+// Of several scales the largest of these numbers says whether one is of either sort.
+__device__ __forceinline__ uint32_t scale_rank(float z) { return __builtin_bit_cast(uint32_t, z) - __builtin_bit_cast(uint32_t, kLeastScale); }
+constexpr uint32_t kRareRank = __builtin_bit_cast(uint32_t, INFINITY) - __builtin_bit_cast(uint32_t, kLeastScale);
 
 // bf16 values of a row -> fp16 with the power of two that brings its largest to [1, 2): the factor, and what undoes it.
 __device__ __forceinline__ f32x2 row_power(float most) {

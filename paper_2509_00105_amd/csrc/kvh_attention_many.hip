@@ -52,7 +52,7 @@ struct Tiles {
   const AttnParams& a;
   uint8_t* lds;                     // two buffers
   uint32_t (*odd)[kWavesPerBlock];  // of each buffer, by the wave that stored them: an infinity or NaN among its values
-  float (*scales)[3][kScales];      // of each buffer, where a tile's tokens lie on pages of any size: K scales, ValueScale's log and inv
+  float (*scales)[3][kScales];      // of each buffer, where a tile's tokens lie on pages of any size: K scales, and V scales' logarithms and inverses
   const int32_t* table;
   int head, end, lane, wave;
   PageRun run;
@@ -68,6 +68,7 @@ struct Tiles {
   uint32_t v[8][kVWords];
   uint32_t none;         // of its 8 tokens of V, those past the end or on no page of the cache
   uint64_t absent;       // the tile's tokens on no page of the cache
+  uint64_t odd_v;        // its others whose V scale is no finite number; known when the tile has been stored, and the scales are ones to be used then
   bool edge;             // some row of the block does not see all of the tile
   float ks[4], vs[4];    // scales of the tile's groups of 16 tokens (PAGE16), or of its token `lane` in [0]
 
@@ -290,11 +291,12 @@ struct Tiles {
       }
     }
     if constexpr (KIND != KVH_CACHE_16) {
-      // Scales below the least that the exponent takes: the rest goes onto the values.
-      bool faint = false;
+      uint32_t rank = 0;
 #pragma unroll
-      for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) faint |= vs[g] < kLeastScale;
-      if (__any(faint)) {
+      for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) rank = rank > scale_rank(vs[g]) ? rank : scale_rank(vs[g]);
+      odd_v = 0;
+      if (__any(rank >= kRareRank)) {
+        // Below the least that the exponent takes the rest goes onto the values.
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float r[2];
@@ -302,12 +304,21 @@ struct Tiles {
           for (int n = 0; n < 2; ++n) {
             const float s = PAGE16 ? (wave == 0 ? vs[0] : wave == 1 ? vs[1] : wave == 2 ? vs[2] : vs[3])
                                    : __int_as_float(__builtin_amdgcn_ds_bpermute(v_token(u, 0) * 4 + 4 * v_token(0, 2 * e + n), __float_as_int(vs[0])));
-            r[n] = ValueScale(s).rest;
+            r[n] = odd_scale(s) ? 1.0f : ValueScale(s).rest;
           }
           const f16x2 by = __builtin_bit_cast(f16x2, narrow2<KVH_F16>(r[0], r[1]));
 #pragma unroll
           for (int j = 0; j < kVChans; ++j) z[e][j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, z[e][j]) * by);
         }
+#pragma unroll
+        for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) {
+          if constexpr (PAGE16)
+            odd_v |= odd_scale(vs[g]) ? (uint64_t)0xffff << 16 * g : 0;
+          else
+            odd_v = __ballot(odd_scale(vs[g]));
+          vs[g] = ValueScale(vs[g]).used;
+        }
+        odd_v &= ~absent;
       }
     }
 #pragma unroll
@@ -317,10 +328,9 @@ struct Tiles {
     }
     if constexpr (KIND != KVH_CACHE_16 && !PAGE16) {
       if (tid < kManyTokens) {
-        const ValueScale z2(vs[0]);
         scales[buffer][0][tid] = ks[0];
-        scales[buffer][1][tid] = z2.log;
-        scales[buffer][2][tid] = z2.inv;
+        scales[buffer][1][tid] = __builtin_amdgcn_logf(vs[0]);
+        scales[buffer][2][tid] = __builtin_amdgcn_rcpf(vs[0]);
       }
     }
   }
@@ -402,7 +412,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
   float m = -INFINITY, l = 0.0f;
-  bool bad = false;
+  bool bad = false, spoiled = false;  // the lane's row sees: a token on no page of the cache; one whose V scale is no finite number
 
   T t(a);
   t.lds = lds, t.odd = odd, t.scales = scales, t.lane = lane, t.head = head, t.end = end;
@@ -419,7 +429,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   for (int s = s0; s < s1; s += 2, buffer ^= 1) {
     const int t0 = steps.token(s);
     t.store_tile(buffer);
-    const uint64_t absent = t.absent;
+    const uint64_t absent = t.absent, odd_v = kScaled ? t.odd_v : 0;
     // An element's exponent of 2 is f x + z, by groups of 16 tokens (one group where there are no scales).
     constexpr int kGroups = kScaled && PAGE16 ? 4 : 1;
     float f[kGroups], z[kGroups], inv[kGroups];
@@ -427,9 +437,8 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     for (int g = 0; g < kGroups; ++g) {
       f[g] = coef, z[g] = 0.0f, inv[g] = 1.0f;
       if constexpr (kScaled && PAGE16) {
-        const ValueScale v(t.vs[g]);
         f[g] = fmaxf(t.ks[g] * coef, 0x1p-126f);  // never 0: a hidden score is minus infinity, and has to stay it
-        z[g] = v.log, inv[g] = v.inv;
+        z[g] = __builtin_amdgcn_logf(t.vs[g]), inv[g] = __builtin_amdgcn_rcpf(t.vs[g]);
       } else if constexpr (kScaled) {
         f[g] = 1.0f;  // its tokens' own scales are applied to the scores at once
       }
@@ -487,6 +496,9 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
           bad |= seen && none;
           x[i][j] = !seen || none ? -INFINITY : x[i][j];
         }
+    }
+    if constexpr (kScaled) {
+      if (odd_v != 0) spoiled |= (sight.seen(a, t0) & odd_v) != 0;
     }
     float most = -INFINITY;
 #pragma unroll
@@ -599,6 +611,12 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
   const float sum = over_halves_sum(l);
+  if (kScaled && __any(spoiled)) {
+#pragma unroll
+    for (int c = 0; c < T::kOuts; ++c)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[c][j] = spoiled ? NAN : o[c][j];
+  }
   if (it.split) {
     if (real) {
       const int64_t row = (it.slot * a.heads + head) * kManyRows + wave * kManyWaveRows + col;

@@ -1,0 +1,107 @@
+"""The serving cache's calls at the ends of what they take.  Tolerances are those of test_gpu_serving_attention.py."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_serving_attention import Batch  # noqa: E402
+
+BAD = 2  # KVH_DEV_BAD_REQUEST
+
+
+@pytest.fixture(scope="module")
+def kvh():
+    import paper_2509_00105_amd as m
+
+    m.lib()
+    return m
+
+
+# ---- scales that are no finite numbers: their pages hold NaN -------------------------------------------------------
+# new tokens, whole pages before the last token's, for few rows of a KV head, pairs of row tiles, and many rows
+ROWS = [([2], 4), ([10], 5), ([40], 9), ([150], 21)]
+ODD = [math.nan, math.inf]
+
+
+def scaled(rows, kind, bt, dim=64, dt="bf16", seed=71):
+    news, pages = ROWS[rows]
+    return Batch(news, [pages * bt + 1], heads=2, group=2, dim=dim, bt=bt, kind=kind, dt=dt, seed=seed, layers=1)  # the last token has a page of its own
+
+
+def spoil(b, which, page, value):
+    """Of one head of the first request."""
+    (b.ks, b.vs)[which][0, int(b.table_h[0, page]), 0] = value
+
+
+def check(b, out, **mask):
+    for s in (b.ks, b.vs):
+        s.masked_fill_(s.isinf(), math.nan)
+    b.check(out, **mask)
+
+
+def some_rows_see(kvh, kind, bt, rows, value, which):
+    """The last token's page, or one in the middle of the new tokens: the rows before are as exact as ever, the others NaN (from a V scale the outputs, and
+    not the logarithm of the sum)."""
+    for dim in (64, 128):
+        for back in (0, 1):
+            b = scaled(rows, kind, bt, dim)
+            spoil(b, which, ROWS[rows][1] - back, value)
+            check(b, b.run(kvh))
+            assert not b.status.any()
+
+
+def no_row_sees(kvh, kind, bt, rows, value, which):
+    """Pages between sink and window share steps with pages that are seen."""
+    for mask in (dict(window=9), dict(window=9, sink=3)):
+        b = scaled(rows, kind, bt)
+        for page in range(1 if "sink" in mask else 0, (b.lens_h[0] - b.news[0] - 9) // bt):
+            spoil(b, which, page, value)
+        check(b, b.run(kvh, **mask), **mask)
+
+
+def another_owns(kvh, kind, bt, rows, value, which):
+    """Tokens on no page of the cache: what page 0, which is none of the request's, holds does not matter."""
+    seed = next(s for s in range(100, 200) if 0 not in scaled(rows, kind, bt, seed=s).table_h[0, :ROWS[rows][1] + 1].tolist())
+    outs = []
+    for scale in (1.0, value):
+        b = scaled(rows, kind, bt, seed=seed)
+        b.table[0, 1] = -1
+        (b.ks, b.vs)[which][0, 0] = scale
+        outs.append((b.run(kvh), b.lse))
+        assert b.status.tolist() == [BAD] and outs[-1][0].isfinite().all()
+        assert torch.equal(outs[-1][0], outs[0][0]) and torch.equal(outs[-1][1], outs[0][1])
+
+
+def scales_of_zero_beside(kvh, kind, bt, rows, value, which):
+    """Zero, next to zero and no number in neighbouring pages."""
+    b = scaled(rows, kind, bt)
+    last = ROWS[rows][1]
+    spoil(b, which, last - 2, 0.0)
+    spoil(b, which, last - 1, 2.0 ** -70)
+    spoil(b, which, last, value)
+    check(b, b.run(kvh))
+
+
+WAYS = [some_rows_see, no_row_sees, another_owns, scales_of_zero_beside]
+
+
+@pytest.mark.parametrize("value", ODD)
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("bt", [16, 24])
+@pytest.mark.parametrize("rows", range(len(ROWS)))
+@pytest.mark.parametrize("way", WAYS)
+def test_v_scale(kvh, way, rows, bt, kind, value):
+    way(kvh, kind, bt, rows, value, 1)
+
+
+@pytest.mark.parametrize("value", ODD)
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("news", [[1], [90]])
+def test_v_scale_where_the_batch_is_cut(kvh, kind, news, value):
+    b = Batch(news, [4001], heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=73, layers=1)
+    spoil(b, 1, 2000 // 16, value)
+    check(b, b.run(kvh, window=200), window=200)
+    spoil(b, 1, 4000 // 16, value)
+    check(b, b.run(kvh))
