@@ -211,15 +211,16 @@ struct Worker {
     float lsv[kScales], inv[kScales], rest[kScales];
     bool rare = false;  // some scale leaves a rest
     if constexpr (kScaled) {
-      uint32_t rank = 0;
+      ScaleRange range;
 #pragma unroll
-      for (int i = 0; i < kScales; ++i) rank = rank > scale_rank(x.vs[i]) ? rank : scale_rank(x.vs[i]);
-      rare = __any(rank >= kRareRank);
-      if (rare) {
+      for (int i = 0; i < kScales; ++i) range.add(x.ks[i], x.vs[i]);
+      rare = __any(range.rare());
+      if (__builtin_expect(rare, 0)) {
 #pragma unroll
         for (int i = 0; i < kScales; ++i) {
           const ValueScale z(x.vs[i]);
           x.vs[i] = z.used, rest[i] = z.rest;
+          if (odd_scale(x.ks[i])) x.ks[i] = NAN;  // and so are the scores, until those are hidden that a row does not see
         }
       }
 #pragma unroll
@@ -293,7 +294,7 @@ struct Worker {
           l[t] = __builtin_fmaf(y[i], inv[of(i)], l[t]);
       }
       if constexpr (kScaled) {
-        if (rare) {
+        if (__builtin_expect(rare, 0)) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const bool none = hidden_any && (!sight[t].sees(a, t0 + 16 * (i / 4) + grp * 4 + i % 4) || (x.absent >> i & 1u) != 0);

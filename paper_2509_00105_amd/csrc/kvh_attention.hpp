@@ -427,9 +427,19 @@ struct ValueScale {
     rest = odd_scale(z) ? NAN : z < kLeastScale ? z * (1.0f / kLeastScale) : 1.0f;
   }
 };
-// Of several scales the largest of these numbers says whether one is of either sort.
-__device__ __forceinline__ uint32_t scale_rank(float z) { return __builtin_bit_cast(uint32_t, z) - __builtin_bit_cast(uint32_t, kLeastScale); }
-constexpr uint32_t kRareRank = __builtin_bit_cast(uint32_t, INFINITY) - __builtin_bit_cast(uint32_t, kLeastScale);
+// Whether one of several scales is of either sort: the words of numbers that are not negative are in their order, infinity and NaN above them.
+struct ScaleRange {
+  uint32_t top = 0, low = ~0u;
+  __device__ __forceinline__ void add(float k, float v) {
+    const uint32_t kw = __builtin_bit_cast(uint32_t, k), vw = __builtin_bit_cast(uint32_t, v);
+    top = top > kw ? top : kw;
+    top = top > vw ? top : vw;
+    low = low < vw ? low : vw;
+  }
+  __device__ __forceinline__ bool rare() const {
+    return top >= __builtin_bit_cast(uint32_t, INFINITY) || low < __builtin_bit_cast(uint32_t, kLeastScale);
+  }
+};
 
 // bf16 values of a row -> fp16 with the power of two that brings its largest to [1, 2): the factor, and what undoes it.
 __device__ __forceinline__ f32x2 row_power(float most) {

@@ -68,7 +68,7 @@ struct Tiles {
   uint32_t v[8][kVWords];
   uint32_t none;         // of its 8 tokens of V, those past the end or on no page of the cache
   uint64_t absent;       // the tile's tokens on no page of the cache
-  uint64_t odd_v;        // its others whose V scale is no finite number; known when the tile has been stored, and the scales are ones to be used then
+  uint64_t odd_k, odd_v; // its others whose K or V scale is no finite number; known when the tile has been stored, and the scales are ones to be used then
   bool edge;             // some row of the block does not see all of the tile
   float ks[4], vs[4];    // scales of the tile's groups of 16 tokens (PAGE16), or of its token `lane` in [0]
 
@@ -291,11 +291,11 @@ struct Tiles {
       }
     }
     if constexpr (KIND != KVH_CACHE_16) {
-      uint32_t rank = 0;
+      ScaleRange range;
 #pragma unroll
-      for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) rank = rank > scale_rank(vs[g]) ? rank : scale_rank(vs[g]);
-      odd_v = 0;
-      if (__any(rank >= kRareRank)) {
+      for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) range.add(ks[g], vs[g]);
+      odd_k = odd_v = 0;
+      if (__builtin_expect(__any(range.rare()), 0)) {
         // Below the least that the exponent takes the rest goes onto the values.
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -312,13 +312,16 @@ struct Tiles {
         }
 #pragma unroll
         for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) {
-          if constexpr (PAGE16)
+          if constexpr (PAGE16) {
+            odd_k |= odd_scale(ks[g]) ? (uint64_t)0xffff << 16 * g : 0;
             odd_v |= odd_scale(vs[g]) ? (uint64_t)0xffff << 16 * g : 0;
-          else
-            odd_v = __ballot(odd_scale(vs[g]));
+          } else {
+            odd_k = __ballot(odd_scale(ks[g])), odd_v = __ballot(odd_scale(vs[g]));
+          }
+          ks[g] = odd_scale(ks[g]) ? 1.0f : ks[g];
           vs[g] = ValueScale(vs[g]).used;
         }
-        odd_v &= ~absent;
+        odd_k &= ~absent, odd_v &= ~absent;
       }
     }
 #pragma unroll
@@ -412,7 +415,8 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[c][j] = 0.0f;
   float m = -INFINITY, l = 0.0f;
-  bool bad = false, spoiled = false;  // the lane's row sees: a token on no page of the cache; one whose V scale is no finite number
+  // The lane's row sees: a token on no page of the cache; one whose V scale is no finite number; one whose K scale is none.
+  bool bad = false, spoiled = false, lost = false;
 
   T t(a);
   t.lds = lds, t.odd = odd, t.scales = scales, t.lane = lane, t.head = head, t.end = end;
@@ -429,7 +433,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   for (int s = s0; s < s1; s += 2, buffer ^= 1) {
     const int t0 = steps.token(s);
     t.store_tile(buffer);
-    const uint64_t absent = t.absent, odd_v = kScaled ? t.odd_v : 0;
+    const uint64_t absent = t.absent, odd_k = kScaled ? t.odd_k : 0, odd_v = kScaled ? t.odd_v : 0;
     // An element's exponent of 2 is f x + z, by groups of 16 tokens (one group where there are no scales).
     constexpr int kGroups = kScaled && PAGE16 ? 4 : 1;
     float f[kGroups], z[kGroups], inv[kGroups];
@@ -437,7 +441,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     for (int g = 0; g < kGroups; ++g) {
       f[g] = coef, z[g] = 0.0f, inv[g] = 1.0f;
       if constexpr (kScaled && PAGE16) {
-        f[g] = fmaxf(t.ks[g] * coef, 0x1p-126f);  // never 0: a hidden score is minus infinity, and has to stay it
+        f[g] = fmaxf(t.ks[g] * coef, 0x1p-126f);  // never 0 or NaN: a hidden score is minus infinity, and has to stay it
         z[g] = __builtin_amdgcn_logf(t.vs[g]), inv[g] = __builtin_amdgcn_rcpf(t.vs[g]);
       } else if constexpr (kScaled) {
         f[g] = 1.0f;  // its tokens' own scales are applied to the scores at once
@@ -452,6 +456,13 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     const bool hidden = t0 + kManyTokens > end || (a.causal && t0 + kManyTokens - 1 > p_least) || (a.window != 0 && t0 <= p_most - a.window) || absent != 0;
     const bool blank = !works || (a.causal && t0 > p_most);  // no row of the wave sees any of it
     if (blank) continue;
+    if constexpr (kScaled) {
+      if (__builtin_expect((odd_k | odd_v) != 0, 0)) {
+        const uint64_t seen = sight.seen(a, t0);
+        spoiled |= (seen & odd_v) != 0;
+        lost |= (seen & odd_k) != 0;
+      }
+    }
     const uint32_t kb = k_at + buffer * T::kBuffer, vb = v_at + buffer * T::kBuffer;
     f32x16 x[2];  // element j of x[i] is token 32 i + 8 (j / 4) + 4 half + j % 4 of the tile, of its group 2 i + j / 8
     {
@@ -496,9 +507,6 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
           bad |= seen && none;
           x[i][j] = !seen || none ? -INFINITY : x[i][j];
         }
-    }
-    if constexpr (kScaled) {
-      if (odd_v != 0) spoiled |= (sight.seen(a, t0) & odd_v) != 0;
     }
     float most = -INFINITY;
 #pragma unroll
@@ -610,7 +618,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   }
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[it.b] = KVH_DEV_BAD_REQUEST;
 
-  const float sum = over_halves_sum(l);
+  const float sum = kScaled && lost ? NAN : over_halves_sum(l);
   if (kScaled && __any(spoiled)) {
 #pragma unroll
     for (int c = 0; c < T::kOuts; ++c)

@@ -105,3 +105,23 @@ def test_v_scale_where_the_batch_is_cut(kvh, kind, news, value):
     check(b, b.run(kvh, window=200), window=200)
     spoil(b, 1, 4000 // 16, value)
     check(b, b.run(kvh))
+
+
+@pytest.mark.parametrize("value", ODD)
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("bt", [16, 24])
+@pytest.mark.parametrize("rows", range(len(ROWS)))
+@pytest.mark.parametrize("way", WAYS)
+def test_k_scale(kvh, way, rows, bt, kind, value):
+    way(kvh, kind, bt, rows, value, 0)
+
+
+@pytest.mark.parametrize("value", ODD)
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("news", [[1], [90]])
+def test_k_scale_where_the_batch_is_cut(kvh, kind, news, value):
+    b = Batch(news, [4001], heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=75, layers=1)
+    spoil(b, 0, 2000 // 16, value)
+    check(b, b.run(kvh, window=200), window=200)
+    spoil(b, 0, 4000 // 16, value)
+    check(b, b.run(kvh))
