@@ -422,9 +422,10 @@ int kvh_append(const kvh_cache* cache, const kvh_requests* requests, kvh_dtype d
  * meet the values.  What a query does not see does not reach its result, whatever it is; infinities and NaN in what it sees do
  * as in the formula.
  * workspace_dev: device memory for partial results where few queries meet many tokens and the tokens of a request are split over
- * the GPU; 16-byte aligned.  kvh_attention_workspace says how much serves a batch best; with less (or none) the call splits
- * less (or not at all) and is slower.  It needs no preparation, is used by this call alone until it has finished, and keeps
- * nothing that another call reads. */
+ * the GPU; 16-byte aligned.  kvh_attention_workspace says how much serves a batch best: 0 where a batch has so many queries that it is never
+ * split (or where the arguments are none of an attention), and 256 MiB at most; memory for batches of several kinds is as large as the largest of theirs.  With
+ * less (or none) the call splits less (or not at all) and is slower.  It needs no preparation, is used by this call alone until it has
+ * finished, and keeps nothing that another call reads. */
 size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int heads, int q_heads, int head_dim);
 int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q,
                   const kvh_rows* out, int q_heads, float* lse_dev, float scale, int causal, int sink, int window,

@@ -692,7 +692,7 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
 
 
 def attention_workspace(n_requests: int, max_new: int, n_tokens: int, heads: int, q_heads: int, head_dim: int = 128) -> int:
-    """kvh_attention_workspace: bytes that serve such a batch best; 0 where the arguments are none of an attention."""
+    """kvh_attention_workspace: bytes that serve such a batch best; 0 where it is never split, or the arguments are none of an attention."""
     return lib().kvh_attention_workspace(n_requests, max_new, n_tokens, heads, q_heads, head_dim)
 
 

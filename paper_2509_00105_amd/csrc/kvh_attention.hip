@@ -646,6 +646,8 @@ struct Plan {
   int64_t tiles;   // row tiles of the batch at most
   int64_t target;  // chunks, where the batch is cut
   size_t slot;     // bytes of a partial result, of all heads
+  // Whether a batch of this size is cut at all: its tiles alone may give every block two of them to do.
+  bool may_cut(int heads) const { return tiles * heads < 2 * kFill; }
   int64_t slots() const { return target + tiles; }
   size_t joints() const { return (size_t)(tiles + 1) * sizeof(Joint); }  // bytes: what the joining kernel reads
 };
@@ -730,7 +732,7 @@ size_t kvh_attention_workspace(int n_requests, int max_new, int n_tokens, int he
   size_t most = 0;
   for (bool two : {false, true}) {
     const Plan p = plan_of(n_requests, max_new, n_tokens, heads, q_heads, head_dim, two);
-    most = std::max(most, p.joints() + (size_t)p.slots() * p.slot);
+    if (p.may_cut(heads)) most = std::max(most, p.joints() + (size_t)p.slots() * p.slot);
   }
   return most;
 }
@@ -789,7 +791,7 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
     gain = whole - std::max<int64_t>(most / kFill * 5 / 4, kLeastSteps);
   }
   const int64_t room = workspace_dev == nullptr || workspace_bytes < p.joints() ? 0 : (int64_t)((workspace_bytes - p.joints()) / p.slot);
-  const bool cut = p.tiles * a.heads < 2 * kFill && gain >= (p.nr == 0 ? kGainMany : kGainFew) && room > p.tiles;
+  const bool cut = p.may_cut(a.heads) && gain >= (p.nr == 0 ? kGainMany : kGainFew) && room > p.tiles;
   if (cut && room < p.slots()) p.target = room - p.tiles;
   a.log_hw = p.log_hw;
   a.by_heads = Divisor((uint32_t)(a.heads >> a.log_hw));

@@ -125,3 +125,19 @@ def test_k_scale_where_the_batch_is_cut(kvh, kind, news, value):
     check(b, b.run(kvh, window=200), window=200)
     spoil(b, 0, 4000 // 16, value)
     check(b, b.run(kvh))
+
+
+# ---- workspace ------------------------------------------------------------------------------------------------------
+def test_a_long_prompt_takes_no_memory_for_parts(kvh):
+    b = Batch([8192], [8192], heads=2, group=4, dim=64, kind="i8", dt="bf16", seed=77, layers=1)
+    q = b.q.repeat(1, 4)  # 8 heads of 64 channels, 32 query heads
+    kc, vc = b.kc.repeat(1, 1, 1, 4), b.vc.repeat(1, 1, 1, 4)
+    ks, vs = b.ks.repeat(1, 1, 4), b.vs.repeat(1, 1, 4)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    out = kvh.attention(q, kc, vc, 0, b.starts, b.lens, b.table, 8192, head_dim=64, k_scale=ks, v_scale=vs)
+    assert torch.cuda.max_memory_allocated() - before <= out.numel() * 2 + (1 << 20)
+    want = kvh.attention(b.q, b.kc, b.vc, 0, b.starts, b.lens, b.table, 8192, head_dim=64, k_scale=b.ks, v_scale=b.vs,
+                         workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))  # whole tiles too
+    assert torch.equal(out[:, :512], want) and torch.equal(out[:, -512:], want)
