@@ -345,8 +345,8 @@ int kvh_load_static(const kvh_load_item* items, int n_items, kvh_dtype dt, int l
  * tensors, lens[b] counts its tokens in the cache WITH the new ones, and its new token i therefore has the logical position
  * p = lens[b] - n_b + i, which is row p % block_tokens of page page_table[b][p / block_tokens].  starts, lens and page_table are
  * int32 arrays in device memory, which the host cannot vet.  What the kernels enforce: a request with n_b < 0 or
- * > max_new, with rows outside [0, n_tokens), with lens[b] < n_b in kvh_append, with lens[b] < 0 or with more tokens than its row of the table has
- * pages for is refused as a whole (nothing of it is read or written); a page outside [0, pages) is never accessed: tokens on it
+ * > max_new, with rows outside [0, n_tokens), with lens[b] < n_b in kvh_append, with lens[b] < 0, with more tokens than its row of the table has
+ * pages for or with more than 2^31 - 128 is refused as a whole (nothing of it is read or written); a page outside [0, pages) is never accessed: tokens on it
  * are not stored by kvh_append and not seen by kvh_attention (a query that should see nothing else gets NaN).  Either sets status_dev[b] (if status_dev is not NULL; zeroed
  * by the caller, one int32 a request) to KVH_DEV_BAD_REQUEST.  Table entries past a request's last page are not read. */
 #define KVH_DEV_BAD_REQUEST 2

@@ -18,6 +18,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxRequests = 65535;
+constexpr int64_t kMaxLength = INT32_MAX - 127;  // tokens of a request: the number past a step or tile that begins below it is an int32 too
 constexpr int64_t kMaxRowStride = 1 << 20;  // elements: lane offsets inside a tile stay far below 2^31 bytes
 
 inline bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -58,10 +59,10 @@ struct Requests {
   const int32_t* table;
   int64_t table_stride;
   int32_t table_pages, n, max_new, n_tokens;
-  int64_t capacity;  // tokens a row of the table has pages for
+  int64_t capacity;  // tokens a row of the table has pages for, and a request may have
   explicit Requests(const kvh_requests& r, int block_tokens)
       : starts(r.starts), lens(r.lens), table(r.page_table), table_stride(r.table_stride), table_pages(r.table_pages), n(r.n_requests),
-        max_new(r.max_new), n_tokens(r.n_tokens), capacity((int64_t)r.table_pages * block_tokens) {}
+        max_new(r.max_new), n_tokens(r.n_tokens), capacity((int64_t)r.table_pages * block_tokens < kMaxLength ? (int64_t)r.table_pages * block_tokens : kMaxLength) {}
   Requests() = default;
 };
 

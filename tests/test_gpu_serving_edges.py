@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 from test_gpu_serving_attention import Batch  # noqa: E402
 
 BAD = 2  # KVH_DEV_BAD_REQUEST
+TOP = 2 ** 31 - 1
 
 
 @pytest.fixture(scope="module")
@@ -141,3 +142,25 @@ def test_a_long_prompt_takes_no_memory_for_parts(kvh):
     want = kvh.attention(b.q, b.kc, b.vc, 0, b.starts, b.lens, b.table, 8192, head_dim=64, k_scale=b.ks, v_scale=b.vs,
                          workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))  # whole tiles too
     assert torch.equal(out[:, :512], want) and torch.equal(out[:, -512:], want)
+
+
+# ---- limits at the top of int32 -------------------------------------------------------------------------------------
+@pytest.mark.parametrize("news", [1, 40])
+def test_lengths_at_the_top_are_refused(kvh, news):
+    """A table that has room for 2^31 tokens (one page, again and again), and a request that says it holds them."""
+    bt, c = 1 << 16, 64
+    kc = torch.zeros((1, 1, bt, c), dtype=torch.int8, device="cuda")
+    vc = torch.zeros_like(kc)
+    ks, vs = torch.ones((1, 1, 1), device="cuda"), torch.ones((1, 1, 1), device="cuda")
+    table = torch.zeros((1, 1 << 15), dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, news], dtype=torch.int32, device="cuda")
+    q = torch.ones((news, c), dtype=torch.float16, device="cuda")
+    for length in (TOP, TOP - 126):
+        lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 5.0)
+        kvh.attention(q, kc, vc, 0, starts, lens, table, news, head_dim=64, k_scale=ks, v_scale=vs, out=out, status=status)
+        assert status.tolist() == [BAD] and (out == 5).all()
+        status.zero_()
+        kvh.append(q[None], q[None], kc, vc, starts, lens, table, news, head_dim=64, k_scale=ks, v_scale=vs, status=status)
+        assert status.tolist() == [BAD] and not kc.any() and not vc.any()
