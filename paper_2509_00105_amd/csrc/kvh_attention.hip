@@ -768,7 +768,8 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   a.pages = cache->pages, a.block_tokens = cache->block_tokens, a.heads = cache->heads;
   a.group = q_heads / cache->heads;
   a.scale = scale;
-  a.causal = causal != 0, a.sink = sink, a.window = window;
+  a.causal = causal != 0, a.window = window;
+  a.sink = (int)std::min<int64_t>(sink, a.req.capacity);  // no request has a token past it, and steps are counted in 32 bits
   a.status = status_dev;
   a.by_block = Divisor((uint32_t)cache->block_tokens);
   a.by_group = Divisor((uint32_t)a.group);
@@ -777,7 +778,7 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   Plan p = plan_of(a.req.n, a.req.max_new, a.req.n_tokens, a.heads, q_heads, cache->head_dim, two_tiles(cache->kind, cache->head_dim));
   // The steps of the longest tile, and what all tiles come to at most.  The lengths are the device's; the host knows what the table has room for.
   int64_t longest = std::min<int64_t>((a.req.capacity + kStep - 1) / kStep, 1 << 26);
-  if (window != 0) longest = std::min(longest, ((int64_t)window + sink + (1 << p.log_rows)) / kStep + 5);
+  if (window != 0) longest = std::min(longest, ((int64_t)window + a.sink + (1 << p.log_rows)) / kStep + 5);
   const int64_t most = std::min<int64_t>(p.tiles * a.heads, 2 * kFill) * longest;
   if (most < kWideSteps) p.target >>= p.log_hw, p.log_hw = 0;
   // What the longest way through the batch is in whole tiles, and cut: with one request the tiles are alike, but for the new tokens that a causal

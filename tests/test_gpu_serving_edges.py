@@ -164,3 +164,12 @@ def test_lengths_at_the_top_are_refused(kvh, news):
         status.zero_()
         kvh.append(q[None], q[None], kc, vc, starts, lens, table, news, head_dim=64, k_scale=ks, v_scale=vs, status=status)
         assert status.tolist() == [BAD] and not kc.any() and not vc.any()
+
+
+@pytest.mark.parametrize("kind", ["16", "i8"])
+@pytest.mark.parametrize("news,lens", [([2], [70]), ([60], [300]), ([1], [5000]), ([90], [2100])])
+def test_sink_of_any_size(kvh, kind, news, lens):
+    """A sink that holds every token there can be: a causal attention."""
+    b = Batch(news, lens, heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=79, layers=1)
+    for sink in (TOP, TOP - 31, 1 << 30):
+        b.check(b.run(kvh, sink=sink, window=5), sink=sink, window=5)
