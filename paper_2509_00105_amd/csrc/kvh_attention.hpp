@@ -342,7 +342,7 @@ struct Sight {
   int last, low;
   __device__ __forceinline__ Sight() {}
   // `end` is past the last token that any row of the item sees.
-  __device__ __forceinline__ Sight(const AttnParams& a, int end, int p) : last(a.causal && p < end ? p : end - 1), low(a.window != 0 ? p - a.window : -1) {}
+  __device__ __forceinline__ Sight(const AttnParams& a, int end, int p) : last(a.causal && p < end ? p : end - 1), low(a.window != 0 ? (p > 0 ? p : 0) - a.window : -1) {}
   __device__ __forceinline__ bool sees(const AttnParams& a, int token) const { return token <= last && (token > low || token < a.sink); }
   // Of tokens [t0, t0 + 64), those it sees.
   __device__ __forceinline__ uint64_t seen(const AttnParams& a, int t0) const {
@@ -362,7 +362,7 @@ struct Steps {
   __device__ __forceinline__ Steps(const AttnParams& a, int p_least, int end) {
     first = sunk = 0;
     if (a.window != 0) {
-      const int from = p_least - a.window + 1;
+      const int from = (p_least > 0 ? p_least : 0) - a.window + 1;  // positions below 0 see nothing
       first = from > 0 ? from / kStep & ~1 : 0;
       sunk = (a.sink + kStep - 1) / kStep + 1 & ~1;
       if (sunk >= first) first = sunk = 0;

@@ -173,3 +173,12 @@ def test_sink_of_any_size(kvh, kind, news, lens):
     b = Batch(news, lens, heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=79, layers=1)
     for sink in (TOP, TOP - 31, 1 << 30):
         b.check(b.run(kvh, sink=sink, window=5), sink=sink, window=5)
+
+
+@pytest.mark.parametrize("group", [1, 2, 8])
+def test_window_of_any_size_and_rows_before_the_first_token(kvh, group):
+    """More queries than tokens, and a window that reaches past every position."""
+    b = Batch([13], [4], heads=2, group=group, dim=64, kind="16", dt="fp16", seed=83, layers=1)
+    for window in (TOP, TOP - 5, 1 << 30):
+        b.check(b.run(kvh, window=window), window=window)
+        b.check(b.run(kvh, window=window, sink=2), window=window, sink=2)
