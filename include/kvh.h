@@ -376,7 +376,7 @@ typedef struct {
   int32_t table_pages;
   int32_t n_requests;        /* 1 .. 65535 */
   int32_t max_new;           /* no request brings more new tokens; >= 1 */
-  int32_t n_tokens;          /* rows of the packed tensors; 0: nothing is done */
+  int32_t n_tokens;          /* rows of the packed tensors; 0: nothing is done, and rows may be NULL */
 } kvh_requests;
 
 /* Rows of 16-bit elements, [layers][n_tokens][channels]; strides in elements, multiples of 8; base 16-byte aligned. */

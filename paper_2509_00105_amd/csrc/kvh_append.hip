@@ -361,18 +361,18 @@ extern "C" int kvh_append(const kvh_cache* cache, const kvh_requests* requests, 
   if (dt != KVH_F16 && dt != KVH_BF16) return KVH_E_ARG;
   if (int rc = check_cache(cache)) return rc;
   if (int rc = check_requests(requests)) return rc;
-  if (kv == nullptr || kv->k == nullptr || kv->v == nullptr) return KVH_E_ARG;
+  if (kv == nullptr) return KVH_E_ARG;
   const int64_t c = (int64_t)cache->heads * cache->head_dim;
   for (void* p : {kv->k, kv->v}) {
     const kvh_rows rows{p, kv->layer_stride, kv->token_stride};
-    if (int rc = check_rows(&rows, c)) return rc;
+    if (int rc = check_rows(&rows, c, requests->n_tokens)) return rc;
   }
   AppendParams a{};
   if (q != nullptr) {
     if (q_out == nullptr) return KVH_E_ARG;
     if (q_heads < 1 || q_heads > 65536) return KVH_E_SHAPE;
     for (const kvh_rows* r : {q, q_out})
-      if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim)) return rc;
+      if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim, requests->n_tokens)) return rc;
     a.q = static_cast<const uint16_t*>(q->p);
     a.q_out = static_cast<uint16_t*>(q_out->p);
     a.q_ls = q->layer_stride, a.q_ts = q->token_stride;

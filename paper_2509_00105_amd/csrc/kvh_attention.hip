@@ -745,7 +745,7 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
   if (int rc = check_requests(requests)) return rc;
   if (layer < 0 || layer >= cache->layers || !heads_fit(cache->heads, q_heads)) return KVH_E_SHAPE;
   for (const kvh_rows* r : {q, out})
-    if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim)) return rc;
+    if (int rc = check_rows(r, (int64_t)q_heads * cache->head_dim, requests->n_tokens)) return rc;
   if (!std::isfinite(scale) || sink < 0 || window < 0 || (window > 0 && !causal) || (window == 0 && sink != 0)) return KVH_E_ARG;
   if (!is_aligned16(workspace_dev) || (reinterpret_cast<uintptr_t>(lse_dev) & 3u) != 0) return KVH_E_ALIGN;
   if (requests->n_tokens == 0) return KVH_OK;

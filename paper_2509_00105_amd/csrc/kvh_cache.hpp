@@ -46,8 +46,8 @@ inline int check_requests(const kvh_requests* r) {
   return KVH_OK;
 }
 
-inline int check_rows(const kvh_rows* r, int64_t channels) {
-  if (r->p == nullptr || r->layer_stride < 0 || r->token_stride < channels) return KVH_E_ARG;
+inline int check_rows(const kvh_rows* r, int64_t channels, int n_tokens) {
+  if ((r->p == nullptr && n_tokens != 0) || r->layer_stride < 0 || r->token_stride < channels) return KVH_E_ARG;
   if (!is_aligned16(r->p) || r->layer_stride % 8 != 0 || r->token_stride % 8 != 0) return KVH_E_ALIGN;
   return KVH_OK;
 }

@@ -6,6 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+import test_gpu_serving_append as appending  # noqa: E402
 from test_gpu_serving_attention import Batch  # noqa: E402
 
 BAD = 2  # KVH_DEV_BAD_REQUEST
@@ -182,3 +183,20 @@ def test_window_of_any_size_and_rows_before_the_first_token(kvh, group):
     for window in (TOP, TOP - 5, 1 << 30):
         b.check(b.run(kvh, window=window), window=window)
         b.check(b.run(kvh, window=window, sink=2), window=window, sink=2)
+
+
+# ---- steps without tokens -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["16", "i8"])
+def test_a_step_without_tokens(kvh, kind):
+    """No row at all, as a step of requests that all wait gives it: nothing is done, and nothing is raised."""
+    b = Batch([0, 0], [40, 0], heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=89, layers=1)
+    before = [t.clone() for t in (b.kc, b.vc)]
+    out = b.run(kvh)
+    assert out.shape == (0, 256)
+    assert kvh.attention(b.q, b.kc, b.vc, 0, b.starts, b.lens, b.table, 1, head_dim=64, k_scale=b.ks, v_scale=b.vs, out=out, lse=b.lse,
+                         workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")) is out
+    x = torch.empty((1, 0, 128), dtype=torch.float16, device="cuda")
+    q = torch.empty((1, 0, 256), dtype=torch.float16, device="cuda")
+    assert kvh.append(x, x, b.kc, b.vc, b.starts, b.lens, b.table, 1, head_dim=64, k_scale=b.ks, v_scale=b.vs, q=q,
+                      rotation=appending.rotation(50, 64).cuda()).shape == q.shape
+    assert not b.status.any() and all(torch.equal(x.view(torch.int8), y.view(torch.int8)) for x, y in zip((b.kc, b.vc), before))
