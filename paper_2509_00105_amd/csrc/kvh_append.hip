@@ -112,7 +112,7 @@ struct Tile {
   float x[kSteps][8];
   bool valid[kSteps];
 
-  // `turn`: rotate.  Returns whether a token had no position in the table.
+  // `turn`: rotate.  Returns whether a token had no position in the table, which then is not valid, rotated or not.
   __device__ __forceinline__ bool load(const AppendParams& a, const uint16_t* src, int64_t ts, const Request& rq, int i0, int i_end,
                                        bool turn, int lane) {
     const int col = lane % kLanes, sub = lane / kLanes;
@@ -127,7 +127,7 @@ struct Tile {
       pos[s] = 0;
       if (valid[s]) {
         raw[s] = *reinterpret_cast<const u32x4*>(src + ((int64_t)rq.start + i) * ts + col * 8);
-        if (turn) {
+        if (a.rot != 0) {
           pos[s] = position(a, rq, i);
           if (pos[s] < 0) {
             bad = true;
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
         const int i = i0 + s < rq.n ? i0 + s : rq.n - 1;
         page[s] = page_of(i);
         raw[s] = get<PAST, u32x4>(src + ((int64_t)rq.start + i) * ts + at);
-        pos[s] = turn ? position(a, rq, i) : 0;
+        pos[s] = a.rot != 0 ? position(a, rq, i) : 0;  // a token without one is not stored, its values no more than its keys
       }
 #pragma unroll
       for (int s = 0; s < kAtOnce; ++s) {

@@ -200,3 +200,45 @@ def test_a_step_without_tokens(kvh, kind):
     assert kvh.append(x, x, b.kc, b.vc, b.starts, b.lens, b.table, 1, head_dim=64, k_scale=b.ks, v_scale=b.vs, q=q,
                       rotation=appending.rotation(50, 64).cuda()).shape == q.shape
     assert not b.status.any() and all(torch.equal(x.view(torch.int8), y.view(torch.int8)) for x, y in zip((b.kc, b.vc), before))
+
+
+# ---- tokens without a position --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["16", "i8", "e4m3"])
+@pytest.mark.parametrize("bt", [16, 40])
+def test_tokens_without_a_position(kvh, kind, bt):
+    """Neither their keys nor their values nor their queries are stored, nor do they count for a page's scales; the others' are."""
+    b = appending.Batch([30, 1, 6], [3, 20, 0], heads=2, dim=64, kind=kind, bt=bt, seed=91)
+    table = appending.rotation(64, 64)
+    pos = torch.randint(0, 64, (37,), dtype=torch.int32)
+    lost = [2, 3, 17, 30]
+    pos[lost] = torch.tensor([64, -1, 1 << 30, -(1 << 31)], dtype=torch.int32)
+    b.v[:, lost] *= 100  # would show in a scale
+    old = [t.clone() if t is not None else None for t in (b.kc, b.vc, b.ks, b.vs)]
+    q_out = torch.full_like(b.q, 5.0)
+    b.append(kvh, rotation=table.cuda(), positions=pos.cuda(), q=b.q, q_out=q_out)
+    assert b.status.tolist() == [BAD, BAD, 0]
+    keep = [t for t in range(37) if t not in lost]
+    split = lambda x: x.float().cpu().unflatten(-1, (-1, 64))  # noqa: E731
+    at = pos.clamp(0, 63).long()
+    k32 = appending.turned32(split(b.k), at, table, False)
+    assert (q_out[:, lost] == 5).all()
+    assert torch.equal(q_out[:, keep].cpu(), appending.turned32(split(b.q), at, table, False).to(b.q.dtype).flatten(-2)[:, keep])
+    slots = [(t, page, row) for _, t, _, page, row in appending.ref.slots(b.starts_h, b.lens_h, b.table_h.tolist(), bt)]
+    for x, before, after, scale0, scale1 in ((k32, old[0], b.kc, old[2], b.ks), (split(b.v), old[1], b.vc, old[3], b.vs)):
+        if kind == "16":
+            want = before.cpu().clone()
+            for t, page, row in slots:
+                if t not in lost:
+                    want[:, page, row] = x[:, t].to(b.k.dtype).flatten(-2)
+            assert torch.equal(after.cpu().view(torch.int16), want.view(torch.int16))
+            continue
+        # the values of the tokens that are not stored count as zeros for the scale; what stands in their rows is of no account
+        x = x.clone()
+        x[:, lost] = 0.0
+        codes, scales = appending.coded32(x, before, scale0, b, kind)
+        got = after.cpu().float()
+        for t, page, row in slots:
+            if t in lost:
+                assert torch.equal(got[:, page, row], before.cpu().float()[:, page, row])
+                got[:, page, row] = codes[:, page, row]
+        assert torch.equal(scale1.cpu(), scales) and torch.equal(got, codes)
