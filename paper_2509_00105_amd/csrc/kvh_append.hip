@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kBlockThreads) void append_kernel(AppendParams a) {
         if (turn) {
           float x[8];
           turn8<DT>(a, raw[s], pos[s] < 0 ? 0 : pos[s], col * 8, lane, x);
-          raw[s] = packed8<DT>(x);
+          if (col * 8 < a.rot) raw[s] = packed8<DT>(x);  // other channels keep every bit, those of a NaN too
         }
         if (i0 + s >= rq.n) continue;
         uint16_t* row = pos[s] < 0 ? nullptr : to(i0 + s, page[s]);

@@ -242,3 +242,18 @@ def test_tokens_without_a_position(kvh, kind, bt):
                 assert torch.equal(got[:, page, row], before.cpu().float()[:, page, row])
                 got[:, page, row] = codes[:, page, row]
         assert torch.equal(scale1.cpu(), scales) and torch.equal(got, codes)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_channels_past_the_rotation_keep_every_pattern(kvh, dt, pairs):
+    """What is not rotated is stored as it is, in rows whose first channels are."""
+    b = appending.Batch([20], [5], heads=2, dim=64, kind="16", dt=dt, seed=97)
+    g = torch.Generator().manual_seed(1)
+    for name in ("k", "q"):
+        x = getattr(b, name)
+        setattr(b, name, torch.randint(-32768, 32768, x.shape, generator=g, dtype=torch.int16).cuda().view(x.dtype))
+    q_out = b.append(kvh, rotation=appending.rotation(64, 32).cuda(), pairs=pairs, q=b.q)
+    got = torch.stack([b.kc[0, page, row] for _, _, _, page, row in appending.ref.slots(b.starts_h, b.lens_h, b.table_h.tolist(), 16)])
+    for x, y in ((got, b.k[0]), (q_out[0], b.q[0])):
+        assert torch.equal(x.view(torch.int16).unflatten(-1, (-1, 64))[..., 32:], y.view(torch.int16).unflatten(-1, (-1, 64))[..., 32:])
