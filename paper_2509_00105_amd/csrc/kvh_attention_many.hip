@@ -68,7 +68,7 @@ struct Tiles {
   uint32_t v[8][kVWords];
   uint32_t none;         // of its 8 tokens of V, those past the end or on no page of the cache
   uint64_t absent;       // the tile's tokens on no page of the cache
-  uint64_t odd_k, odd_v; // its others whose K or V scale is no finite number; known when the tile has been stored, and the scales are ones to be used then
+  bool odd_page;         // a scale of the tile is no finite number; known when the tile has been stored, and the scales are ones to be used then
   bool edge;             // some row of the block does not see all of the tile
   float ks[4], vs[4];    // scales of the tile's groups of 16 tokens (PAGE16), or of its token `lane` in [0]
 
@@ -229,6 +229,21 @@ struct Tiles {
     return w;
   }
 
+  // The tokens of the tile at t0 whose scales are no finite numbers, again from the cache.
+  __device__ __forceinline__ void odd_tokens(int t0, uint64_t& k, uint64_t& v) const {
+    int lane = this->lane;
+    asm volatile("" : "+v"(lane));  // as in odd_ones
+    bool odd_k = false, odd_v = false;
+    if (t0 + lane < end) {
+      const int page = table[a.by_block.quotient((uint32_t)(t0 + lane))];
+      if (page >= 0 && page < a.pages) {
+        odd_k = odd_scale(a.sk[(int64_t)page * a.s_ps + head]);
+        odd_v = odd_scale(a.sv[(int64_t)page * a.s_ps + head]);
+      }
+    }
+    k = __ballot(odd_k), v = __ballot(odd_v);
+  }
+
   // Stores what was fetched into a buffer, as operands.
   __device__ __forceinline__ void store_tile(int buffer) {
     const uint32_t kb = k_to + buffer * kBuffer, vb = v_to + buffer * kBuffer;
@@ -294,7 +309,7 @@ struct Tiles {
       ScaleRange range;
 #pragma unroll
       for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) range.add(ks[g], vs[g]);
-      odd_k = odd_v = 0;
+      odd_page = false;
       if (__builtin_expect(__any(range.rare()), 0)) {
         // Below the least that the exponent takes the rest goes onto the values.
 #pragma unroll
@@ -312,16 +327,10 @@ struct Tiles {
         }
 #pragma unroll
         for (int g = 0; g < (PAGE16 ? 4 : 1); ++g) {
-          if constexpr (PAGE16) {
-            odd_k |= odd_scale(ks[g]) ? (uint64_t)0xffff << 16 * g : 0;
-            odd_v |= odd_scale(vs[g]) ? (uint64_t)0xffff << 16 * g : 0;
-          } else {
-            odd_k = __ballot(odd_scale(ks[g])), odd_v = __ballot(odd_scale(vs[g]));
-          }
+          odd_page |= __any(odd_scale(ks[g]) || odd_scale(vs[g]));
           ks[g] = odd_scale(ks[g]) ? 1.0f : ks[g];
           vs[g] = ValueScale(vs[g]).used;
         }
-        odd_k &= ~absent, odd_v &= ~absent;
       }
     }
 #pragma unroll
@@ -433,7 +442,8 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
   for (int s = s0; s < s1; s += 2, buffer ^= 1) {
     const int t0 = steps.token(s);
     t.store_tile(buffer);
-    const uint64_t absent = t.absent, odd_k = kScaled ? t.odd_k : 0, odd_v = kScaled ? t.odd_v : 0;
+    const uint64_t absent = t.absent;
+    const bool odd_page = kScaled && t.odd_page;
     // An element's exponent of 2 is f x + z, by groups of 16 tokens (one group where there are no scales).
     constexpr int kGroups = kScaled && PAGE16 ? 4 : 1;
     float f[kGroups], z[kGroups], inv[kGroups];
@@ -457,10 +467,12 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, int 
     const bool blank = !works || (a.causal && t0 > p_most);  // no row of the wave sees any of it
     if (blank) continue;
     if constexpr (kScaled) {
-      if (__builtin_expect((odd_k | odd_v) != 0, 0)) {
+      if (__builtin_expect(odd_page, 0)) {
         const uint64_t seen = sight.seen(a, t0);
-        spoiled |= (seen & odd_v) != 0;
-        lost |= (seen & odd_k) != 0;
+        uint64_t k, v;
+        t.odd_tokens(t0, k, v);
+        spoiled |= (seen & v) != 0;
+        lost |= (seen & k) != 0;
       }
     }
     const uint32_t kb = k_at + buffer * T::kBuffer, vb = v_at + buffer * T::kBuffer;
