@@ -582,17 +582,26 @@ CACHE_16, CACHE_I8, CACHE_E4M3 = 0, 1, 2
 _CODES = {torch.int8: CACHE_I8, torch.float8_e4m3fn: CACHE_E4M3}
 
 
+def _step(t, dim, alone):
+    """The stride of a dimension; `alone` where it has one entry at most, whose stride is of no account."""
+    return t.stride(dim) if t.shape[dim] > 1 else alone
+
+
+def _steps(t):
+    return [_step(t, d, 1) for d in range(t.dim())]
+
+
 def _cache(k_cache, v_cache, k_scale, v_scale, head_dim, dtype):
     """kvh_cache of [l][P][block][c] tensors (codes or the 16-bit type of the call) and [l][P][heads] scales."""
     _require_cuda(k_cache, v_cache, k_scale, v_scale)
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or _steps(k_cache) != _steps(v_cache) or k_cache.dtype != v_cache.dtype:
         raise ValueError("the K and V caches must be [l][P][block][c] with equal shapes, strides and types")
     kind = CACHE_16 if k_cache.dtype == dtype else _CODES.get(k_cache.dtype)
     if kind is None:
         raise ValueError("the cache must hold the type of the call, int8 or float8_e4m3fn")
     l, pages, block, c = k_cache.shape
     row = k_cache.stride(2) if block > 1 else k_cache.stride(1) if pages > 1 else c
-    if k_cache.stride(3) != 1 or (pages > 1 and k_cache.stride(1) != row * block):
+    if _step(k_cache, 3, 1) != 1 or (pages > 1 and k_cache.stride(1) != row * block):
         raise ValueError("channel stride must be 1 and blocks of a paged cache densely packed")
     if head_dim < 1 or c % head_dim:
         raise ValueError("c must be a multiple of head_dim")
@@ -602,12 +611,12 @@ def _cache(k_cache, v_cache, k_scale, v_scale, head_dim, dtype):
             raise ValueError("a 16-bit cache has no scales")
     else:
         for t in (k_scale, v_scale):
-            if t is None or t.dtype != torch.float32 or t.shape != (l, pages, heads) or t.stride() != k_scale.stride():
+            if t is None or t.dtype != torch.float32 or t.shape != (l, pages, heads) or _steps(t) != _steps(k_scale):
                 raise ValueError("an 8-bit cache needs float32 scales [l][P][heads] for K and V, of equal strides")
-        if k_scale.stride(2) != 1 and heads > 1:
+        if _step(k_scale, 2, 1) != 1:
             raise ValueError("the heads of a page's scales must be dense")
-        ls, ps = k_scale.stride(0), k_scale.stride(1) if pages > 1 else heads
-    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), k_cache.stride(0), row,
+        ls, ps = _step(k_scale, 0, 0), _step(k_scale, 1, heads)
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), _step(k_cache, 0, 0), row,
                   ls, ps, l, pages, block, heads, head_dim, kind)
 
 
@@ -626,7 +635,7 @@ def _empty(shape, dtype, device, stream):
 def _int32(t, name, dim, least=0):
     if t is not None:
         _require_cuda(t)
-        if t.dtype != torch.int32 or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1) or t.shape[0] < least:
+        if t.dtype != torch.int32 or t.dim() != dim or _step(t, -1, 1) != 1 or t.shape[0] < least:
             raise ValueError("%s must be a dense int32 tensor of %d dimension(s) with enough entries" % (name, dim))
 
 
@@ -636,15 +645,15 @@ def _requests(starts, lens, page_table, max_new, n_tokens, status):
     _int32(starts, "starts", 1, n + 1)
     _int32(page_table, "page_table", 2, n)
     _int32(status, "status", 1, n)
-    return _Requests(starts.data_ptr(), lens.data_ptr(), page_table.data_ptr(), page_table.stride(0), page_table.shape[1], n, max_new, n_tokens)
+    return _Requests(starts.data_ptr(), lens.data_ptr(), page_table.data_ptr(), _step(page_table, 0, page_table.shape[1]), page_table.shape[1], n, max_new, n_tokens)
 
 
 def _rows(t, layers, n_tokens, head_dim, dtype, name):
     """kvh_rows of [l][T][heads * head_dim], and its heads."""
     _require_cuda(t)
-    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != layers or t.shape[1] != n_tokens or t.shape[2] % head_dim or t.stride(2) != 1:
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != layers or t.shape[1] != n_tokens or t.shape[2] % head_dim or _step(t, 2, 1) != 1:
         raise ValueError("%s must be [l][T][heads * head_dim] of the call's type, with channel stride 1" % name)
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1) if n_tokens > 1 else max(t.stride(1), t.shape[2])), t.shape[2] // head_dim
+    return _Rows(t.data_ptr(), _step(t, 0, 0), _step(t, 1, t.shape[2])), t.shape[2] // head_dim
 
 
 def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
@@ -660,13 +669,16 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     if rc is not None:
         _check(rc, "kvh_append")
         return q_out
-    view, dt = _view(k, v)
+    _require_cuda(k, v)
+    if k.dtype not in _TORCH_DT or v.dtype != k.dtype:
+        raise ValueError("K and V must both be float16 or both bfloat16")
+    if k.dim() != 3 or k.shape != v.shape or _steps(k) != _steps(v) or _step(k, 2, 1) != 1:
+        raise ValueError("K and V must be [l][T][c] with equal shapes and strides, and channel stride 1")
     l, T, c = k.shape
+    view, dt = _KVView(k.data_ptr(), v.data_ptr(), _step(k, 0, 0), _step(k, 1, c)), _TORCH_DT[k.dtype]
     cache = _cache(k_cache, v_cache, k_scale, v_scale, head_dim, k.dtype)
     if (l, c) != (cache.layers, cache.heads * head_dim):
         raise ValueError("K and V must have the cache's layers and channels")
-    if T <= 1:
-        view.token_stride = max(view.token_stride, c)
     req = _requests(starts, lens, page_table, max_new, T, status)
     rows = out = rot = None
     q_heads = 0
@@ -679,10 +691,10 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
             raise ValueError("q_out must have the shape of q")
     if rotation is not None:
         _require_cuda(rotation)
-        if rotation.dtype != torch.float32 or rotation.dim() != 2 or rotation.stride(1) != 1:
+        if rotation.dtype != torch.float32 or rotation.dim() != 2 or _step(rotation, 1, 1) != 1:
             raise ValueError("rotation must be float32 [positions][rot], dense in rot")
         _int32(positions, "positions", 1, T)
-        rot = _Rotation(rotation.data_ptr(), _ptr(positions), rotation.stride(0), rotation.shape[0], rotation.shape[1], int(pairs))
+        rot = _Rotation(rotation.data_ptr(), _ptr(positions), _step(rotation, 0, rotation.shape[1]), rotation.shape[0], rotation.shape[1], int(pairs))
     elif positions is not None:
         raise ValueError("positions without a rotation")
     ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731

@@ -257,3 +257,33 @@ def test_channels_past_the_rotation_keep_every_pattern(kvh, dt, pairs):
     got = torch.stack([b.kc[0, page, row] for _, _, _, page, row in appending.ref.slots(b.starts_h, b.lens_h, b.table_h.tolist(), 16)])
     for x, y in ((got, b.k[0]), (q_out[0], b.q[0])):
         assert torch.equal(x.view(torch.int16).unflatten(-1, (-1, 64))[..., 32:], y.view(torch.int16).unflatten(-1, (-1, 64))[..., 32:])
+
+
+# ---- strides of one entry -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["16", "i8"])
+@pytest.mark.parametrize("by_ctypes", [False, True])
+def test_a_stride_of_one_entry_is_of_no_account(kvh, kind, by_ctypes, monkeypatch):
+    """One token, one layer: keys beside values of another tensor, whatever the strides of those dimensions are, by either way into the calls."""
+    import paper_2509_00105_amd.binding as binding
+
+    if by_ctypes:
+        monkeypatch.setattr(binding, "_fast", None)
+    b = Batch([1], [33], heads=2, group=2, dim=64, kind=kind, dt="fp16", seed=93, layers=1)
+    g = torch.Generator().manual_seed(2)
+    row = torch.randn((1, 516), generator=g).half().cuda()  # queries, keys and values of a token; 516 is no multiple of 8
+    q, k, v = row[None, :, :256], row[None, :, 256:384], row[:, 384:512].clone()[None]
+    k, q = k.as_strided(k.shape, (3, 5, 1)), q.as_strided(q.shape, (7, 516, 1))
+    table = appending.rotation(64, 64).cuda()
+    want = [t.clone() if t is not None else None for t in (b.kc, b.vc, b.ks, b.vs)]
+    out = kvh.append(k.contiguous(), v, *want[:2], b.starts, b.lens, b.table, 1, head_dim=64, k_scale=want[2], v_scale=want[3], q=q.contiguous(), rotation=table)
+    odd = lambda t: None if t is None else t.as_strided(t.shape, (5, *t.stride()[1:]))  # noqa: E731
+    for q_out in (None, torch.empty((1, 1, 256), dtype=torch.float16, device="cuda")):
+        got = [t.clone() if t is not None else None for t in (b.kc, b.vc, b.ks, b.vs)]
+        assert torch.equal(out, kvh.append(k, v, odd(got[0]), got[1], b.starts, b.lens, b.table, 1, head_dim=64, k_scale=got[2], v_scale=odd(got[3]), q=q, q_out=q_out,
+                                           rotation=table))
+        assert all(x is None or torch.equal(x.view(torch.int8), y.view(torch.int8)) for x, y in zip(got, want))
+    plain = kvh.attention(out[0], *want[:2], 0, b.starts, b.lens, b.table, 1, head_dim=64, k_scale=want[2], v_scale=want[3])
+    room = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for o, ws in ((None, None), (torch.empty_like(plain), room)):
+        assert torch.equal(plain, kvh.attention(out[0].as_strided((1, 256), (3, 1)), odd(want[0]), want[1], 0, b.starts, b.lens, b.table, 1, head_dim=64,
+                                                k_scale=want[2], v_scale=odd(want[3]), out=o, workspace=ws))
