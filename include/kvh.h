@@ -348,7 +348,8 @@ int kvh_load_static(const kvh_load_item* items, int n_items, kvh_dtype dt, int l
  * > max_new, with rows outside [0, n_tokens), with lens[b] < n_b in kvh_append, with lens[b] < 0, with more tokens than its row of the table has
  * pages for or with more than 2^31 - 128 is refused as a whole (nothing of it is read or written); a page outside [0, pages) is never accessed: tokens on it
  * are not stored by kvh_append and not seen by kvh_attention (a query that should see nothing else gets NaN).  Either sets status_dev[b] (if status_dev is not NULL; zeroed
- * by the caller, one int32 a request) to KVH_DEV_BAD_REQUEST.  Table entries past a request's last page are not read. */
+ * by the caller, one int32 a request) to KVH_DEV_BAD_REQUEST.  Table entries past a request's last page are not read.  starts must not fall: where a request is refused
+ * because they do, requests may share rows, and what these and later requests' rows become is unspecified (no other memory is touched). */
 #define KVH_DEV_BAD_REQUEST 2
 
 typedef enum { KVH_CACHE_16 = 0, KVH_CACHE_I8 = 1, KVH_CACHE_E4M3 = 2 } kvh_cache_kind;
@@ -419,8 +420,14 @@ int kvh_append(const kvh_cache* cache, const kvh_requests* requests, kvh_dtype d
  * u / (q_heads / heads).  A query that sees nothing gets zeros, and minus infinity in lse.  lse (nullable): [n_tokens][q_heads]
  * floats, the natural logarithm of sum_j w_ij.
  * Precision: products in the matrix cores, sums, maxima and the softmax in fp32; the weights are rounded to 16 bits before they
- * meet the values.  What a query does not see does not reach its result, whatever it is; infinities and NaN in what it sees do
- * as in the formula.
+ * meet the values.  Over 8-bit caches bf16 queries become fp16, scaled by a power of two of their row and head: channels 2^14 and more below the largest lose
+ * bits.  V scales are exact factors from 2^-60 to 2^60; below, values lose bits and become zeros.  What a query does not see does not reach its result,
+ * whatever it is, codes and scales; infinities and NaN in what it sees do as in the formula, except that an infinity whose weight is too small for the weights'
+ * type may give NaN.
+ * Speed: how a call is laid out follows from what the host knows - counts, max_new and the room of the page table, not lens.  With a table much wider than the
+ * longest request a batch may be split that need not be (one token of 300, 16 bits, 8 KV heads of 128: 8.6 us with a table as wide as the request, 12 with one
+ * for 8192 tokens, 20 for 131072): pass the columns in use where that matters.  A batch is split only while its row tiles times heads stay below 1024 (8 KV heads and
+ * groups of 4: up to 102 single tokens), and one request's queries decide for all whether tiles of 16 or 128 rows are used.
  * workspace_dev: device memory for partial results where few queries meet many tokens and the tokens of a request are split over
  * the GPU; 16-byte aligned.  kvh_attention_workspace says how much serves a batch best: 0 where a batch has so many queries that it is never
  * split (or where the arguments are none of an attention), and 256 MiB at most; memory for batches of several kinds is as large as the largest of theirs.  With

@@ -7,8 +7,9 @@
 // other half of a rotated pair is 0 lanes away or rot / 16 lanes, and comes by a lane exchange, which also makes q_out == q safe.
 //
 // Memory bounds it (some 6 operations an element), or for a step of single tokens the launch.  Measured, 8 KV heads of 128, 32 query heads: a
-// prompt of 8192 into e4m3, rotated: 38.7 us = 4.9 TB/s, what a plain copy reaches; 16 prompts of 1500 in 16 bits (10 KV heads of 64): 48.6 us = 5.0
-// TB/s; 32 layers of 256 tokens into int8: 11.5 us = 4.4 TB/s; 64 single tokens into int8: 5.3 us, one: 4.7 us, a kernel of 3.6.
+// prompt of 8192 into e4m3, rotated: 38.9 us = 4.9 TB/s, what a plain copy reaches; 16 prompts of 1500 in 16 bits (10 KV heads of 64): 49.8 us = 4.9
+// TB/s; 32 layers of 256 tokens into int8: 11.5 us = 4.4 TB/s; 64 single tokens into int8: 5.5 us, one: 4.7 us, a kernel of 3.7.  The grid is as wide as the
+// request with the most new tokens for every one: a prompt of 8192 beside 63 single tokens takes 234 us, apart 39 and 5.
 #include "kvh_cache.hpp"
 
 namespace kvh {

@@ -9,14 +9,14 @@
 // A code enters the products as the number it is (an int8 or e4m3 is exact in fp16; the queries are brought to fp16 with a power of
 // two of their row's own), the K scale of its page multiplies the finished dot product, and the V scale sv of its page enters the
 // exponent: with s' = s + log2 sv and m' = max s', the weight exp2(s' - m') <= 1 multiplies the code and exp2(s' - m') / sv adds
-// to the sum.  A weight is thus as exact as fp16 is, however the scales of a request's pages differ.
+// to the sum.  A weight is thus as exact as fp16 is, however the scales of a request's pages differ between 2^-60 (kLeastScale) and 2^60.
 //
 // This kernel is the one for few rows (single tokens, short questions): each byte of the cache is read once and used by 16 rows at most, so it is bound
 // by memory, and where little is read by the chain table -> page -> scores -> values of a step.  Keys and values go from memory to the
 // registers that the matrix instructions take them from, without LDS: no other wave wants them.
-// Measured: 64 requests of 4096 tokens (lognormal), 8 KV heads of 128, 32 query heads: bf16 185 us = 5.2 TB/s (a plain read reaches 6.5), int8 109 us =
-// 4.5 TB/s (a head's rows are 128 bytes there; without any arithmetic it takes as long); one of 131072, e4m3: 67 us = 4.0 TB/s, 10 of them
-// joining; one of 300: 8.7 us.
+// Measured: 64 requests of 4096 tokens (lognormal), 8 KV heads of 128, 32 query heads: bf16 186 us = 5.2 TB/s (a plain read reaches 6.5), int8 and e4m3 110 us =
+// 4.4 TB/s (a head's rows are 128 bytes there; waves wait for memory 57 % of their time, vector instructions take 39 % of the SIMDs': too little is under
+// way at a time); one of 131072, e4m3: 67 us = 4.0 TB/s, 10 of them joining; one of 300: 8.6 us.
 #include "kvh_attention.hpp"
 
 #include <algorithm>
@@ -38,7 +38,8 @@ struct Worker {
   static constexpr int kVWords = kChans * kWidth / 4;  // words of V that a lane reads of a token
   static constexpr int kScales = kScaled ? (PAGE16 ? 2 : 8) : 1;
   // Loads of the next step under way while this one is worked on: where lanes look pages up before they load and registers allow it (40 requests
-  // of 4000, e4m3, D 64, pages of 24: 61 us, 76 without; D 128: 84 and 83; pages of 16, 64 requests of 4096, int8, D 128: 113 and 109).
+  // of 4000, pages of 24, D 64: int8 63 us, 74 without, e4m3 60 and 63; D 128, where it was not kept: 83 and 83, 80 and 80; pages of 16, 64 requests of 4096, int8,
+  // D 128: 114 and 110).
   static constexpr bool kAhead = NR == 1 && kScaled && !PAGE16 && D == 64;
 
   // A step's tokens as they are in the cache.  Token slot 4 i + r of a lane is token 16 i + 4 grp + r of the step.
@@ -619,7 +620,8 @@ __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, int l
 
 // ---- launch -------------------------------------------------------------------------------------------------------
 // Rules with both sides measured (us, 8 KV heads of 128, 32 query heads unless said; "after": new tokens after cached ones).
-// Blocks of 4 waves that fill the chip: their registers leave room for 2 on a compute unit.  Chunks for 512 / 256 / 1024 blocks: 512 after 32768,
+// Blocks of 4 waves that fill the chip: 2 on a compute unit, for which 16 bits of 128 channels have registers (190).  Others would have room for more (int8
+// of 128 channels 3, at 130 registers; heads of 64 4, at 100 to 127), which is not tried.  Chunks for 512 / 256 / 1024 blocks: 512 after 32768,
 // int8: 391 / 590 / 419; one of 131072, e4m3: 67 / 62 / 67; 64 of 4096, int8: 113 / - / 119.
 constexpr int kFill = 512;
 // Steps of a chunk at least: 4, one for each wave (one request of 2100: 12; 16 steps: 15), but 16 where a wave takes all of a chunk by itself
@@ -629,11 +631,12 @@ constexpr int kLeastSteps = 4, kLeastWide = 16;
 // 13; 16 of 500 cut 18, whole 12.  Many: 128 after 1000 cut 25, whole 45; a prompt of 1024 cut 53, whole 42; 8 of 300 after 500 cut 98, whole 70.
 constexpr int kGainFew = 16, kGainMany = 24;
 // Steps of all heads from which on a block's waves take neighbouring heads, whose rows of a token lie together, and not parts of one head's tokens, which
-// shorten what a step waits for: 64 of 4096, int8: 113, 126 by tokens; 4 of 10000, int8: 28 by tokens, 35 by heads; one of 8000: 16 and 32.
+// shorten what a step waits for: 64 of 4096, int8: 110, 126 by tokens; 4 of 10000, int8: 28 by tokens, 35 by heads; one of 8000: 16 and 32.
 constexpr int kWideSteps = 40 * kFill;
 
-// 17 to 32 rows: two tiles of 16 share what is read where both tiles' outputs fit the registers beside it, which is not so for 128 channels of 16
-// bits; the kernel for many rows takes those.  16 requests, 8 after 4000: int8 62, with the other kernel 68; bf16 95 and 82; bf16 with heads of 64: 46 and 52.
+// 17 to 32 rows: two tiles of 16 share what is read, but for 128 channels of 16 bits, where both tiles' outputs do not fit the registers beside it; the
+// kernel for many rows takes those.  16 requests, 8 after 4000: int8 62, with the other kernel 68; e4m3, which spills 25 registers of 128 channels, 64 and
+// 70 (pages of 24, 38 spilled: 77 and 73); bf16 95 and 82; bf16 with heads of 64: 46 and 52.
 // More rows are the other kernel's (9 after 8000: 25; with pairs of tiles 44).
 template <int KIND, int D>
 constexpr bool kTwoTiles = KIND != KVH_CACHE_16 || D == 64;
@@ -669,7 +672,7 @@ Plan plan_of(int n_requests, int max_new, int n_tokens, int heads, int q_heads, 
 
 template <int DT, int KIND, int D, int NR>
 void launch_pages(const AttnParams& a, dim3 grid, hipStream_t stream) {
-  if (a.block_tokens % 16 == 0)  // 64 requests of 4096, int8: 109 us, 122 by looking every token up; one of 300: 9 and 11
+  if (a.block_tokens % 16 == 0)  // 64 requests of 4096, int8: 110 us, 124 by looking every token up; one of 300: 8.5 and 9.3
     launch_kernel(attention_kernel<DT, KIND, D, NR, true>, grid, dim3(kFewThreads), 0, stream, a);
   else
     launch_kernel(attention_kernel<DT, KIND, D, NR, false>, grid, dim3(kFewThreads), 0, stream, a);

@@ -6,15 +6,17 @@
 // and O^T = V^T P^T put a query row on a column, so a lane keeps the statistics of its own row, and the weights leave the first product in
 // the lanes in which the second takes them; the values' tokens lie in LDS in the order in which the weights' lanes hold them.
 // Two buffers: the next tile's loads are under way while this one is multiplied, and it is stored into the other buffer afterwards, so a
-// tile costs one barrier.  16-byte units are placed by an exclusive or with bits of their row, which keeps both the stores and the matrix
-// operands' loads free of bank conflicts.
+// tile costs one barrier.  16-byte units are placed by an exclusive or with bits of their row, which spreads both the stores and the matrix
+// operands' loads over the banks.
 //
-// Measured, 8 KV heads of 128, 32 query heads: a prompt of 8192, bf16: 668 to 700 us from card to card = 790 to 820 TFLOP/s (a plain product reaches 1200); 512 new
-// tokens after 32768, int8: 393 us = 705 TFLOP/s.
+// Measured, 8 KV heads of 128, 32 query heads: a prompt of 8192, bf16: 662 to 700 us from card to card = 790 to 830 TFLOP/s (a plain product reaches 1200), e4m3:
+// 730; 512 new tokens after 32768, int8: 396 us = 700 TFLOP/s, e4m3: 407.
 //
-// Bounds: per 64 tokens and 32 rows the matrix instructions take 1024 cycles of a SIMD, the softmax about 900 (512 of them exponentials), the
-// operands 32 KiB of LDS reads of a wave (4 waves: what LDS delivers in 1024 cycles).  Two blocks a compute unit let one's softmax run
-// under the other's products.
+// What bounds it, by counters over the prompt: 64 tokens and 32 rows take 2890 cycles of a SIMD, where its matrix instructions are busy for 1024 of them (35 %), other
+// vector instructions for some 1080 (37 %; 512 of them exponentials), and LDS for 1070 (37 %, a quarter of it bank conflicts) for the four
+// SIMDs' pieces.  No unit is full: with two blocks a compute unit, which is what registers allow, the three take turns more than they overlap.  512 after
+// 32768, int8: matrix 29 %, all vector instructions 47 % (codes are widened), LDS 33 %.  Registers: 224 to 256 with 128 channels; e4m3 over pages that are no
+// multiple of 16 tokens spills 7 to 9 there.
 #include "kvh_attention.hpp"
 
 namespace kvh {
