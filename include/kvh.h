@@ -402,7 +402,7 @@ typedef struct {
  * (NULL: none), with q_heads heads of head_dim, are rotated into q_out, which may be q itself.  kv: k, v [layers][n_tokens][c].
  * rotation NULL: nothing is rotated, q is copied.
  * 16 bits: the value rounded to the nearest (what is not rotated is stored as it is).
- * 8 bits, for K and V of each page and KV head apart: a = the largest |x| among the new tokens on the page;
+ * 8 bits, for K and V of each page and KV head apart: a = the largest |x| among the new tokens stored on the page;
  * t = a < 2^-100 ? 0 : a * (1 / 127) (e4m3: a * (1 / 448); the reciprocal rounded to fp32); the scale becomes s = max(t, the scale it had), or t where no earlier token is on
  * the page (what was stored there before is of no account); code = rne(x * (1 / s)), 0 where s is 0.  Where s grew from s0 > 0,
  * the codes that the page's earlier tokens have become rne(code * (s0 / s)): a page is always described by one scale, and every
