@@ -438,6 +438,102 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
                   const kvh_rows* out, int q_heads, float* lse_dev, float scale, int causal, int sink, int window,
                   void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream);
 
+/* ---- Attention over selected pages ---------------------------------------------------------------------
+ * A long request need not be read as a whole for every token: the pages of the cache carry bounds of their keys, a cheap score from
+ * these says which pages a token's queries may find large products on, and attention reads those only.  Three calls:
+ * kvh_bound_keys after an append, kvh_select_pages for the new tokens' queries, kvh_attention_pages over what it chose.
+ *
+ * Bounds: for each page, KV head and channel the lowest and the highest key, as int8 codes rounded outwards with one fp32 scale
+ * per page and head.  With x the values of a 16-bit page (or the codes of an 8-bit one) over the page's tokens, a the largest |x| of the
+ * head: lowest = floor(127 min x / a), highest = ceil(127 max x / a), scale = a / 127 times the page's K scale, quotients in fp32; zeros
+ * where a < 2^-100.  A page and head that holds an infinity or NaN (its K scale among that) has codes of zero and a scale of NaN. */
+typedef struct {
+  int8_t* codes;  /* [layers][pages][heads][2][head_dim]: lowest, highest; 16-byte aligned, a page dense */
+  float* scale;   /* [layers][pages][heads], heads dense */
+  int64_t layer_stride, page_stride;             /* of the codes, multiples of 16 */
+  int64_t scale_layer_stride, scale_page_stride; /* floats */
+  int32_t layers, pages, block_tokens, heads, head_dim; /* as the cache has them */
+  int32_t reserved; /* 0 */
+} kvh_bounds;
+
+/* Computes the bounds of every page that new tokens lie on, all layers, from the tokens that the page holds (up to lens[b]; what lies behind
+ * them on the page is of no account), so that a call can be repeated.  The new tokens of request b are counted by starts as in kvh_append;
+ * requests->n_tokens only bounds them (INT32_MAX will do).  dt: the type of a 16-bit cache.  The cache's v and v_scale are not read, but are checked as
+ * everywhere (k and k_scale will do).  Pages and requests are refused as by kvh_append. */
+int kvh_bound_keys(const kvh_cache* cache, const kvh_requests* requests, kvh_dtype dt, const kvh_bounds* bounds, int32_t* status_dev, void* stream);
+
+/* The pages that each new token and KV head shall read.  The token at position p of a request chooses among its pages 0 .. p / block_tokens:
+ * the first `first` and the last `last` ones always, of the others those with the highest scores, `count` in all (or all there are);
+ * of equal scores the one that comes first.  With c_u = round(127 q_u / a_u) (half to even; a_u the largest |q_u|) for each query head u of the KV head:
+ *   score = fl(max_u fl(a_u sum_d max(c_ud lowest_d, c_ud highest_d)) * scale), fl rounding to fp32; the sum is a whole number below 2^24.
+ * It bounds the dot products of the queries' codes with every key of the page.  Heads u whose queries are not all finite, or all below 2^-100,
+ * count as zeros; a score that is no number, and that of a page whose scale is no finite one, as plus infinity.  The same inputs give the same pages,
+ * however a call is laid out.
+ * pages_dev: int32 [n_tokens][heads][count], dense: logical pages, ascending, then -1.  first >= 0, last >= 1, first + last <= count <= 4096.
+ * A page outside [0, pages) in the table is not chosen (status_dev).  Rows of refused requests, and rows of no request, are left as they are; a token at a
+ * position below 0 gets -1 throughout.
+ * workspace_dev: scores, 16-byte aligned; kvh_select_workspace says how much serves best (64 MiB at most, where a token's own scores do not take more); with less the
+ * call takes the tokens in turns.  KVH_E_SIZE where it does not hold one token's scores (4 heads table_pages bytes, rounded up to 16).  It needs no preparation and keeps
+ * nothing that another call reads. */
+size_t kvh_select_workspace(int n_requests, int n_tokens, int heads, int table_pages);
+int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q, int q_heads, int first, int last,
+                     int count, int32_t* pages_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream);
+
+/* Attention of the new tokens over the pages listed for each of them and each KV head: kvh_attention with causal set, where query i of head h sees only tokens on pages
+ * of its list, up to its own position.  pages_dev: int32 [n_tokens][heads][count], dense, count 1 .. 4096: logical pages, ascending, -1 past the last
+ * one; a list ends at its first negative entry.  An entry that is not larger than the one before it, or past the token's own page, ends its list too, with status_dev.
+ * Types, precision, lse, refusals, infinities and NaN: as kvh_attention.  count * block_tokens is at most 2^31 - 128.
+ * workspace_dev: partial results where few tokens read many pages, as for kvh_attention; kvh_attention_pages_workspace says how much serves best, less or none is
+ * slower where it is used. */
+size_t kvh_attention_pages_workspace(int n_tokens, int heads, int q_heads, int head_dim, int block_tokens, int count);
+int kvh_attention_pages(const kvh_cache* cache, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q, const kvh_rows* out, int q_heads,
+                        const int32_t* pages_dev, int count, float* lse_dev, float scale, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev,
+                        void* stream);
+
+/* ---- Pages ------------------------------------------------------------------------------------------------
+ * Who holds which page, on the device, so that a loop that reorders, forks and ends requests needs no host.  Requests are rows of the page table:
+ * row b holds ceil(lens[b] / block_tokens) pages.  refs[page] (int32) says how many rows hold a page (and holders besides the rows, which a program may count in it);
+ * a page with 0 is free.  All arrays are device memory, which the host cannot vet: entries outside [0, pages) are never accessed.  Outputs must not
+ * overlap inputs.  bounds (nullable) go along with their pages. */
+#define KVH_DEV_NO_PAGES 3
+
+/* Copies page src[i] to page dst[i], i < n: K, V, scales and bounds of all layers.  A pair with src[i] < 0 is skipped, and src[i] == dst[i] copies nothing; another with an
+ * entry outside [0, pages) is refused (status_dev[i], if not NULL: KVH_DEV_BAD_REQUEST).  A page that is the destination of two pairs, or of one and the source of another, has
+ * unspecified contents afterwards.  dt does not matter: a 16-bit cache is copied as it is.  n <= 2^24; 0: nothing is done. */
+int kvh_copy_pages(const kvh_cache* cache, const kvh_bounds* bounds, const int32_t* src_dev, const int32_t* dst_dev, int n, int32_t* status_dev, void* stream);
+
+/* The rows of a page table, before and after a call.  Host struct holding device pointers. */
+typedef struct {
+  const int32_t* table;  /* [n_requests][table_pages]; entries past a row's pages are not read */
+  int32_t* table_out;    /* the same shape; entries past a row's pages become -1 */
+  int64_t table_stride, table_out_stride;
+  const int32_t* lens;   /* n_requests */
+  const int32_t* refs;   /* pages */
+  int32_t* refs_out;
+  int32_t table_pages, n_requests; /* the latter 1 .. 65535 */
+} kvh_rows_of_pages;
+
+/* Fork: row b becomes a child of row a = parents[b] and grows by grow[b] tokens: lens_out[b] = lens[a] + grow[b].  parents NULL: every row is its own child;
+ * parents[b] < 0: of none, an empty row.  grow NULL: zeros.  A step's growth, beams that are reordered, samples of one prompt, requests that begin and end are
+ * one call of this.  The full pages of lens[a] tokens are shared.  A page that they do not fill stays with the first of a's children; the others get a
+ * copy of it (all layers, scales, bounds) on a fresh page, so that each row appends to a page of its own: such a page must be in no other row before the call.
+ * Fresh pages are those that no row holds afterwards and nothing else does, lowest numbers first, handed to the rows in order; refs_out counts what rows hold after the
+ * call in place of what they held before it.  A page that is given up and one that is handed out may be the same: the old rows are of no use afterwards.
+ * Refused rows become empty (lens_out 0): KVH_DEV_BAD_REQUEST for parents[b] >= n_requests, grow[b] < 0, a parent's length below 0 or past the
+ * table, an entry of its outside [0, pages), a new length past the table or 2^31 - 128; KVH_DEV_NO_PAGES where the fresh pages that rows up to this one need are more than there are.
+ * workspace_dev: kvh_fork_workspace bytes, 4-byte aligned; KVH_E_SIZE with less. */
+size_t kvh_fork_workspace(int n_requests, int pages);
+int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, const int32_t* parents_dev, const int32_t* grow_dev,
+             int32_t* lens_out_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream);
+
+/* Compact: with U pages in use (refs > 0), those numbered U or more move, in order, to the free numbers below U, in order; all others stay.  table_out and
+ * refs_out are the table and counts with the new numbers, moved_out[page] (int32, one a page) the new number of each page in use and -1 for free ones, for what else holds
+ * pages.  lens stay as they are.  An entry outside [0, pages), or of a page that is not in use, becomes -1, a row with a length below 0 or past the table empty (status_dev of the row:
+ * KVH_DEV_BAD_REQUEST).  workspace_dev: kvh_compact_workspace bytes, 4-byte aligned; KVH_E_SIZE with less. */
+size_t kvh_compact_workspace(int pages);
+int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, int32_t* moved_out_dev, void* workspace_dev,
+                size_t workspace_bytes, int32_t* status_dev, void* stream);
+
 /* ---- Storage policy (host only; no device work) -------------------------------------------------------
  * The paper's policy optimizer (Design section): Utility(i) = Freq(i) * (alpha * Quality(i, M_i, R_i) -
  * size(i, M_i, R_i) / Bandwidth); the marginal utility drop of going from rate m to rate n is

@@ -48,6 +48,17 @@ class _Rotation(ctypes.Structure):
                 ("n_positions", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32)]
 
 
+class _Bounds(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("scale_layer_stride", ctypes.c_int64), ("scale_page_stride", ctypes.c_int64), ("layers", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("block_tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _RowsOfPages(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("table_out_stride", ctypes.c_int64),
+                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("refs_out", ctypes.c_void_p), ("table_pages", ctypes.c_int32), ("n_requests", ctypes.c_int32)]
+
+
 # Device-resident job descriptors, built as structured numpy arrays and uploaded by the caller.
 ENC_ITEM = np.dtype([("blob", "<u8"), ("src_token0", "<i8"), ("n_tokens", "<i4"), ("level", "<i4")], align=True)
 DEC_ITEM = np.dtype([("blob", "<u8"), ("n_tokens", "<i4"), ("level", "<i4"), ("dst_token0", "<i8"),
@@ -130,6 +141,27 @@ def lib() -> ctypes.CDLL:
         L.kvh_attention_workspace.argtypes = [i32] * 6
         L.kvh_attention.restype = i32
         L.kvh_attention.argtypes = [cache, i32, requests, i32, rows, rows, i32, vp, ctypes.c_float, i32, i32, i32, vp, sz, vp, vp]
+        bounds, held = ctypes.POINTER(_Bounds), ctypes.POINTER(_RowsOfPages)
+        L.kvh_bound_keys.restype = i32
+        L.kvh_bound_keys.argtypes = [cache, requests, i32, bounds, vp, vp]
+        L.kvh_select_workspace.restype = sz
+        L.kvh_select_workspace.argtypes = [i32] * 4
+        L.kvh_select_pages.restype = i32
+        L.kvh_select_pages.argtypes = [bounds, i32, requests, i32, rows, i32, i32, i32, i32, vp, vp, sz, vp, vp]
+        L.kvh_attention_pages_workspace.restype = sz
+        L.kvh_attention_pages_workspace.argtypes = [i32] * 6
+        L.kvh_attention_pages.restype = i32
+        L.kvh_attention_pages.argtypes = [cache, i32, requests, i32, rows, rows, i32, vp, i32, vp, ctypes.c_float, vp, sz, vp, vp]
+        L.kvh_copy_pages.restype = i32
+        L.kvh_copy_pages.argtypes = [cache, bounds, vp, vp, i32, vp, vp]
+        L.kvh_fork_workspace.restype = sz
+        L.kvh_fork_workspace.argtypes = [i32, i32]
+        L.kvh_fork.restype = i32
+        L.kvh_fork.argtypes = [cache, bounds, held, vp, vp, vp, vp, sz, vp, vp]
+        L.kvh_compact_workspace.restype = sz
+        L.kvh_compact_workspace.argtypes = [i32]
+        L.kvh_compact.restype = i32
+        L.kvh_compact.argtypes = [cache, bounds, held, vp, vp, sz, vp, vp]
         f64 = ctypes.c_double
         L.kvh_policy_utility.restype = f64
         L.kvh_policy_utility.argtypes = [f64] * 5
@@ -745,6 +777,214 @@ def attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lay
                                head_dim ** -0.5 if scale is None else scale, int(causal), sink, window, workspace.data_ptr(), workspace.numel(), _ptr(status),
                                _stream_ptr(stream)), "kvh_attention")
     return out
+
+
+# ---- attention over selected pages ----------------------------------------------------------------------------------
+def _here(*tensors):
+    """These calls run on the current device, on memory of its own."""
+    _require_cuda(*tensors)
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("all tensors must be on the current device")
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _bounds(codes, scale, block_tokens):
+    """kvh_bounds of int8 [l][P][heads][2][head_dim] and float32 [l][P][heads]."""
+    if codes is None and scale is None:
+        return None
+    _here(codes, scale)
+    if codes is None or codes.dtype != torch.int8 or codes.dim() != 5 or codes.shape[3] != 2:
+        raise ValueError("bounds must be int8 [l][P][heads][2][head_dim]")
+    l, pages, heads, _, dim = codes.shape
+    if _step(codes, 4, 1) != 1 or codes.stride(3) != dim or _step(codes, 2, 2 * dim) != 2 * dim:
+        raise ValueError("the bounds of a page must be dense")
+    if scale is None or scale.dtype != torch.float32 or scale.shape != (l, pages, heads) or _step(scale, 2, 1) != 1:
+        raise ValueError("the bounds need float32 scales [l][P][heads], dense in the heads")
+    return _Bounds(codes.data_ptr(), scale.data_ptr(), _step(codes, 0, 0), _step(codes, 1, 2 * heads * dim), _step(scale, 0, 0), _step(scale, 1, heads),
+                   l, pages, block_tokens, heads, dim, 0)
+
+
+def _space(workspace, size, device, stream):
+    """The caller's workspace, or one of `size` bytes."""
+    if workspace is None:
+        return _empty(size, torch.uint8, device, stream)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a dense uint8 tensor")
+    _here(workspace)
+    return workspace
+
+
+def bound_keys(k_cache: torch.Tensor, bounds: torch.Tensor, bound_scale: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor,
+               max_new: int, k_scale: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None) -> None:
+    """kvh_bound_keys: the bounds, int8 [l][P][heads][2][head_dim] and float32 [l][P][heads], of the pages that the requests' new tokens lie on,
+    from a K cache [l][P][block][c] (16-bit, int8 or float8_e4m3fn with scales [l][P][heads])."""
+    _here(k_cache, k_scale, starts, lens, page_table, status)
+    if bounds.dim() != 5:
+        raise ValueError("bounds must be int8 [l][P][heads][2][head_dim]")
+    dt = k_cache.dtype if k_cache.dtype in _TORCH_DT else torch.float16
+    cache = _cache(k_cache, k_cache, k_scale, k_scale, bounds.shape[4], dt)
+    to = _bounds(bounds, bound_scale, cache.block_tokens)
+    req = _requests(starts, lens, page_table, max_new, 2 ** 31 - 1, status)
+    _check(lib().kvh_bound_keys(ctypes.byref(cache), ctypes.byref(req), _TORCH_DT[dt], ctypes.byref(to), _ptr(status), _stream_ptr(stream)), "kvh_bound_keys")
+
+
+def select_workspace(n_requests: int, n_tokens: int, heads: int, table_pages: int) -> int:
+    """kvh_select_workspace: bytes that serve such a batch best."""
+    return lib().kvh_select_workspace(n_requests, n_tokens, heads, table_pages)
+
+
+def select_pages(q: torch.Tensor, bounds: torch.Tensor, bound_scale: torch.Tensor, layer: int, starts: torch.Tensor, lens: torch.Tensor,
+                 page_table: torch.Tensor, max_new: int, count: int, block_tokens: int = 16, first: int = 1, last: int = 1, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """kvh_select_pages: for queries [T][q_heads * head_dim] the `count` pages of each new token and KV head, int32 [T][heads][count]: logical pages, ascending,
+    then -1.  workspace: uint8, kept by programs that call often (see select_workspace); made here if none is given."""
+    _here(q, starts, lens, page_table, out, status)
+    if q.dtype not in _TORCH_DT or q.dim() != 2:
+        raise ValueError("q must be float16 or bfloat16 [T][q_heads * head_dim]")
+    box = _bounds(bounds, bound_scale, block_tokens)
+    if box is None:
+        raise ValueError("bounds must be int8 [l][P][heads][2][head_dim]")
+    T = q.shape[0]
+    rows, q_heads = _rows(q.unsqueeze(0), 1, T, box.head_dim, q.dtype, "q")
+    req = _requests(starts, lens, page_table, max_new, T, status)
+    if out is None:
+        out = _empty((T, box.heads, count), torch.int32, q.device, stream)
+    elif out.dtype != torch.int32 or out.shape != (T, box.heads, count) or not out.is_contiguous():
+        raise ValueError("out must be a dense int32 [T][heads][count]")
+    workspace = _space(workspace, select_workspace(req.n_requests, T, box.heads, req.table_pages), q.device, stream)
+    _check(lib().kvh_select_pages(ctypes.byref(box), layer, ctypes.byref(req), _TORCH_DT[q.dtype], ctypes.byref(rows), q_heads, first, last, count, out.data_ptr(),
+                                  workspace.data_ptr(), workspace.numel(), _ptr(status), _stream_ptr(stream)), "kvh_select_pages")
+    return out
+
+
+def attention_pages_workspace(n_tokens: int, heads: int, q_heads: int, head_dim: int, block_tokens: int, count: int) -> int:
+    """kvh_attention_pages_workspace: bytes that serve such a batch best; 0 where it is never split."""
+    return lib().kvh_attention_pages_workspace(n_tokens, heads, q_heads, head_dim, block_tokens, count)
+
+
+def attention_pages(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, layer: int, pages: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+                    page_table: torch.Tensor, max_new: int, head_dim: int = 128, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None,
+                    scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                    status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """kvh_attention_pages: queries [T][q_heads * head_dim] of the requests' new tokens over the pages listed for each of them and each KV head (int32
+    [T][heads][count], as select_pages gives them) of layer `layer` of the cache.  Otherwise as attention."""
+    _here(q, k_cache, v_cache, k_scale, v_scale, pages, starts, lens, page_table, out, lse, status)
+    if q.dtype not in _TORCH_DT or q.dim() != 2:
+        raise ValueError("q must be float16 or bfloat16 [T][q_heads * head_dim]")
+    cache = _cache(k_cache, v_cache, k_scale, v_scale, head_dim, q.dtype)
+    T = q.shape[0]
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    rows, q_heads = _rows(q.unsqueeze(0), 1, T, head_dim, q.dtype, "q")
+    to, out_heads = _rows(out.unsqueeze(0), 1, T, head_dim, q.dtype, "out")
+    if out_heads != q_heads:
+        raise ValueError("out must have the shape of q")
+    if pages.dtype != torch.int32 or pages.dim() != 3 or pages.shape[:2] != (T, cache.heads) or not pages.is_contiguous():
+        raise ValueError("pages must be a dense int32 [T][heads][count]")
+    req = _requests(starts, lens, page_table, max_new, T, status)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (T, q_heads) or not lse.is_contiguous()):
+        raise ValueError("lse must be a dense float32 [T][q_heads]")
+    count = pages.shape[2]
+    workspace = _space(workspace, attention_pages_workspace(T, cache.heads, q_heads, head_dim, cache.block_tokens, count), q.device, stream)
+    _check(lib().kvh_attention_pages(ctypes.byref(cache), layer, ctypes.byref(req), _TORCH_DT[q.dtype], ctypes.byref(rows), ctypes.byref(to), q_heads,
+                                     pages.data_ptr(), count, _ptr(lse), head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel(),
+                                     _ptr(status), _stream_ptr(stream)), "kvh_attention_pages")
+    return out
+
+
+# ---- pages ------------------------------------------------------------------------------------------------------------
+def _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim):
+    """kvh_cache of a cache whose 16-bit type does not matter."""
+    _here(k_cache, v_cache, k_scale, v_scale)
+    return _cache(k_cache, v_cache, k_scale, v_scale, head_dim, k_cache.dtype if k_cache.dtype in _TORCH_DT else torch.float16)
+
+
+def copy_pages(k_cache: torch.Tensor, v_cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, head_dim: int = 128, k_scale: torch.Tensor | None = None,
+               v_scale: torch.Tensor | None = None, bounds: torch.Tensor | None = None, bound_scale: torch.Tensor | None = None,
+               status: torch.Tensor | None = None, stream=None) -> None:
+    """kvh_copy_pages: page src[i] of all layers to page dst[i] (int32), with scales and bounds; src[i] < 0: none."""
+    cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
+    box = _bounds(bounds, bound_scale, cache.block_tokens)
+    _here(src, dst, status)
+    _int32(src, "src", 1)
+    _int32(dst, "dst", 1)
+    if src.shape != dst.shape:
+        raise ValueError("src and dst must have as many entries")
+    _int32(status, "status", 1, src.shape[0])
+    _check(lib().kvh_copy_pages(ctypes.byref(cache), _ref(box), src.data_ptr(), dst.data_ptr(), src.shape[0], _ptr(status), _stream_ptr(stream)), "kvh_copy_pages")
+
+
+def _held(page_table, table_out, lens, refs, refs_out, pages, stream):
+    """kvh_rows_of_pages, and its outputs, made here if none are given."""
+    _here(page_table, table_out, lens, refs, refs_out)
+    n = lens.shape[0]
+    _int32(lens, "lens", 1)
+    _int32(page_table, "page_table", 2, n)
+    _int32(refs, "refs", 1)
+    if refs.shape[0] != pages or page_table.shape[0] != n:
+        raise ValueError("page_table must be [n][table_pages] and refs [P]")
+    table_out = _empty(page_table.shape, torch.int32, page_table.device, stream) if table_out is None else table_out
+    refs_out = _empty(refs.shape, torch.int32, refs.device, stream) if refs_out is None else refs_out
+    _int32(table_out, "table_out", 2)
+    _int32(refs_out, "refs_out", 1)
+    if table_out.shape != page_table.shape or refs_out.shape != refs.shape:
+        raise ValueError("table_out and refs_out must have the shapes of page_table and refs")
+    w = page_table.shape[1]
+    return _RowsOfPages(page_table.data_ptr(), table_out.data_ptr(), _step(page_table, 0, w), _step(table_out, 0, w), lens.data_ptr(), refs.data_ptr(),
+                        refs_out.data_ptr(), w, n), table_out, refs_out
+
+
+def fork_workspace(n_requests: int, pages: int) -> int:
+    """kvh_fork_workspace: bytes that such a call needs."""
+    return lib().kvh_fork_workspace(n_requests, pages)
+
+
+def fork(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, parents: torch.Tensor | None = None,
+         grow: torch.Tensor | None = None, head_dim: int = 128, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None,
+         bounds: torch.Tensor | None = None, bound_scale: torch.Tensor | None = None, table_out: torch.Tensor | None = None,
+         lens_out: torch.Tensor | None = None, refs_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+         status: torch.Tensor | None = None, stream=None):
+    """kvh_fork: row b of the page table becomes a child of row parents[b] (negative: none; not given: its own) and grows by grow[b] tokens.  refs: int32 [P], how
+    many rows hold a page.  -> (page_table, lens, refs) after it, in the given outputs or new ones; they must not overlap the inputs."""
+    cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
+    box = _bounds(bounds, bound_scale, cache.block_tokens)
+    rows, table_out, refs_out = _held(page_table, table_out, lens, refs, refs_out, cache.pages, stream)
+    n = rows.n_requests
+    _here(parents, grow, lens_out, status)
+    lens_out = _empty(lens.shape, torch.int32, lens.device, stream) if lens_out is None else lens_out
+    for t, name in ((parents, "parents"), (grow, "grow"), (lens_out, "lens_out"), (status, "status")):
+        _int32(t, name, 1, n)
+    workspace = _space(workspace, fork_workspace(n, cache.pages), lens.device, stream)
+    _check(lib().kvh_fork(ctypes.byref(cache), _ref(box), ctypes.byref(rows), _ptr(parents), _ptr(grow), lens_out.data_ptr(), workspace.data_ptr(),
+                          workspace.numel(), _ptr(status), _stream_ptr(stream)), "kvh_fork")
+    return table_out, lens_out, refs_out
+
+
+def compact_workspace(pages: int) -> int:
+    """kvh_compact_workspace: bytes that such a call needs."""
+    return lib().kvh_compact_workspace(pages)
+
+
+def compact(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, head_dim: int = 128,
+            k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None, bounds: torch.Tensor | None = None,
+            bound_scale: torch.Tensor | None = None, table_out: torch.Tensor | None = None, refs_out: torch.Tensor | None = None,
+            moved_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """kvh_compact: the pages in use move to the lowest numbers.  -> (page_table, refs, moved) after it: moved[page] is a page's new number, -1 where it is free."""
+    cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
+    box = _bounds(bounds, bound_scale, cache.block_tokens)
+    rows, table_out, refs_out = _held(page_table, table_out, lens, refs, refs_out, cache.pages, stream)
+    _here(moved_out, status)
+    moved_out = _empty(refs.shape, torch.int32, refs.device, stream) if moved_out is None else moved_out
+    _int32(moved_out, "moved_out", 1, cache.pages)
+    _int32(status, "status", 1, rows.n_requests)
+    workspace = _space(workspace, compact_workspace(cache.pages), lens.device, stream)
+    _check(lib().kvh_compact(ctypes.byref(cache), _ref(box), ctypes.byref(rows), moved_out.data_ptr(), workspace.data_ptr(), workspace.numel(), _ptr(status),
+                             _stream_ptr(stream)), "kvh_compact")
+    return table_out, refs_out, moved_out
 
 
 def policy_utility(freq: float, alpha: float, quality: float, size_bytes: float, bandwidth: float) -> float:

@@ -223,13 +223,6 @@ struct Items {
   }
 };
 
-// Says which requests are refused; the kernels pass over them.
-__device__ __forceinline__ void tell_refused(const AttnParams& a) {
-  if (blockIdx.x != 0 || a.status == nullptr) return;
-  for (int b = threadIdx.x; b < a.req.n; b += kBlockThreads)
-    if (!request_ok(a.req, a.req.starts[b], a.req.starts[b + 1], a.req.lens[b])) a.status[b] = KVH_DEV_BAD_REQUEST;
-}
-
 // ---- operands -----------------------------------------------------------------------------------------------------
 template <int DT, int KIND>
 constexpr bool kBf16 = KIND == KVH_CACHE_16 && DT == KVH_BF16;  // the products' type; fp16 otherwise
@@ -376,22 +369,6 @@ struct Steps {
     end = it.last || it.from + it.count > count ? count : it.from + it.count;
   }
 };
-
-// Whether a word of values holds an infinity or NaN.
-template <int DT, int KIND>
-__device__ __forceinline__ bool has_odd(uint32_t w) {
-  if constexpr (KIND == KVH_CACHE_E4M3) {
-    bool odd = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) odd |= (w >> 8 * e & 0x7fu) == 0x7fu;
-    return odd;
-  } else if constexpr (KIND == KVH_CACHE_16) {
-    constexpr uint32_t kExp = DT == KVH_BF16 ? 0x7f80u : 0x7c00u;
-    return (w & kExp) == kExp || (w >> 16 & kExp) == kExp;
-  } else {
-    return false;
-  }
-}
 
 // Operands of the second product where it holds an infinity or NaN that some rows do not see.  A weight of zero does not keep these from a row,
 // so they are taken out of the product, and what they do to the rows that see them comes from products of ones: where (ones of the tokens

@@ -52,6 +52,23 @@ inline int check_rows(const kvh_rows* r, int64_t channels, int n_tokens) {
   return KVH_OK;
 }
 
+inline int check_bounds(const kvh_bounds* b) {
+  if (b == nullptr || b->codes == nullptr || b->scale == nullptr) return KVH_E_ARG;
+  if (b->head_dim != 64 && b->head_dim != 128) return KVH_E_SHAPE;
+  if (b->layers < 1 || b->layers > 32767 || b->pages < 1 || b->heads < 1 || b->heads > 4096) return KVH_E_SHAPE;
+  if (b->block_tokens < 1) return KVH_E_ARG;
+  if (b->layer_stride < 0 || b->page_stride < (int64_t)b->heads * 2 * b->head_dim || b->scale_layer_stride < 0 || b->scale_page_stride < b->heads) return KVH_E_ARG;
+  if (!is_aligned16(b->codes) || b->layer_stride % 16 != 0 || b->page_stride % 16 != 0 || (reinterpret_cast<uintptr_t>(b->scale) & 3u) != 0) return KVH_E_ALIGN;
+  return KVH_OK;
+}
+// Whether the bounds are those of such a cache.
+inline int check_bounds_of(const kvh_bounds* b, const kvh_cache* c) {
+  if (int rc = check_bounds(b)) return rc;
+  return b->layers == c->layers && b->pages == c->pages && b->block_tokens == c->block_tokens && b->heads == c->heads && b->head_dim == c->head_dim ? KVH_OK : KVH_E_SHAPE;
+}
+
+inline bool heads_fit(int heads, int q_heads) { return heads >= 1 && q_heads >= heads && q_heads % heads == 0 && q_heads <= 65536; }
+
 // The requests as the kernels see them.
 struct Requests {
   const int32_t* starts;
@@ -74,6 +91,48 @@ struct Request {
 // Whether a request is one that the call can serve: see include/kvh.h.
 __device__ __forceinline__ bool request_ok(const Requests& r, int32_t start, int32_t end, int32_t len) {
   return start >= 0 && end >= start && end <= r.n_tokens && end - start <= r.max_new && len >= 0 && len <= r.capacity;
+}
+
+// The request that a row of the packed tensors belongs to; all lanes of a wave ask for the same row.  False where it is in none, or in one that is refused.
+__device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
+  int first = 0, many = r.n;  // the last start that is not past the row is one of these
+  while (many > 1) {
+    const int step = (many + kWave - 1) / kWave, at = lane * step;
+    const uint64_t below = __ballot(at < many && r.starts[first + at] <= row);
+    const int k = below == 0 ? 0 : 63 - __builtin_clzll(below);
+    first += k * step;
+    many = many - k * step < step ? many - k * step : step;
+  }
+  b = uniform(first);
+  rq.start = uniform(r.starts[b]);
+  const int32_t end = uniform(r.starts[b + 1]);
+  rq.len = uniform(r.lens[b]);
+  rq.n = end - rq.start;
+  rq.ok = request_ok(r, rq.start, end, rq.len) && rq.start <= row && row < end;
+  return rq.ok;
+}
+
+// Says which requests are refused; the kernels pass over them.
+__device__ __forceinline__ void tell_refused(const Requests& r, int32_t* status) {
+  if (blockIdx.x != 0 || status == nullptr) return;
+  for (int b = threadIdx.x; b < r.n; b += kBlockThreads)
+    if (!request_ok(r, r.starts[b], r.starts[b + 1], r.lens[b])) status[b] = KVH_DEV_BAD_REQUEST;
+}
+
+// Whether a word of values holds an infinity or NaN.
+template <int DT, int KIND>
+__device__ __forceinline__ bool has_odd(uint32_t w) {
+  if constexpr (KIND == KVH_CACHE_E4M3) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= (w >> 8 * e & 0x7fu) == 0x7fu;
+    return odd;
+  } else if constexpr (KIND == KVH_CACHE_16) {
+    constexpr uint32_t kExp = DT == KVH_BF16 ? 0x7f80u : 0x7c00u;
+    return (w & kExp) == kExp || (w >> 16 & kExp) == kExp;
+  } else {
+    return false;
+  }
 }
 
 // 8 values of 16 bits <-> fp32.

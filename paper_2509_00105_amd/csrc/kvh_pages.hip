@@ -1,0 +1,421 @@
+// kvh_copy_pages, kvh_fork, kvh_compact: pages of the serving cache change hands.
+//
+// Contents move by one copy kernel over pairs of pages; memory bounds it.  Who holds what is integer work on the table and the counts, in a few small
+// launches, which their latency bounds.  Counts change by atomic additions of whole numbers, whose order is of no account.
+#include "kvh_cache.hpp"
+
+#include <algorithm>
+
+namespace kvh {
+namespace {
+
+// ---- copying ------------------------------------------------------------------------------------------------------
+struct CopyParams {
+  const int32_t *src, *dst;
+  int32_t* status;
+  uint8_t *ck, *cv;
+  float *sk, *sv;
+  int8_t* codes;   // of the bounds, or nullptr
+  float* b_scale;
+  int64_t c_ls, c_ts, s_ls, s_ps, b_ls, b_ps, bs_ls, bs_ps;  // cache and bounds' codes in bytes, scales in floats
+  int pages, block_tokens, heads, box;  // box: 16-byte words of a page's bounds
+  uint32_t row_words, words;  // 16-byte words of a row, and of a page
+  uint32_t parts;             // blocks of a page and layer: those of K, those of V, one for the rest
+  uint32_t layers;
+  Divisor by_parts, by_layers, by_row;
+};
+
+constexpr int kCopyWords = 4;  // 16-byte words of a thread
+
+__global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) {
+  const uint32_t unit = a.by_parts.quotient(blockIdx.x), part = blockIdx.x - unit * a.parts;
+  const uint32_t i = a.by_layers.quotient(unit), layer = unit - i * a.layers;
+  const int src = a.src[i], dst = a.dst[i];
+  if (src < 0 || src == dst) return;
+  if (src >= a.pages || dst < 0 || dst >= a.pages) {
+    if (threadIdx.x == 0 && part == 0 && layer == 0 && a.status != nullptr) a.status[i] = KVH_DEV_BAD_REQUEST;
+    return;
+  }
+  const uint32_t half = (a.parts - 1) / 2;
+  if (part < 2 * half) {
+    uint8_t* base = (part < half ? a.ck : a.cv) + layer * a.c_ls;
+    const uint32_t w0 = (part < half ? part : part - half) * (kBlockThreads * kCopyWords) + threadIdx.x;
+    const uint8_t* from = base + (int64_t)src * a.block_tokens * a.c_ts;
+    uint8_t* to = base + (int64_t)dst * a.block_tokens * a.c_ts;
+    u32x4 x[kCopyWords];
+    int64_t at[kCopyWords];
+#pragma unroll
+    for (int e = 0; e < kCopyWords; ++e) {
+      const uint32_t w = w0 + e * kBlockThreads, row = a.by_row.quotient(w);
+      at[e] = row * a.c_ts + (int64_t)(w - row * a.row_words) * 16;
+      if (w < a.words) x[e] = *reinterpret_cast<const u32x4*>(from + at[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < kCopyWords; ++e)
+      if (w0 + e * kBlockThreads < a.words) *reinterpret_cast<u32x4*>(to + at[e]) = x[e];
+    return;
+  }
+  for (int h = threadIdx.x; h < a.heads; h += kBlockThreads) {
+    if (a.sk != nullptr) {
+      float *k = a.sk + layer * a.s_ls + h, *v = a.sv + layer * a.s_ls + h;
+      k[dst * a.s_ps] = k[src * a.s_ps];
+      v[dst * a.s_ps] = v[src * a.s_ps];
+    }
+    if (a.b_scale != nullptr) {
+      float* s = a.b_scale + layer * a.bs_ls + h;
+      s[dst * a.bs_ps] = s[src * a.bs_ps];
+    }
+  }
+  if (a.codes != nullptr) {
+    int8_t* codes = a.codes + layer * a.b_ls;
+    for (int w = threadIdx.x; w < a.box; w += kBlockThreads)
+      *reinterpret_cast<u32x4*>(codes + dst * a.b_ps + (int64_t)w * 16) = *reinterpret_cast<const u32x4*>(codes + src * a.b_ps + (int64_t)w * 16);
+  }
+}
+
+// `pairs` of them at most; what bounds and scales there are goes along.
+int launch_copy(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int64_t pairs, int32_t* status, hipStream_t stream) {
+  CopyParams a{};
+  const int width = c.kind == KVH_CACHE_16 ? 2 : 1;
+  a.src = src, a.dst = dst, a.status = status;
+  a.ck = static_cast<uint8_t*>(c.k), a.cv = static_cast<uint8_t*>(c.v);
+  a.sk = c.k_scale, a.sv = c.v_scale;
+  a.c_ls = c.layer_stride * width, a.c_ts = c.token_stride * width, a.s_ls = c.scale_layer_stride, a.s_ps = c.scale_page_stride;
+  a.pages = c.pages, a.block_tokens = c.block_tokens, a.heads = c.heads;
+  if (b != nullptr) {
+    a.codes = b->codes, a.b_scale = b->scale;
+    a.b_ls = b->layer_stride, a.b_ps = b->page_stride, a.bs_ls = b->scale_layer_stride, a.bs_ps = b->scale_page_stride;
+    a.box = c.heads * 2 * c.head_dim / 16;
+  }
+  a.row_words = (uint32_t)(c.heads * c.head_dim * width / 16);
+  const int64_t words = (int64_t)a.row_words * c.block_tokens, half = (words + kBlockThreads * kCopyWords - 1) / (kBlockThreads * kCopyWords);
+  if (words >= (int64_t)1 << 30) return KVH_E_SHAPE;
+  a.words = (uint32_t)words;
+  a.parts = (uint32_t)(2 * half + 1);
+  a.layers = (uint32_t)c.layers;
+  a.by_parts = Divisor(a.parts), a.by_layers = Divisor(a.layers), a.by_row = Divisor(a.row_words);
+  const int64_t each = (int64_t)a.parts * a.layers, most = (((int64_t)1 << 31) - 1) / each;  // pairs of a launch
+  if (most < 1) return KVH_E_SHAPE;
+  for (int64_t i = 0; i < pairs; i += most) {
+    const int64_t n = std::min(most, pairs - i);
+    launch_kernel(copy_kernel, dim3((unsigned)(n * each)), dim3(kBlockThreads), 0, stream, a);
+    KVH_HIP_CHECK_LAUNCH();
+    a.src += n, a.dst += n;
+    if (a.status != nullptr) a.status += n;
+  }
+  return KVH_OK;
+}
+
+// ---- forking ------------------------------------------------------------------------------------------------------
+struct RowsParams {
+  const int32_t* table;
+  int32_t* table_out;
+  int64_t ts, to_ts;
+  const int32_t* lens;
+  const int32_t* refs;
+  int32_t* refs_out;
+  int table_pages, n, pages, block_tokens;
+  int64_t capacity;  // tokens that a row has pages for, and a request may have
+  int32_t* status;
+  Divisor by_block;
+};
+
+struct ForkParams {
+  RowsParams r;
+  const int32_t *parents, *grow;
+  int32_t* lens_out;
+  // workspace
+  int32_t *need, *base;  // of each row: fresh pages it needs; how many rows before it need, or -1 where it is refused
+  int32_t *src, *dst;    // pairs to copy
+  int32_t* fresh;        // free pages in order
+};
+
+__device__ __forceinline__ int pages_of(const RowsParams& r, int tokens) { return tokens > 0 ? (int)r.by_block.quotient((uint32_t)tokens - 1) + 1 : 0; }
+
+// What becomes of row b.
+struct Child {
+  int parent;       // -1: none
+  int old_len, len; // the parent's tokens, and the row's
+  int full, kept, after;  // pages that are shared, that are not fresh, and all
+  bool ok, copies;  // whether an unfilled page is copied
+};
+
+__global__ __launch_bounds__(kBlockThreads) void start_kernel(RowsParams r) {
+  const int p = blockIdx.x * kBlockThreads + threadIdx.x;
+  if (p < r.pages) r.refs_out[p] = r.refs[p];
+}
+
+// All threads of a block.  The lengths and the entries are checked, and whether the row is the first of its parent's children.
+__device__ __forceinline__ Child child_of(const ForkParams& a, int b) {
+  const RowsParams& r = a.r;
+  Child c;
+  c.parent = a.parents == nullptr ? b : a.parents[b];
+  if (c.parent < 0) c.parent = -1;
+  const int64_t grow = a.grow == nullptr ? 0 : a.grow[b];
+  c.ok = c.parent < r.n && grow >= 0;
+  c.old_len = c.ok && c.parent >= 0 ? r.lens[c.parent] : 0;
+  c.ok = c.ok && c.old_len >= 0 && c.old_len + grow <= r.capacity;
+  if (!c.ok) c.old_len = 0;
+  c.len = c.ok ? (int)(c.old_len + grow) : 0;
+  c.full = (int)r.by_block.quotient((uint32_t)c.old_len);
+  const bool open = c.old_len - c.full * r.block_tokens != 0;
+  c.after = pages_of(r, c.len);
+  bool odd = false, other = false;
+  if (c.parent >= 0) {
+    const int32_t* from = r.table + (int64_t)c.parent * r.ts;
+    for (int j = threadIdx.x; j < c.full + open; j += kBlockThreads) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
+    if (open && a.parents != nullptr)
+      for (int i = threadIdx.x; i < b; i += kBlockThreads) other |= a.parents[i] == c.parent;
+  }
+  odd = __syncthreads_or(odd) != 0;
+  other = __syncthreads_or(other) != 0;
+  if (odd) c.ok = false;
+  if (!c.ok) c.len = c.full = c.after = 0;
+  c.copies = c.ok && open && other;
+  c.kept = c.full + (c.ok && open && !other);
+  return c;
+}
+
+__global__ __launch_bounds__(kBlockThreads) void count_kernel(ForkParams a) {
+  const RowsParams& r = a.r;
+  const int b = blockIdx.x;
+  const Child c = child_of(a, b);
+  const int32_t len = r.lens[b];
+  if (len > 0 && len <= r.capacity) {
+    const int32_t* old = r.table + (int64_t)b * r.ts;
+    for (int j = threadIdx.x; j < pages_of(r, len); j += kBlockThreads)
+      if ((uint32_t)old[j] < (uint32_t)r.pages) atomicSub(&r.refs_out[old[j]], 1);
+  }
+  if (c.parent >= 0) {
+    const int32_t* from = r.table + (int64_t)c.parent * r.ts;
+    for (int j = threadIdx.x; j < c.kept; j += kBlockThreads) atomicAdd(&r.refs_out[from[j]], 1);
+  }
+  if (threadIdx.x == 0) {
+    a.need[b] = c.after - c.kept;
+    if (!c.ok && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
+  }
+}
+
+constexpr int kScanThreads = 1024, kScanWaves = kScanThreads / kWave;
+
+// The sum of all threads' values before this one's, and of all; one block of kScanThreads.
+__device__ __forceinline__ int64_t before_me(int64_t v, int64_t* lds, int64_t& all) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int64_t x = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int64_t y = __shfl_up((long long)x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) lds[wave] = x;
+  __syncthreads();
+  int64_t base = 0;
+  all = 0;
+  for (int w = 0; w < kScanWaves; ++w) {
+    if (w == wave) base = all;
+    all += lds[w];
+  }
+  return base + x - v;
+}
+
+// The free pages in order, and each row's place among those that need some.
+__global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
+  __shared__ int64_t lds[kScanWaves];
+  const RowsParams& r = a.r;
+  int64_t many = 0;
+  for (int p0 = 0; p0 < r.pages; p0 += kScanThreads) {
+    const int p = p0 + threadIdx.x;
+    const bool free = p < r.pages && r.refs_out[p] == 0;
+    int64_t all;
+    const int64_t at = many + before_me(free, lds, all);
+    if (free) a.fresh[at] = p;
+    many += all;
+  }
+  int64_t wanted = 0;
+  for (int b0 = 0; b0 < r.n; b0 += kScanThreads) {
+    const int b = b0 + threadIdx.x;
+    const int need = b < r.n ? a.need[b] : 0;
+    int64_t all;
+    const int64_t at = wanted + before_me(need, lds, all);
+    if (b < r.n) a.base[b] = need == 0 ? 0 : at + need <= many ? (int32_t)at : -1;
+    wanted += all;
+  }
+}
+
+__global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a) {
+  const RowsParams& r = a.r;
+  const int b = blockIdx.x;
+  const Child c = child_of(a, b);
+  const int base = a.base[b];
+  const bool served = base >= 0;
+  const int32_t* from = r.table + (int64_t)(c.parent < 0 ? 0 : c.parent) * r.ts;
+  int32_t* to = r.table_out + (int64_t)b * r.to_ts;
+  for (int j = threadIdx.x; j < r.table_pages; j += kBlockThreads) {
+    int page = -1;
+    if (j < c.kept) {
+      page = from[j];
+      if (!served) {
+        atomicSub(&r.refs_out[page], 1);
+        page = -1;
+      }
+    } else if (j < c.after && served) {
+      page = a.fresh[base + j - c.kept];
+      r.refs_out[page] = 1;
+    }
+    to[j] = page;
+  }
+  if (threadIdx.x == 0) {
+    a.lens_out[b] = served ? c.len : 0;
+    if (!served && r.status != nullptr) r.status[b] = KVH_DEV_NO_PAGES;
+    const bool copies = served && c.copies;
+    a.src[b] = copies ? from[c.full] : -1;
+    a.dst[b] = copies ? a.fresh[base] : -1;
+  }
+}
+
+// ---- compacting ---------------------------------------------------------------------------------------------------
+struct CompactParams {
+  RowsParams r;
+  int32_t* moved;
+  int32_t *src, *dst;  // pairs to copy, pages / 2 of them at most
+};
+
+__global__ __launch_bounds__(kScanThreads) void place_kernel(CompactParams a) {
+  __shared__ int64_t lds[kScanWaves];
+  const RowsParams& r = a.r;
+  int64_t mine = 0, used;
+  for (int p = threadIdx.x; p < r.pages; p += kScanThreads) mine += r.refs[p] > 0;
+  before_me(mine, lds, used);
+  for (int i = threadIdx.x; i < r.pages / 2; i += kScanThreads) a.src[i] = a.dst[i] = -1;
+  __syncthreads();
+  int64_t holes = 0, strays = 0;  // free pages below `used` and pages in use above, so far: as many of both in the end
+  for (int p0 = 0; p0 < r.pages; p0 += kScanThreads) {
+    const int p = p0 + threadIdx.x;
+    const bool in_use = p < r.pages && r.refs[p] > 0;
+    const bool hole = p < used && !in_use, stray = p >= used && in_use;
+    int64_t all;
+    const int64_t at = before_me((int64_t)hole | (int64_t)stray << 32, lds, all);
+    if (hole) a.dst[holes + (at & 0xffffffff)] = p;
+    if (stray) a.src[strays + (at >> 32)] = p;
+    holes += all & 0xffffffff, strays += all >> 32;
+    if (p < r.pages) {
+      a.moved[p] = in_use ? p : -1;
+      r.refs_out[p] = in_use ? r.refs[p] : 0;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < strays; i += kScanThreads) {
+    const int src = a.src[i], dst = a.dst[i];
+    a.moved[src] = dst;
+    r.refs_out[dst] = r.refs[src];
+    r.refs_out[src] = 0;
+  }
+}
+
+__global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a) {
+  const RowsParams& r = a.r;
+  const int b = blockIdx.x;
+  const int32_t len = r.lens[b];
+  bool bad = len < 0 || len > r.capacity;
+  const int held = bad ? 0 : pages_of(r, len);
+  const int32_t* from = r.table + (int64_t)b * r.ts;
+  int32_t* to = r.table_out + (int64_t)b * r.to_ts;
+  for (int j = threadIdx.x; j < r.table_pages; j += kBlockThreads) {
+    int page = -1;
+    if (j < held) {
+      page = from[j];
+      page = (uint32_t)page < (uint32_t)r.pages ? a.moved[page] : -1;
+      bad |= page < 0;
+    }
+    to[j] = page;
+  }
+  if (bad && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
+}
+
+// ---- arguments ----------------------------------------------------------------------------------------------------
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int rows_params(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, int32_t* status, RowsParams& r) {
+  if (int rc = check_cache(cache)) return rc;
+  if (bounds != nullptr)
+    if (int rc = check_bounds_of(bounds, cache)) return rc;
+  if (rows == nullptr || rows->table == nullptr || rows->table_out == nullptr || rows->lens == nullptr || rows->refs == nullptr || rows->refs_out == nullptr) return KVH_E_ARG;
+  if (rows->n_requests < 1 || rows->n_requests > kMaxRequests || rows->table_pages < 1) return KVH_E_ARG;
+  const int64_t least = rows->n_requests > 1 ? rows->table_pages : 0;
+  if (rows->table_stride < least || rows->table_out_stride < least) return KVH_E_ARG;
+  if (rows->table == rows->table_out || rows->refs == rows->refs_out) return KVH_E_ARG;
+  if (!aligned4(rows->table) || !aligned4(rows->table_out) || !aligned4(rows->lens) || !aligned4(rows->refs) || !aligned4(rows->refs_out)) return KVH_E_ALIGN;
+  r.table = rows->table, r.table_out = rows->table_out;
+  r.ts = rows->table_stride, r.to_ts = rows->table_out_stride;
+  r.lens = rows->lens, r.refs = rows->refs, r.refs_out = rows->refs_out;
+  r.table_pages = rows->table_pages, r.n = rows->n_requests, r.pages = cache->pages, r.block_tokens = cache->block_tokens;
+  r.capacity = std::min<int64_t>((int64_t)rows->table_pages * cache->block_tokens, kMaxLength);
+  r.status = status;
+  r.by_block = Divisor((uint32_t)cache->block_tokens);
+  return KVH_OK;
+}
+
+}  // namespace
+}  // namespace kvh
+
+using namespace kvh;
+
+extern "C" {
+
+int kvh_copy_pages(const kvh_cache* cache, const kvh_bounds* bounds, const int32_t* src_dev, const int32_t* dst_dev, int n, int32_t* status_dev, void* stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (bounds != nullptr)
+    if (int rc = check_bounds_of(bounds, cache)) return rc;
+  if (n < 0 || n > 1 << 24 || (n > 0 && (src_dev == nullptr || dst_dev == nullptr))) return KVH_E_ARG;
+  if (!aligned4(src_dev) || !aligned4(dst_dev)) return KVH_E_ALIGN;
+  return launch_copy(*cache, bounds, src_dev, dst_dev, n, status_dev, static_cast<hipStream_t>(stream));
+}
+
+size_t kvh_fork_workspace(int n_requests, int pages) {
+  if (n_requests < 1 || n_requests > kMaxRequests || pages < 1) return 0;
+  return ((size_t)4 * n_requests + pages) * sizeof(int32_t);
+}
+
+int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, const int32_t* parents_dev, const int32_t* grow_dev,
+             int32_t* lens_out_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream) {
+  ForkParams a{};
+  if (int rc = rows_params(cache, bounds, rows, status_dev, a.r)) return rc;
+  if (lens_out_dev == nullptr || lens_out_dev == rows->lens || workspace_dev == nullptr) return KVH_E_ARG;
+  if (!aligned4(lens_out_dev) || !aligned4(parents_dev) || !aligned4(grow_dev) || !aligned4(workspace_dev)) return KVH_E_ALIGN;
+  if (workspace_bytes < kvh_fork_workspace(a.r.n, a.r.pages)) return KVH_E_SIZE;
+  a.parents = parents_dev, a.grow = grow_dev, a.lens_out = lens_out_dev;
+  a.need = static_cast<int32_t*>(workspace_dev);
+  a.base = a.need + a.r.n, a.src = a.base + a.r.n, a.dst = a.src + a.r.n, a.fresh = a.dst + a.r.n;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  launch_kernel(start_kernel, dim3((unsigned)(((int64_t)a.r.pages + kBlockThreads - 1) / kBlockThreads)), dim3(kBlockThreads), 0, s, a.r);
+  KVH_HIP_CHECK_LAUNCH();
+  hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
+  KVH_HIP_CHECK_LAUNCH();
+  hipLaunchKernelGGL(hand_out_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
+  KVH_HIP_CHECK_LAUNCH();
+  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
+  KVH_HIP_CHECK_LAUNCH();
+  return launch_copy(*cache, bounds, a.src, a.dst, a.r.n, nullptr, s);
+}
+
+size_t kvh_compact_workspace(int pages) { return pages < 1 ? 0 : (size_t)2 * (pages / 2 + 1) * sizeof(int32_t); }
+
+int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, int32_t* moved_out_dev, void* workspace_dev,
+                size_t workspace_bytes, int32_t* status_dev, void* stream) {
+  CompactParams a{};
+  if (int rc = rows_params(cache, bounds, rows, status_dev, a.r)) return rc;
+  if (moved_out_dev == nullptr || workspace_dev == nullptr) return KVH_E_ARG;
+  if (!aligned4(moved_out_dev) || !aligned4(workspace_dev)) return KVH_E_ALIGN;
+  if (workspace_bytes < kvh_compact_workspace(a.r.pages)) return KVH_E_SIZE;
+  a.moved = moved_out_dev;
+  a.src = static_cast<int32_t*>(workspace_dev), a.dst = a.src + a.r.pages / 2 + 1;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  launch_kernel(place_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
+  KVH_HIP_CHECK_LAUNCH();
+  hipLaunchKernelGGL(renumber_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
+  KVH_HIP_CHECK_LAUNCH();
+  return launch_copy(*cache, bounds, a.src, a.dst, a.r.pages / 2, nullptr, s);
+}
+
+}  // extern "C"
