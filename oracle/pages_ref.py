@@ -118,7 +118,7 @@ def fork(table, lens, refs, bt, parents=None, grow=None):
             status[b] = BAD
             continue
         full = length // bt
-        first = a not in parents[:b]
+        first = not any(parents[i] == a and grow[i] >= 0 and length + grow[i] <= room for i in range(b))
         kept[b] = list(table[a][:full + (1 if length % bt and first else 0)]) if a >= 0 else []
         wanted[b] = (length + grow[b], table[a][full] if length % bt and not first else -1)
         for p in kept[b]:

@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kBlockThreads) void start_kernel(RowsParams r) {
   if (p < r.pages) r.refs_out[p] = r.refs[p];
 }
 
-// All threads of a block.  The lengths and the entries are checked, and whether the row is the first of its parent's children.
+// All threads of a block.  The lengths and the entries are checked, and whether the row is the first of its parent's children (those that are not refused here).
 __device__ __forceinline__ Child child_of(const ForkParams& a, int b) {
   const RowsParams& r = a.r;
   Child c;
@@ -165,7 +165,8 @@ __device__ __forceinline__ Child child_of(const ForkParams& a, int b) {
     const int32_t* from = r.table + (int64_t)c.parent * r.ts;
     for (int j = threadIdx.x; j < c.full + open; j += kBlockThreads) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
     if (open && a.parents != nullptr)
-      for (int i = threadIdx.x; i < b; i += kBlockThreads) other |= a.parents[i] == c.parent;
+      for (int i = threadIdx.x; i < b; i += kBlockThreads)  // (what a child that is refused would keep is not kept, and may be handed out)
+        if (a.parents[i] == c.parent) other |= a.grow == nullptr || (a.grow[i] >= 0 && c.old_len + (int64_t)a.grow[i] <= r.capacity);
   }
   odd = __syncthreads_or(odd) != 0;
   other = __syncthreads_or(other) != 0;

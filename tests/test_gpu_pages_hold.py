@@ -220,6 +220,16 @@ def test_fork_with_no_page_to_spare(kvh):
     assert said == [0, 0, NO_PAGES, 0]
 
 
+def test_fork_first_child_refused(kvh):
+    """The first child grows past the table: the second one keeps the page, which nobody else is handed, the third one gets a copy."""
+    held = Held(random.Random(4), 4, 0, 16, 3, 0)
+    held.pages, held.lens, held.refs = 5, [20, 0, 0, 0], [1, 1, 0, 0, 0]
+    held.table = [[1, 0, -1], [-1] * 3, [-1] * 3, [-1] * 3]
+    pool = Pool(5, bt=16, seed=4)
+    said, pairs = fork(kvh, pool, held, [0, -1, 0, 0], [29, 20, 1, 2])
+    assert said == [BAD, 0, 0, 0] and held.table == [[-1] * 3, [2, 3, -1], [1, 0, -1], [1, 4, -1]] and pairs == [(0, 4)]
+
+
 @pytest.mark.parametrize("store", ["fp16", "e4m3"])
 @pytest.mark.parametrize("n,bt,columns,spare,share", [(1, 16, 4, 0, 1), (6, 7, 20, 50, 2), (30, 16, 40, 3000, 3), (2, 1, 3, 1, 1), (90, 4, 30, 700, 1)])
 def test_compact(kvh, n, bt, columns, spare, share, store):
