@@ -472,9 +472,9 @@ int kvh_bound_keys(const kvh_cache* cache, const kvh_requests* requests, kvh_dty
  * pages_dev: int32 [n_tokens][heads][count], dense: logical pages, ascending, then -1.  first >= 0, last >= 1, first + last <= count <= 4096.
  * A page outside [0, pages) in the table is not chosen (status_dev).  Rows of refused requests, and rows of no request, are left as they are; a token at a
  * position below 0 gets -1 throughout.
- * workspace_dev: scores, 16-byte aligned; kvh_select_workspace says how much serves best (64 MiB at most, where a token's own scores do not take more); with less the
- * call takes the tokens in turns.  KVH_E_SIZE where it does not hold one token's scores (4 heads table_pages bytes, rounded up to 16).  It needs no preparation and keeps
- * nothing that another call reads. */
+ * workspace_dev: scores, 16-byte aligned, where there are few tokens or very many pages; kvh_select_workspace says how much serves best (0 where none is used; 64 MiB at
+ * most, where a token's own scores do not take more).  With less the call takes the tokens in turns, or a slower way; KVH_E_SIZE where the table has room for more than 14000 pages and
+ * the workspace does not hold one token's scores (4 heads table_pages bytes, table_pages rounded up to a multiple of 4).  It needs no preparation and keeps nothing that another call reads. */
 size_t kvh_select_workspace(int n_requests, int n_tokens, int heads, int table_pages);
 int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q, int q_heads, int first, int last,
                      int count, int32_t* pages_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream);
@@ -515,7 +515,7 @@ typedef struct {
 
 /* Fork: row b becomes a child of row a = parents[b] and grows by grow[b] tokens: lens_out[b] = lens[a] + grow[b].  parents NULL: every row is its own child;
  * parents[b] < 0: of none, an empty row.  grow NULL: zeros.  A step's growth, beams that are reordered, samples of one prompt, requests that begin and end are
- * one call of this.  The full pages of lens[a] tokens are shared.  A page that they do not fill stays with the first of a's children; the others get a
+ * one call of this.  The full pages of lens[a] tokens are shared.  A page that they do not fill stays with the first of a's children that is no KVH_DEV_BAD_REQUEST; the others get a
  * copy of it (all layers, scales, bounds) on a fresh page, so that each row appends to a page of its own: such a page must be in no other row before the call.
  * Fresh pages are those that no row holds afterwards and nothing else does, lowest numbers first, handed to the rows in order; refs_out counts what rows hold after the
  * call in place of what they held before it.  A page that is given up and one that is handed out may be the same: the old rows are of no use afterwards.

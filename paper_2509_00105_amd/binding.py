@@ -189,7 +189,8 @@ def lib() -> ctypes.CDLL:
         if _fastcall is not None and _raw_stream is not None:
             _fast = _fastcall.Calls(torch.cuda.current_device, _raw_stream, *[
                 ctypes.cast(f, vp).value for f in (L.kvh_encode, L.kvh_encode_batch, L.kvh_decode, L.kvh_decode_batch,
-                                                   L.kvh_encode_kept, L.kvh_decode_kept, L.kvh_append, L.kvh_attention)])
+                                                   L.kvh_encode_kept, L.kvh_decode_kept, L.kvh_append, L.kvh_attention, L.kvh_bound_keys,
+                                                   L.kvh_select_pages, L.kvh_attention_pages, L.kvh_copy_pages, L.kvh_fork, L.kvh_compact)])
         _lib = L
     return _lib
 
@@ -822,6 +823,9 @@ def bound_keys(k_cache: torch.Tensor, bounds: torch.Tensor, bound_scale: torch.T
                max_new: int, k_scale: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None) -> None:
     """kvh_bound_keys: the bounds, int8 [l][P][heads][2][head_dim] and float32 [l][P][heads], of the pages that the requests' new tokens lie on,
     from a K cache [l][P][block][c] (16-bit, int8 or float8_e4m3fn with scales [l][P][heads])."""
+    rc = _fast.bound_keys(k_cache, bounds, bound_scale, starts, lens, page_table, max_new, k_scale, status, stream) if _fast is not None else None
+    if rc is not None:
+        return _check(rc, "kvh_bound_keys")
     _here(k_cache, k_scale, starts, lens, page_table, status)
     if bounds.dim() != 5:
         raise ValueError("bounds must be int8 [l][P][heads][2][head_dim]")
@@ -842,6 +846,11 @@ def select_pages(q: torch.Tensor, bounds: torch.Tensor, bound_scale: torch.Tenso
                  workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """kvh_select_pages: for queries [T][q_heads * head_dim] the `count` pages of each new token and KV head, int32 [T][heads][count]: logical pages, ascending,
     then -1.  workspace: uint8, kept by programs that call often (see select_workspace); made here if none is given."""
+    rc = _fast.select_pages(q, bounds, bound_scale, layer, starts, lens, page_table, max_new, count, block_tokens, first, last, out, workspace, status,
+                            stream) if _fast is not None and workspace is not None and out is not None else None
+    if rc is not None:
+        _check(rc, "kvh_select_pages")
+        return out
     _here(q, starts, lens, page_table, out, status)
     if q.dtype not in _TORCH_DT or q.dim() != 2:
         raise ValueError("q must be float16 or bfloat16 [T][q_heads * head_dim]")
@@ -872,6 +881,11 @@ def attention_pages(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """kvh_attention_pages: queries [T][q_heads * head_dim] of the requests' new tokens over the pages listed for each of them and each KV head (int32
     [T][heads][count], as select_pages gives them) of layer `layer` of the cache.  Otherwise as attention."""
+    rc = _fast.attention_pages(q, k_cache, v_cache, layer, pages, starts, lens, page_table, max_new, head_dim, k_scale, v_scale, scale, out, lse, workspace, status,
+                               stream) if _fast is not None and workspace is not None and out is not None else None
+    if rc is not None:
+        _check(rc, "kvh_attention_pages")
+        return out
     _here(q, k_cache, v_cache, k_scale, v_scale, pages, starts, lens, page_table, out, lse, status)
     if q.dtype not in _TORCH_DT or q.dim() != 2:
         raise ValueError("q must be float16 or bfloat16 [T][q_heads * head_dim]")
@@ -907,6 +921,9 @@ def copy_pages(k_cache: torch.Tensor, v_cache: torch.Tensor, src: torch.Tensor, 
                v_scale: torch.Tensor | None = None, bounds: torch.Tensor | None = None, bound_scale: torch.Tensor | None = None,
                status: torch.Tensor | None = None, stream=None) -> None:
     """kvh_copy_pages: page src[i] of all layers to page dst[i] (int32), with scales and bounds; src[i] < 0: none."""
+    rc = _fast.copy_pages(k_cache, v_cache, src, dst, head_dim, k_scale, v_scale, bounds, bound_scale, status, stream) if _fast is not None else None
+    if rc is not None:
+        return _check(rc, "kvh_copy_pages")
     cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
     box = _bounds(bounds, bound_scale, cache.block_tokens)
     _here(src, dst, status)
@@ -950,6 +967,11 @@ def fork(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
          status: torch.Tensor | None = None, stream=None):
     """kvh_fork: row b of the page table becomes a child of row parents[b] (negative: none; not given: its own) and grows by grow[b] tokens.  refs: int32 [P], how
     many rows hold a page.  -> (page_table, lens, refs) after it, in the given outputs or new ones; they must not overlap the inputs."""
+    rc = _fast.fork(k_cache, v_cache, page_table, lens, refs, parents, grow, head_dim, k_scale, v_scale, bounds, bound_scale, table_out, lens_out, refs_out,
+                    workspace, status, stream) if _fast is not None and workspace is not None and table_out is not None else None
+    if rc is not None:
+        _check(rc, "kvh_fork")
+        return table_out, lens_out, refs_out
     cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
     box = _bounds(bounds, bound_scale, cache.block_tokens)
     rows, table_out, refs_out = _held(page_table, table_out, lens, refs, refs_out, cache.pages, stream)
@@ -974,6 +996,11 @@ def compact(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tens
             bound_scale: torch.Tensor | None = None, table_out: torch.Tensor | None = None, refs_out: torch.Tensor | None = None,
             moved_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
     """kvh_compact: the pages in use move to the lowest numbers.  -> (page_table, refs, moved) after it: moved[page] is a page's new number, -1 where it is free."""
+    rc = _fast.compact(k_cache, v_cache, page_table, lens, refs, head_dim, k_scale, v_scale, bounds, bound_scale, table_out, refs_out, moved_out, workspace, status,
+                       stream) if _fast is not None and workspace is not None and table_out is not None else None
+    if rc is not None:
+        _check(rc, "kvh_compact")
+        return table_out, refs_out, moved_out
     cache = _any_cache(k_cache, v_cache, k_scale, v_scale, head_dim)
     box = _bounds(bounds, bound_scale, cache.block_tokens)
     rows, table_out, refs_out = _held(page_table, table_out, lens, refs, refs_out, cache.pages, stream)

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvh.so")
 CALLS = os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))  # for the interpreter that builds it alone
 SOURCES = ["kvh_api.hip", "kvh_decode.hip", "kvh_encode.hip", "kvh_transcode.hip", "kvh_loader.hip", "kvh_policy.cpp"]
-CACHE_SOURCES = ["kvh_append.hip", "kvh_attention.hip", "kvh_attention_many.hip", "kvh_bounds.hip", "kvh_attention_pages.hip", "kvh_pages.hip"]  # what reads a caller's cache as it is: NaN and infinities are values there
+CACHE_SOURCES = ["kvh_append.hip", "kvh_attention.hip", "kvh_attention_many.hip", "kvh_bounds.hip", "kvh_select.hip", "kvh_attention_pages.hip", "kvh_pages.hip"]  # what reads a caller's cache as it is: NaN and infinities are values there
 
 # -ffp-contract=off: the codec's arithmetic fuses only where the source says fma.
 # -fno-honor-nans (the codec's sources only): inputs are finite by contract; without it every min/max of a value unpacked with

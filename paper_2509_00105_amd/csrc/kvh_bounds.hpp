@@ -1,0 +1,19 @@
+// What the bounds of keys and the selection by them share: codes of 127ths.
+#pragma once
+
+#include "kvh_cache.hpp"
+
+namespace kvh {
+
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
+  return ((uint32_t)(int)a & 0xffu) | ((uint32_t)(int)b & 0xffu) << 8 | ((uint32_t)(int)c & 0xffu) << 16 | (uint32_t)(int)d << 24;
+}
+
+// 127 x / a for |x| <= a, rounded once: x has 11 bits at most, so 127/128 of it is exact, and a >= 2^-100.
+struct Part127 {
+  float by;
+  __device__ __forceinline__ explicit Part127(float a) : by(a * (1.0f / 128.0f)) {}
+  __device__ __forceinline__ float of(float x) const { return x * (127.0f / 128.0f) / by; }
+};
+
+}  // namespace kvh

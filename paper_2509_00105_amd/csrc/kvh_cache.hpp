@@ -95,20 +95,26 @@ __device__ __forceinline__ bool request_ok(const Requests& r, int32_t start, int
 
 // The request that a row of the packed tensors belongs to; all lanes of a wave ask for the same row.  False where it is in none, or in one that is refused.
 __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
-  int first = 0, many = r.n;  // the last start that is not past the row is one of these
-  while (many > 1) {
-    const int step = (many + kWave - 1) / kWave, at = lane * step;
-    const uint64_t below = __ballot(at < many && r.starts[first + at] <= row);
-    const int k = below == 0 ? 0 : 63 - __builtin_clzll(below);
-    first += k * step;
-    many = many - k * step < step ? many - k * step : step;
+  int32_t start, end, len;
+  if (r.n <= kWave) {  // all of them at once: one trip to memory, not two
+    start = INT32_MAX, end = len = 0;
+    if (lane < r.n) start = r.starts[lane], end = r.starts[lane + 1], len = r.lens[lane];
+    const uint64_t below = __ballot(start <= row);
+    b = below == 0 ? 0 : 63 - __builtin_clzll(below);
+    start = __builtin_amdgcn_readlane(start, b), end = __builtin_amdgcn_readlane(end, b), len = __builtin_amdgcn_readlane(len, b);
+  } else {
+    int first = 0, many = r.n;  // the last start that is not past the row is one of these
+    while (many > 1) {
+      const int step = (many + kWave - 1) / kWave, at = lane * step;
+      const uint64_t below = __ballot(at < many && r.starts[first + at] <= row);
+      const int k = below == 0 ? 0 : 63 - __builtin_clzll(below);
+      first += k * step;
+      many = many - k * step < step ? many - k * step : step;
+    }
+    b = uniform(first);
+    start = uniform(r.starts[b]), end = uniform(r.starts[b + 1]), len = uniform(r.lens[b]);
   }
-  b = uniform(first);
-  rq.start = uniform(r.starts[b]);
-  const int32_t end = uniform(r.starts[b + 1]);
-  rq.len = uniform(r.lens[b]);
-  rq.n = end - rq.start;
-  rq.ok = request_ok(r, rq.start, end, rq.len) && rq.start <= row && row < end;
+  rq = Request{start, end - start, len, request_ok(r, start, end, len) && start <= row && row < end};
   return rq.ok;
 }
 

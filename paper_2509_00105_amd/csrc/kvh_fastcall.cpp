@@ -9,6 +9,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/kvh.h"
 
@@ -41,6 +42,12 @@ struct Calls {
   decltype(&kvh_decode_kept) decode_kept;
   decltype(&kvh_append) append;
   decltype(&kvh_attention) attention;
+  decltype(&kvh_bound_keys) bound_keys;
+  decltype(&kvh_select_pages) select_pages;
+  decltype(&kvh_attention_pages) attention_pages;
+  decltype(&kvh_copy_pages) copy_pages;
+  decltype(&kvh_fork) fork;
+  decltype(&kvh_compact) compact;
   PyObject *current_device, *raw_stream;
 };
 
@@ -48,6 +55,8 @@ struct Calls {
 // meets the same one, but not what is no error of the call (an interrupt, an exit).
 struct Reader {
   bool ok = true;
+  int on = -1;         // the device of the tensors whose fields were read
+  bool apart = false;  // they are on several
 
   bool is_true(PyObject* t, PyObject* name) {
     PyObject* r = PyObject_GetAttr(t, name);
@@ -294,7 +303,7 @@ struct Fields {
   void* p = nullptr;
   Type type = Type::kNone;
   int n = 0;
-  int64_t size[4], stride[4];
+  int64_t size[5], stride[5];
   bool dense(int d) const { return size[d] <= 1 || stride[d] == 1; }
 };
 
@@ -320,6 +329,8 @@ Fields read_fields(Reader& r, PyObject* t, int dims, bool optional = false) {
     r.ok = false;
     return f;
   }
+  if (r.on >= 0 && r.on != d.device.device_id) r.apart = true;
+  r.on = d.device.device_id;
   f.p = static_cast<char*>(d.data) + d.byte_offset;
   f.type = type_of(d.dtype);
   f.n = dims;
@@ -472,6 +483,203 @@ PyObject* attention(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
+// What the calls on pages ask of their tensors: they are on the current device.
+void expect_here(Reader& r, Calls* self) {
+  if (!r.ok) return;
+  PyObject* dev = PyObject_CallNoArgs(self->current_device);
+  r.ok = dev != nullptr && PyLong_CheckExact(dev) && !r.apart && PyLong_AsLong(dev) == r.on;
+  Py_XDECREF(dev);
+  if (PyErr_Occurred()) r.ok = false;
+}
+
+// The bounds of [l][P][heads][2][head_dim] codes and [l][P][heads] scales, as binding.py's _bounds takes them; both None: none.
+kvh_bounds read_bounds(Reader& r, PyObject* codes, PyObject* scale, int block_tokens, bool optional) {
+  kvh_bounds b{};
+  const Fields c = read_fields(r, codes, 5, optional), s = read_fields(r, scale, 3, optional);
+  if (!r.ok || (c.p == nullptr && s.p == nullptr)) return b;
+  expect(r, c.p != nullptr && s.p != nullptr && c.type == Type::kI8 && s.type == Type::kF32);
+  if (!r.ok) return b;
+  const int64_t dim = c.size[4];
+  expect(r, c.size[3] == 2 && c.dense(4) && c.stride[3] == dim && (c.size[2] == 1 || c.stride[2] == 2 * dim) && s.dense(2));
+  for (int i = 0; i < 3; ++i) expect(r, c.size[i] == s.size[i]);
+  b.codes = static_cast<int8_t*>(c.p), b.scale = static_cast<float*>(s.p);
+  b.layer_stride = c.size[0] > 1 ? c.stride[0] : 0, b.page_stride = c.size[1] > 1 ? c.stride[1] : 2 * c.size[2] * dim;
+  b.scale_layer_stride = s.size[0] > 1 ? s.stride[0] : 0, b.scale_page_stride = s.size[1] > 1 ? s.stride[1] : s.size[2];
+  b.layers = (int32_t)c.size[0], b.pages = (int32_t)c.size[1], b.block_tokens = block_tokens, b.heads = (int32_t)c.size[2], b.head_dim = (int32_t)dim;
+  return b;
+}
+
+// A cache whose 16-bit type does not matter.
+kvh_cache read_any_cache(Reader& r, PyObject* kc, PyObject* vc, PyObject* ks, PyObject* vs, int head_dim) {
+  const Fields k = read_fields(r, kc, 4);
+  const bool half = k.type == Type::kF16 || k.type == Type::kBF16;
+  return read_cache(r, kc, vc, ks, vs, head_dim, half ? k.type : Type::kF16);
+}
+
+// bound_keys(k_cache, bounds, bound_scale, starts, lens, page_table, max_new, k_scale, status, stream)
+PyObject* bound_keys(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(10);
+  if (self->bound_keys == nullptr) Py_RETURN_NONE;
+  const Fields k = read_fields(r, a[0], 4), c = read_fields(r, a[1], 5);
+  const bool half = k.type == Type::kF16 || k.type == Type::kBF16;
+  kvh_cache cache{};
+  kvh_bounds box{};
+  kvh_requests req{};
+  if (r.ok) {
+    expect(r, c.size[4] <= INT32_MAX);
+    cache = read_cache(r, a[0], a[0], a[7], a[7], (int)c.size[4], half ? k.type : Type::kF16);
+    box = read_bounds(r, a[1], a[2], cache.block_tokens, false);
+    req = read_requests(r, a[3], a[4], a[5], a[6], INT32_MAX);
+  }
+  int32_t* status = read_words(r, a[8], req.n_requests, true);
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[9]);
+  return finish(r, [&] { return self->bound_keys(&cache, &req, k.type == Type::kBF16 ? KVH_BF16 : KVH_F16, &box, status, stream); });
+}
+
+// A dense int32 [tokens][heads][count]: its last size.
+int read_lists(Reader& r, const Fields& f, int64_t tokens, int64_t heads) {
+  if (!r.ok) return 0;
+  expect(r, f.type == Type::kI32 && f.size[0] == tokens && f.size[1] == heads && f.dense(2) && (heads == 1 || f.stride[1] == f.size[2]) &&
+                (tokens == 1 || f.stride[0] == heads * f.size[2]));
+  return (int)f.size[2];
+}
+
+// select_pages(q, bounds, bound_scale, layer, starts, lens, page_table, max_new, count, block_tokens, first, last, out, workspace, status, stream)
+PyObject* select_pages(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(16);
+  if (self->select_pages == nullptr) Py_RETURN_NONE;
+  const Fields q = read_fields(r, a[0], 2), o = read_fields(r, a[12], 3), ws = read_fields(r, a[13], 1);
+  const int layer = r.narrow(a[3]), count = r.narrow(a[8]), block = r.narrow(a[9]), first = r.narrow(a[10]), last = r.narrow(a[11]);
+  const kvh_bounds box = read_bounds(r, a[1], a[2], block, false);
+  kvh_requests req{};
+  kvh_rows rows{};
+  int q_heads = 0;
+  if (r.ok) {
+    expect(r, (q.type == Type::kF16 || q.type == Type::kBF16) && ws.type == Type::kU8 && ws.dense(0) && q.size[1] % box.head_dim == 0 &&
+                  read_lists(r, o, q.size[0], box.heads) == count);
+    q_heads = (int)(q.size[1] / box.head_dim);
+    req = read_requests(r, a[4], a[5], a[6], a[7], q.size[0]);
+    rows = rows_of(r, q, q.type, 1, q.size[0], q.size[1]);
+  }
+  int32_t* status = read_words(r, a[14], req.n_requests, true);
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[15]);
+  return finish(r, [&] {
+    return self->select_pages(&box, layer, &req, q.type == Type::kF16 ? KVH_F16 : KVH_BF16, &rows, q_heads, first, last, count, static_cast<int32_t*>(o.p), ws.p,
+                              (size_t)ws.size[0], status, stream);
+  });
+}
+
+// attention_pages(q, k_cache, v_cache, layer, pages, starts, lens, page_table, max_new, head_dim, k_scale, v_scale, scale or None, out, lse, workspace, status,
+// stream)
+PyObject* attention_pages(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(18);
+  if (self->attention_pages == nullptr) Py_RETURN_NONE;
+  const Fields q = read_fields(r, a[0], 2), list = read_fields(r, a[4], 3), o = read_fields(r, a[13], 2), lse = read_fields(r, a[14], 2, true),
+               ws = read_fields(r, a[15], 1);
+  const int layer = r.narrow(a[3]), head_dim = r.narrow(a[9]);
+  if (a[12] != Py_None && !PyFloat_CheckExact(a[12])) r.ok = false;
+  expect(r, r.ok && (q.type == Type::kF16 || q.type == Type::kBF16) && ws.type == Type::kU8 && ws.dense(0) && head_dim > 0 && q.size[1] % head_dim == 0);
+  kvh_cache c{};
+  kvh_requests req{};
+  kvh_rows from{}, to{};
+  int q_heads = 0, count = 0;
+  if (r.ok) {
+    c = read_cache(r, a[1], a[2], a[10], a[11], head_dim, q.type);
+    req = read_requests(r, a[5], a[6], a[7], a[8], q.size[0]);
+  }
+  if (r.ok) {
+    q_heads = (int)(q.size[1] / head_dim);
+    from = rows_of(r, q, q.type, 1, q.size[0], q.size[1]);
+    to = rows_of(r, o, q.type, 1, q.size[0], q.size[1]);
+    count = read_lists(r, list, q.size[0], c.heads);
+    if (lse.p != nullptr)
+      expect(r, lse.type == Type::kF32 && lse.size[0] == q.size[0] && lse.size[1] == q_heads && lse.dense(1) && (lse.size[0] == 1 || lse.stride[0] == q_heads));
+  }
+  int32_t* status = read_words(r, a[16], req.n_requests, true);
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[17]);
+  const float scale = a[12] == Py_None ? (r.ok ? (float)std::pow((double)head_dim, -0.5) : 0.0f) : (float)PyFloat_AS_DOUBLE(a[12]);
+  return finish(r, [&] {
+    return self->attention_pages(&c, layer, &req, q.type == Type::kF16 ? KVH_F16 : KVH_BF16, &from, &to, q_heads, static_cast<const int32_t*>(list.p), count,
+                                 static_cast<float*>(lse.p), scale, ws.p, (size_t)ws.size[0], status, stream);
+  });
+}
+
+// copy_pages(k_cache, v_cache, src, dst, head_dim, k_scale, v_scale, bounds, bound_scale, status, stream)
+PyObject* copy_pages(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(11);
+  if (self->copy_pages == nullptr) Py_RETURN_NONE;
+  const int head_dim = r.narrow(a[4]);
+  expect(r, head_dim > 0);
+  const Fields src = read_fields(r, a[2], 1), dst = read_fields(r, a[3], 1);
+  kvh_cache c{};
+  kvh_bounds box{};
+  if (r.ok) {
+    expect(r, src.type == Type::kI32 && dst.type == Type::kI32 && src.dense(0) && dst.dense(0) && src.size[0] == dst.size[0]);
+    c = read_any_cache(r, a[0], a[1], a[5], a[6], head_dim);
+    box = read_bounds(r, a[7], a[8], c.block_tokens, true);
+  }
+  int32_t* status = read_words(r, a[9], r.ok ? src.size[0] : 0, true);
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[10]);
+  return finish(r, [&] {
+    return self->copy_pages(&c, box.codes != nullptr ? &box : nullptr, static_cast<const int32_t*>(src.p), static_cast<const int32_t*>(dst.p), (int)src.size[0], status,
+                            stream);
+  });
+}
+
+kvh_rows_of_pages read_held(Reader& r, PyObject* table, PyObject* table_out, PyObject* lens, PyObject* refs, PyObject* refs_out, int64_t pages) {
+  kvh_rows_of_pages h{};
+  const Fields t = read_fields(r, table, 2), o = read_fields(r, table_out, 2), l = read_fields(r, lens, 1), c = read_fields(r, refs, 1), to = read_fields(r, refs_out, 1);
+  if (!r.ok) return h;
+  for (const Fields* f : {&t, &o}) expect(r, f->type == Type::kI32 && f->dense(1) && f->size[0] == l.size[0] && f->size[1] == t.size[1]);
+  for (const Fields* f : {&l, &c, &to}) expect(r, f->type == Type::kI32 && f->dense(0));
+  expect(r, c.size[0] == pages && to.size[0] == pages);
+  h.table = static_cast<const int32_t*>(t.p), h.table_out = static_cast<int32_t*>(o.p);
+  h.table_stride = t.size[0] > 1 ? t.stride[0] : t.size[1], h.table_out_stride = t.size[0] > 1 ? o.stride[0] : t.size[1];
+  h.lens = static_cast<const int32_t*>(l.p), h.refs = static_cast<const int32_t*>(c.p), h.refs_out = static_cast<int32_t*>(to.p);
+  h.table_pages = (int32_t)t.size[1], h.n_requests = (int32_t)l.size[0];
+  return h;
+}
+
+// fork(k_cache, v_cache, page_table, lens, refs, parents, grow, head_dim, k_scale, v_scale, bounds, bound_scale, table_out, lens_out, refs_out, workspace, status,
+// stream)
+PyObject* fork(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(18);
+  if (self->fork == nullptr) Py_RETURN_NONE;
+  const int head_dim = r.narrow(a[7]);
+  expect(r, head_dim > 0);
+  const kvh_cache c = r.ok ? read_any_cache(r, a[0], a[1], a[8], a[9], head_dim) : kvh_cache{};
+  const kvh_bounds box = read_bounds(r, a[10], a[11], c.block_tokens, true);
+  const kvh_rows_of_pages h = read_held(r, a[2], a[12], a[3], a[4], a[14], c.pages);
+  const int32_t *parents = read_words(r, a[5], h.n_requests, true), *grow = read_words(r, a[6], h.n_requests, true);
+  int32_t *lens_out = read_words(r, a[13], h.n_requests), *status = read_words(r, a[16], h.n_requests, true);
+  const Fields ws = read_fields(r, a[15], 1);
+  expect(r, ws.type == Type::kU8 && ws.dense(0));
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[17]);
+  return finish(r, [&] { return self->fork(&c, box.codes != nullptr ? &box : nullptr, &h, parents, grow, lens_out, ws.p, (size_t)ws.size[0], status, stream); });
+}
+
+// compact(k_cache, v_cache, page_table, lens, refs, head_dim, k_scale, v_scale, bounds, bound_scale, table_out, refs_out, moved_out, workspace, status, stream)
+PyObject* compact(PyObject* self_, PyObject* const* a, Py_ssize_t n_args) {
+  KVH_ARGS(16);
+  if (self->compact == nullptr) Py_RETURN_NONE;
+  const int head_dim = r.narrow(a[5]);
+  expect(r, head_dim > 0);
+  const kvh_cache c = r.ok ? read_any_cache(r, a[0], a[1], a[6], a[7], head_dim) : kvh_cache{};
+  const kvh_bounds box = read_bounds(r, a[8], a[9], c.block_tokens, true);
+  const kvh_rows_of_pages h = read_held(r, a[2], a[10], a[3], a[4], a[11], c.pages);
+  int32_t *moved = read_words(r, a[12], c.pages), *status = read_words(r, a[14], h.n_requests, true);
+  const Fields ws = read_fields(r, a[13], 1);
+  expect(r, ws.type == Type::kU8 && ws.dense(0));
+  expect_here(r, self);
+  void* stream = read_stream(r, self, a[15]);
+  return finish(r, [&] { return self->compact(&c, box.codes != nullptr ? &box : nullptr, &h, moved, ws.p, (size_t)ws.size[0], status, stream); });
+}
+
 void find_exchange() {
   PyObject* capsule = PyObject_GetAttrString(tensor_type, "__dlpack_c_exchange_api__");
   if (capsule != nullptr && PyCapsule_IsValid(capsule, "dlpack_exchange_api")) {
@@ -485,6 +693,12 @@ void find_exchange() {
 // Without the interface these calls are binding.py's.
 PyObject* append(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
 PyObject* attention(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* bound_keys(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* select_pages(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* attention_pages(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* copy_pages(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* fork(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
+PyObject* compact(PyObject*, PyObject* const*, Py_ssize_t) { Py_RETURN_NONE; }
 void find_exchange() {}
 #endif
 
@@ -492,8 +706,9 @@ void find_exchange() {}
 // calls then go the ctypes way)
 PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
   PyObject *dev, *raw;
-  unsigned long long p[8] = {};
-  if (!PyArg_ParseTuple(args, "OOKKKKKK|KK", &dev, &raw, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7])) return nullptr;
+  unsigned long long p[14] = {};
+  if (!PyArg_ParseTuple(args, "OOKKKKKK|KKKKKKKK", &dev, &raw, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12], &p[13]))
+    return nullptr;
   Calls* c = reinterpret_cast<Calls*>(type->tp_alloc(type, 0));
   if (c == nullptr) return nullptr;
   c->encode = reinterpret_cast<decltype(c->encode)>((uintptr_t)p[0]);
@@ -504,6 +719,12 @@ PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
   c->decode_kept = reinterpret_cast<decltype(c->decode_kept)>((uintptr_t)p[5]);
   c->append = reinterpret_cast<decltype(c->append)>((uintptr_t)p[6]);
   c->attention = reinterpret_cast<decltype(c->attention)>((uintptr_t)p[7]);
+  c->bound_keys = reinterpret_cast<decltype(c->bound_keys)>((uintptr_t)p[8]);
+  c->select_pages = reinterpret_cast<decltype(c->select_pages)>((uintptr_t)p[9]);
+  c->attention_pages = reinterpret_cast<decltype(c->attention_pages)>((uintptr_t)p[10]);
+  c->copy_pages = reinterpret_cast<decltype(c->copy_pages)>((uintptr_t)p[11]);
+  c->fork = reinterpret_cast<decltype(c->fork)>((uintptr_t)p[12]);
+  c->compact = reinterpret_cast<decltype(c->compact)>((uintptr_t)p[13]);
   Py_INCREF(dev);
   Py_INCREF(raw);
   c->current_device = dev;
@@ -522,7 +743,9 @@ void calls_dealloc(PyObject* o) {
 
 #define KVH_METHOD(F) {#F, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(F)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KVH_METHOD(encode), KVH_METHOD(encode_batch), KVH_METHOD(decode), KVH_METHOD(decode_batch),
-                         KVH_METHOD(encode_kept), KVH_METHOD(decode_kept), KVH_METHOD(append), KVH_METHOD(attention), {nullptr, nullptr, 0, nullptr}};
+                         KVH_METHOD(encode_kept), KVH_METHOD(decode_kept), KVH_METHOD(append), KVH_METHOD(attention),
+                         KVH_METHOD(bound_keys), KVH_METHOD(select_pages), KVH_METHOD(attention_pages), KVH_METHOD(copy_pages), KVH_METHOD(fork),
+                         KVH_METHOD(compact), {nullptr, nullptr, 0, nullptr}};
 PyType_Slot slots[] = {{Py_tp_new, reinterpret_cast<void*>(calls_new)}, {Py_tp_dealloc, reinterpret_cast<void*>(calls_dealloc)},
                        {Py_tp_methods, methods}, {0, nullptr}};
 PyType_Spec spec = {"kvh_fastcall.Calls", sizeof(Calls), 0, Py_TPFLAGS_DEFAULT, slots};

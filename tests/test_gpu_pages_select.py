@@ -281,8 +281,10 @@ def test_odd_scores(kvh):
 
 
 def test_workspace_in_turns(kvh):
-    b = Batch([3, 1, 9], [100, 700, 90], heads=2, group=4, seed=34)
+    """Too many pages for a block to keep their scores: through memory, all tokens at once and in turns."""
+    b = Batch([3, 1, 9], [100, 18001, 90], heads=2, group=4, dim=64, bt=1, seed=34, layers=1)
     want = b.run(kvh, 20)
+    assert np.array_equal(want.cpu().numpy(), b.want(20))
     pitch = -(-len(b.table_h[0]) // 4) * 4
     for tokens in (1, 2, 5):
         room = torch.full((2 * pitch * 4 * tokens + 8,), 255, dtype=torch.uint8, device="cuda")
@@ -290,6 +292,15 @@ def test_workspace_in_turns(kvh):
     with pytest.raises(kvh.KVHError) as e:
         b.run(kvh, 20, workspace=room[:2 * pitch * 4 - 1])
     assert e.value.status == -4
+
+
+@pytest.mark.parametrize("group", [1, 4, 6, 17])
+def test_with_and_without_a_workspace(kvh, group):
+    """Scores through memory or not, tokens together or each by itself: the same pages."""
+    b = Batch([2, 5], [9000, 40], heads=1, group=group, dim=64, bt=2, seed=37, layers=1)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    one, two = b.run(kvh, 50), b.run(kvh, 50, workspace=none)
+    assert torch.equal(one, two) and np.array_equal(one.cpu().numpy(), b.want(50))
 
 
 def test_selection_refusals(kvh):

@@ -85,7 +85,8 @@ def test_select_arguments(b):
     for kw in (dict(first=-1), dict(last=0), dict(first=3, last=2), dict(count=0), dict(count=4097), dict(first=2 ** 31 - 1), dict(last=2 ** 31 - 1)):
         assert select(b, **kw) == ARG, kw
     assert select(b, ws=72) == ALIGN and select(b, out=66) == ALIGN
-    assert select(b, ws=None) == SIZE and select(b, size=8 * 16 - 1) == SIZE  # 8 heads of 4 pages
+    wide = requests(b, table_pages=20001, table_stride=20001)
+    assert select(b, r=wide, ws=None) == SIZE and select(b, r=wide, size=8 * 20004 * 4 - 1) == SIZE
 
 
 def test_attention_arguments(b):
@@ -123,7 +124,8 @@ def test_fork_and_compact_arguments(b):
 def test_workspaces(b):
     lib = b.lib()
     assert lib.kvh_select_workspace(0, 1, 8, 4) == 0 and lib.kvh_select_workspace(1, 0, 8, 4) == 0 and lib.kvh_select_workspace(1, 1, 0, 4) == 0
-    assert lib.kvh_select_workspace(1, 1, 8, 5) >= 8 * 5 * 4 and lib.kvh_select_workspace(1, 1 << 20, 8, 4096) <= 64 << 20
+    assert lib.kvh_select_workspace(1, 1, 8, 20001) >= 8 * 20001 * 4 and lib.kvh_select_workspace(1, 1 << 20, 8, 20001) <= 64 << 20
+    assert lib.kvh_select_workspace(64, 64, 8, 256) == 0
     size = lib.kvh_attention_pages_workspace
     assert size(0, 8, 32, 128, 16, 64) == 0 and size(1, 8, 12, 128, 16, 64) == 0 and size(1, 8, 32, 96, 16, 64) == 0 and size(1, 8, 32, 128, 0, 64) == 0
     assert size(1, 8, 32, 128, 16, 0) == 0 and size(1, 8, 32, 128, 16, 4097) == 0 and size(1, 8, 32, 128, 16, 256) > 0 and size(512, 8, 32, 128, 16, 256) == 0
