@@ -285,32 +285,6 @@ __device__ __forceinline__ Words<N> fetch(const uint8_t* p) {
   return r;
 }
 
-// The two values of lanes 32 apart, and of lanes 16 apart, in both: moves between lanes without LDS.
-__device__ __forceinline__ f32x2 apart32(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
-  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
-}
-__device__ __forceinline__ f32x2 apart16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
-  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
-}
-__device__ __forceinline__ float over_halves_max(float v) {  // of the 2 lanes that hold a row of the kernel for many rows
-  const f32x2 x = apart32(v);
-  return fmaxf(x[0], x[1]);
-}
-__device__ __forceinline__ float over_halves_sum(float v) {
-  const f32x2 x = apart32(v);
-  return x[0] + x[1];
-}
-__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row of the kernel for few
-  const f32x2 x = apart16(v);
-  return over_halves_max(fmaxf(x[0], x[1]));
-}
-__device__ __forceinline__ float over_groups_sum(float v) {
-  const f32x2 x = apart16(v);
-  return over_halves_sum(x[0] + x[1]);
-}
-
 // ---- the page table, 64 entries at a time in the lanes ---------------------------------------------------------------
 struct PageRun {
   int base, entry;  // entry of page base + lane; -1 where it is none of the cache's

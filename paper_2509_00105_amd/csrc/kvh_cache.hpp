@@ -93,6 +93,32 @@ __device__ __forceinline__ bool request_ok(const Requests& r, int32_t start, int
   return start >= 0 && end >= start && end <= r.n_tokens && end - start <= r.max_new && len >= 0 && len <= r.capacity;
 }
 
+// The two values of lanes 32 apart, and of lanes 16 apart, in both: moves between lanes without LDS.
+__device__ __forceinline__ f32x2 apart32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
+}
+__device__ __forceinline__ f32x2 apart16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+  return f32x2{__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])};
+}
+__device__ __forceinline__ float over_halves_max(float v) {  // of the 2 lanes that hold a row of the kernel for many rows
+  const f32x2 x = apart32(v);
+  return fmaxf(x[0], x[1]);
+}
+__device__ __forceinline__ float over_halves_sum(float v) {
+  const f32x2 x = apart32(v);
+  return x[0] + x[1];
+}
+__device__ __forceinline__ float over_groups_max(float v) {  // of the 4 lanes that hold a row of the kernel for few
+  const f32x2 x = apart16(v);
+  return over_halves_max(fmaxf(x[0], x[1]));
+}
+__device__ __forceinline__ float over_groups_sum(float v) {
+  const f32x2 x = apart16(v);
+  return over_halves_sum(x[0] + x[1]);
+}
+
 // The request that a row of the packed tensors belongs to; all lanes of a wave ask for the same row.  False where it is in none, or in one that is refused.
 __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
   int32_t start, end, len;
@@ -118,10 +144,11 @@ __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane,
   return rq.ok;
 }
 
-// Says which requests are refused; the kernels pass over them.
+// Says which requests are refused; the kernels, of THREADS threads a block, pass over them.
+template <int THREADS = kBlockThreads>
 __device__ __forceinline__ void tell_refused(const Requests& r, int32_t* status) {
   if (blockIdx.x != 0 || status == nullptr) return;
-  for (int b = threadIdx.x; b < r.n; b += kBlockThreads)
+  for (int b = threadIdx.x; b < r.n; b += THREADS)
     if (!request_ok(r, r.starts[b], r.starts[b + 1], r.lens[b])) status[b] = KVH_DEV_BAD_REQUEST;
 }
 

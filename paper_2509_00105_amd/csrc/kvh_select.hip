@@ -24,6 +24,31 @@ __device__ __forceinline__ uint32_t order_of(float score) {
   return (w >> 31) != 0 ? ~w : w | 0x80000000u;
 }
 
+// Lanes of a row of 16 exchange by moves; rows through scalar registers.
+template <int CTRL>
+__device__ __forceinline__ uint32_t of_row(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }  // 0 from past the row
+constexpr int kFromAbove = 0x100, kFromBelow = 0x110;  // + n: the lane n above, n below
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, of_row<kFromBelow + 1>(v));
+  v = max(v, of_row<kFromBelow + 2>(v));
+  v = max(v, of_row<kFromBelow + 4>(v));
+  v = max(v, of_row<kFromBelow + 8>(v));
+  const uint32_t a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47), d = __builtin_amdgcn_readlane(v, 63);
+  return max(max(a, b), max(c, d));
+}
+// The sum of the lane's value and those of the lanes above it in its row.
+__device__ __forceinline__ uint32_t row_sum_from(uint32_t v) {
+  v += of_row<kFromAbove + 1>(v);
+  v += of_row<kFromAbove + 2>(v);
+  v += of_row<kFromAbove + 4>(v);
+  v += of_row<kFromAbove + 8>(v);
+  return v;
+}
+
+// The sum over the first row's lanes, where the others are of no account.
+__device__ __forceinline__ uint32_t row_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)row_sum_from(v), 0); }
+
 struct SelectParams {
   Requests req;
   const uint16_t* q;
@@ -38,250 +63,316 @@ struct SelectParams {
   int64_t pitch;    // keys of a token and head
   int token0;       // the turn's first token
   uint32_t tiles;   // blocks that score a token and head
-  int in_lds;       // whether the picking kernel has room for a token's keys
   Divisor by_block, by_heads, by_tiles;
 };
 
-// Rows of up to 16 query heads of one token, as the product's rows: lane l holds row l % 16, bytes 64 kk + 16 (l / 16) and on of [q-, q+].
+// The product's 16 rows: row r is query head u0 + r % (16 / TPT) of token row0 + r / (16 / TPT), as [q-, q+] in bytes, and a_u (0 where it counts as zeros).
+template <int D>
+struct QueryLds {
+  static constexpr int kPitch = 2 * D + 16;  // bytes of a row
+  alignas(16) uint8_t code[16][kPitch];
+  float size[16];
+};
+
+// By the first 16 D / 8 threads of a block: 8 channels each, which are loaded ahead.
+template <int D, int TPT>
+__device__ __forceinline__ u32x4 load_queries(const SelectParams& a, int row0, int past, int head, int u0) {
+  constexpr int kLanes = D / 8, kRows = 16 / TPT;
+  const int r = threadIdx.x / kLanes, c = threadIdx.x % kLanes, u = u0 + r % kRows, row = row0 + r / kRows;
+  u32x4 raw = {0, 0, 0, 0};
+  if (r < 16 && u < a.group && row < past) raw = *reinterpret_cast<const u32x4*>(a.q + (int64_t)row * a.q_ts + ((int64_t)head * a.group + u) * D + c * 8);
+  return raw;
+}
+
 template <int DT, int D>
+__device__ __forceinline__ void quantise(const u32x4& raw, QueryLds<D>& lds) {
+  constexpr int kLanes = D / 8;
+  const int r = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  if (r >= 16) return;
+  float x[8], most = 0.0f;
+  widen8<DT>(raw, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (has_odd<DT, KVH_CACHE_16>(raw[e])) most = INFINITY;
+#pragma unroll
+  for (int d = 1; d < kLanes; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  const bool none = !(most < INFINITY) || most < 0x1p-100f;
+  const Part127 part127(none ? 1.0f : most);
+  u32x2 below, above;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = none ? 0.0f : __builtin_rintf(part127.of(x[4 * w + e]));
+    below[w] = four_codes(fminf(v[0], 0.0f), fminf(v[1], 0.0f), fminf(v[2], 0.0f), fminf(v[3], 0.0f));
+    above[w] = four_codes(fmaxf(v[0], 0.0f), fmaxf(v[1], 0.0f), fmaxf(v[2], 0.0f), fmaxf(v[3], 0.0f));
+  }
+  *reinterpret_cast<u32x2*>(&lds.code[r][c * 8]) = below;
+  *reinterpret_cast<u32x2*>(&lds.code[r][D + c * 8]) = above;
+  if (c == 0) lds.size[r] = none ? 0.0f : most;
+}
+
+// A wave's rows of the product: lane l has row l % 16, bytes 64 kk + 16 (l / 16) and on, and the sizes of the four rows whose results it gets.
+template <int D, int TPT>
 struct Queries {
   static constexpr int kSums = 2 * D / 64;
   i32x4 code[kSums];
-  float size;  // a_u of the lane's row; 0 where it counts as zeros
-
-  __device__ __forceinline__ void load(const uint16_t* row, bool real, int grp) {
-    constexpr int kSets = D / 64;  // of 16 channels that the lane holds, for q- and again for q+
-    u32x4 raw[kSets][2];
-    float most = 0.0f;
-    bool odd = false;
+  float size[4];
+  bool real[4];
+  __device__ __forceinline__ Queries(const SelectParams& a, const QueryLds<D>& lds, int u0, int lane) {
 #pragma unroll
-    for (int i = 0; i < kSets; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        raw[i][h] = u32x4{0, 0, 0, 0};
-        if (real) raw[i][h] = *reinterpret_cast<const u32x4*>(row + i * 64 + grp * 16 + h * 8);
-        float x[8];
-        widen8<DT>(raw[i][h], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= has_odd<DT, KVH_CACHE_16>(raw[i][h][e]);
-      }
-    if (odd) most = INFINITY;
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const bool none = !(most < INFINITY) || most < 0x1p-100f;
-    size = none ? 0.0f : most;
-    const Part127 part127(none ? 1.0f : most);
-#pragma unroll
-    for (int i = 0; i < kSets; ++i) {
-      float c[16];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x[8];
-        widen8<DT>(raw[i][h], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) c[8 * h + e] = none ? 0.0f : __builtin_rintf(part127.of(x[e]));
-      }
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float *v = c + 4 * w;
-        code[i][w] = (int32_t)four_codes(fminf(v[0], 0.0f), fminf(v[1], 0.0f), fminf(v[2], 0.0f), fminf(v[3], 0.0f));
-        code[i + kSets][w] = (int32_t)four_codes(fmaxf(v[0], 0.0f), fmaxf(v[1], 0.0f), fmaxf(v[2], 0.0f), fmaxf(v[3], 0.0f));
-      }
-    }
-  }
-};
-
-// What a token asks of its request's pages.
-struct Asked {
-  int end;  // pages that it may choose from
-  __device__ __forceinline__ Asked() : end(0) {}
-  __device__ __forceinline__ Asked(const SelectParams& a, const Request& rq, int row) {
-    const int p = rq.len - rq.n + (row - rq.start);
-    end = p < 0 ? 0 : (int)a.by_block.quotient((uint32_t)p) + 1;
-  }
-};
-
-// The scores of pages [base, base + 64) for TPT tokens, by one wave: lane l looks up page base + l; a product takes 16 of them.  `put(token, page, key)` is called by
-// the lanes that hold a key.  end[i] is 0 for what is no token of the request.
-template <int DT, int D, int TPT, typename Put>
-__device__ __forceinline__ bool score64(const SelectParams& a, const int32_t* table, int head, int base, int most, const int (&end)[TPT], const Queries<DT, D>& first,
-                                        const uint16_t* rows, int lane, Put&& put) {
-  constexpr int kSums = 2 * D / 64, kTiles = 4;
-  const int l16 = lane % 16, grp = lane / 16;
-  int page = -1;
-  if (base + lane < most) page = table[base + lane];
-  const bool there = page >= 0 && page < a.pages;
-  const bool bad = base + lane < most && !there;
-  if (!there) page = 0;
-  i32x4 box[kTiles][kSums];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    const int8_t* from = a.codes + (int64_t)__shfl(page, 16 * t + l16) * a.b_ps + (int64_t)head * 2 * D + grp * 16;
-    if (base + 16 * t < most) {
-#pragma unroll
-      for (int kk = 0; kk < kSums; ++kk) box[t][kk] = *reinterpret_cast<const i32x4*>(from + kk * 64);
-    }
-  }
-  const float scale = a.scale[(int64_t)page * a.bs_ps + head];
-  const uint64_t here = __ballot(there);
-  float best[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) best[t] = -INFINITY;
-  auto take = [&](const Queries<DT, D>& q, int u0) {
-    float size[4];
-    bool real[4];
+    for (int kk = 0; kk < kSums; ++kk) code[kk] = *reinterpret_cast<const i32x4*>(&lds.code[lane % 16][kk * 64 + lane / 16 * 16]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = grp * 4 + i;
-      size[i] = __shfl(q.size, r);
+      const int r = lane / 16 * 4 + i;
+      size[i] = lds.size[r];
       real[i] = u0 + r % (16 / TPT) < a.group;
     }
+  }
+};
+
+// Pages that a token of the request may choose from.
+__device__ __forceinline__ int pages_seen(const SelectParams& a, const Request& rq, int row) {
+  const int p = rq.len - rq.n + (row - rq.start);
+  return p < 0 ? 0 : (int)a.by_block.quotient((uint32_t)p) + 1;
+}
+
+// The scores of pages [base, base + kSpan) for TPT tokens, by one wave, 16 of them a product; entry[t] is the table's entry of page base + 16 t + l % 16 in lane l.  end[i] is
+// 0 for what is no token of the request.  `best_of(token, page)` and `put(token, page, word)` are called by the lanes that hold a score: where the query heads come in
+// several turns of 16, the largest so far is kept as it is, and the last turn makes the key of it.
+constexpr int kTiles = 2, kSpan = 16 * kTiles;
+
+template <int D>
+struct Boxes {
+  static constexpr int kSums = 2 * D / 64;
+  i32x4 box[kTiles][kSums];
+  float scale[kTiles];
+  bool there[kTiles];
+  __device__ __forceinline__ Boxes(const SelectParams& a, const int (&entry)[kTiles], int head, int lane) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      if (base + 16 * t >= most) break;
-      i32x4 dot = {0, 0, 0, 0};
+      there[t] = entry[t] >= 0 && entry[t] < a.pages;
+      const int page = there[t] ? entry[t] : 0;  // (what lies past the last page is read as page 0 and not used: a condition would have each tile wait for the one before)
+      const int8_t* from = a.codes + (int64_t)page * a.b_ps + (int64_t)head * 2 * D + lane / 16 * 16;
 #pragma unroll
-      for (int kk = 0; kk < kSums; ++kk) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.code[kk], box[t][kk], dot, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (real[i]) best[t] = fmaxf(best[t], (float)dot[i] * size[i]);
-    }
-  };
-  take(first, 0);
-  if constexpr (TPT == 1) {
-    for (int u0 = 16; u0 < a.group; u0 += 16) {
-      Queries<DT, D> q;
-      const bool real = u0 + l16 < a.group;
-      q.load(rows + (u0 + (real ? l16 : 0)) * D, real, grp);
-      take(q, u0);
+      for (int kk = 0; kk < kSums; ++kk) box[t][kk] = *reinterpret_cast<const i32x4*>(from + kk * 64);
+      scale[t] = a.scale[(int64_t)page * a.bs_ps + head];
     }
   }
+};
+
+template <int D, int TPT, typename Best, typename Put>
+__device__ __forceinline__ bool score_span(const SelectParams& a, const Boxes<D>& x, int base, int most, const int (&end)[TPT], const Queries<D, TPT>& q,
+                                           bool first, bool last, int lane, Best&& best_of, Put&& put) {
+  constexpr int kSums = 2 * D / 64;
+  const int l16 = lane % 16, grp = lane / 16;
+  bool bad = false;
   const int token = grp * TPT / 4, own = end[token];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    if (base + 16 * t >= most) break;
-    if constexpr (TPT <= 2) best[t] = fmaxf(best[t], __shfl_xor(best[t], 16));
-    if constexpr (TPT == 1) best[t] = fmaxf(best[t], __shfl_xor(best[t], 32));
+    i32x4 dot = {0, 0, 0, 0};
+#pragma unroll
+    for (int kk = 0; kk < kSums; ++kk) dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.code[kk], x.box[t][kk], dot, 0, 0, 0);
+    float best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (q.real[i]) best = fmaxf(best, (float)dot[i] * q.size[i]);
+    if constexpr (TPT == 2) {
+      const f32x2 x = apart16(best);
+      best = fmaxf(x[0], x[1]);
+    }
+    if constexpr (TPT == 1) best = over_groups_max(best);
     const int j = base + 16 * t + l16;
-    const float s = __shfl(scale, 16 * t + l16), score = best[t] * s;
-    uint32_t key = !(score == score) || !(fabsf(s) < INFINITY) ? kInfinite : order_of(score);
+    bad |= j < most && !x.there[t];
+    if (grp % (4 / TPT) != 0 || j >= own) continue;
+    if (!first) best = fmaxf(best, best_of(token, j));
+    if (!last) {
+      put(token, j, __builtin_bit_cast(uint32_t, best));
+      continue;
+    }
+    const float score = best * x.scale[t];
+    uint32_t key = !(score == score) || !(fabsf(x.scale[t]) < INFINITY) ? kInfinite : order_of(score);
     if (j < a.first || j >= own - a.last) key = kAlways;
-    if (grp % (4 / TPT) == 0 && j < own) put(token, j, (here >> (16 * t + l16) & 1u) != 0 ? key : 0u);
+    put(token, j, x.there[t] ? key : 0u);
   }
   return bad;
+}
+
+// The table's entries of pages [base, base + kSpan) as score_span takes them.
+__device__ __forceinline__ void look_up(const int32_t* table, int base, int most, int lane, int (&entry)[kTiles]) {
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const int j = base + 16 * t + lane % 16;
+    entry[t] = j < most ? table[j] : -1;
+  }
 }
 
 // ---- picking ------------------------------------------------------------------------------------------------------
 // W waves choose `count` of n keys; a block has GROUPS such teams, whose barriers are common.  The keys' range is cut into bins and counted, then that of the bin
 // in which the last chosen key lies, until that bin is a single key, or is chosen as a whole.
-constexpr int kLogBins = 10, kBins = 1 << kLogBins;
+constexpr int kLogBins = 10, kBins = 1 << kLogBins, kLaneBins = kBins / kWave;
 
 template <int W, int GROUPS>
 struct PickLds {
-  uint32_t bins[GROUPS][kBins];
-  uint32_t low[GROUPS][W], high[GROUPS][W], some[GROUPS][W], sure[GROUPS][W];
-  uint32_t found[GROUPS][3];
+  alignas(16) uint32_t bins[GROUPS][kBins];
+  uint32_t low[GROUPS][W], high[GROUPS][W], more[GROUPS][W], same[GROUPS][W];
+  uint32_t found[GROUPS][2], open[GROUPS];
 };
 
-template <int W, int GROUPS, typename Keys>
-__device__ __forceinline__ void pick(const Keys& key, int n, int count, int32_t* out, PickLds<W, GROUPS>& lds, int team, int wave, int lane) {
+// The sum of the lane's value and those of all lanes below it, and the sum of all.
+__device__ __forceinline__ uint32_t wave_sum_to(uint32_t v, uint32_t& all) {
+  v += of_row<kFromBelow + 1>(v);
+  v += of_row<kFromBelow + 2>(v);
+  v += of_row<kFromBelow + 4>(v);
+  v += of_row<kFromBelow + 8>(v);
+  const uint32_t a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31), c = b + __builtin_amdgcn_readlane(v, 47), lane = threadIdx.x % kWave;
+  all = c + __builtin_amdgcn_readlane(v, 63);
+  return v + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
+}
+
+// four(g): keys 4 g .. 4 g + 3, 0 past the last one.  The code is short on purpose: it runs once, and its instructions have to be fetched.
+template <int W, int GROUPS, typename Four>
+__device__ __forceinline__ void pick(const Four& four, int n, int count, int first, int last, int32_t* out, PickLds<W, GROUPS>& lds, int team, int wave, int lane) {
   constexpr int kThreads = W * kWave;
-  const int id = wave * kWave + lane;
-  uint32_t low = ~0u, high = 0, some = 0, sure = 0;
-  for (int j0 = wave * kWave; j0 < n; j0 += kThreads) {
-    const uint32_t k = j0 + lane < n ? key(j0 + lane) : 0;
-    const bool candidate = k != 0 && k != kAlways;
-    if (candidate) low = min(low, k), high = max(high, k);
-    some += __popcll(__ballot(candidate)), sure += __popcll(__ballot(k == kAlways));
+  const int groups = (n + 3) / 4, each = (groups + kThreads - 1) / kThreads * kWave, begin = wave * each;  // a wave has a run of the keys
+  const int stop = begin + each < groups ? begin + each : groups;
+  // Those that are chosen in any case lie at the ends; they, and what is no candidate, take no part in the range.
+  uint32_t sure = 0;
+  for (int i = 0; i < first + last; i += kWave) {
+    const int at = i + lane, j = at < first ? at : n - (first + last) + at;
+    sure += __popcll(__ballot(at < first + last && j >= 0 && j < n && (at < first || j >= first) && four(j / 4)[j % 4] == kAlways));
   }
+  uint32_t high = 0, not_low = 0;  // the largest key + 1, and the inverse of the least key - 1, in numbers that wrap
+#pragma unroll 2
+  for (int g = begin + lane; g < stop; g += kWave) {
+    const u32x4 k = four(g);
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    low = min(low, (uint32_t)__shfl_xor((int)low, d));
-    high = max(high, (uint32_t)__shfl_xor((int)high, d));
+    for (int e = 0; e < 4; ++e) high = max(high, k[e] + 1), not_low = max(not_low, ~(k[e] - 1));
   }
-  if (lane == 0) lds.low[team][wave] = low, lds.high[team][wave] = high, lds.some[team][wave] = some, lds.sure[team][wave] = sure;
+  high = wave_max(high), not_low = wave_max(not_low);
+  uint32_t want = (uint32_t)count - sure;  // first + last <= count
+  bool open = n > count && want != 0;
+  if (lane == 0) lds.low[team][wave] = not_low, lds.high[team][wave] = high;
+  if (wave == 0 && lane == 0) lds.open[team] = open;
+#pragma unroll 1
+  for (int i = wave * kWave + lane; i < kBins / 4; i += kThreads) reinterpret_cast<u32x4*>(lds.bins[team])[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
-  some = sure = 0;
+  bool any_open = false;  // of the block's teams, whether one still looks for its least key
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    low = min(low, lds.low[team][w]), high = max(high, lds.high[team][w]);
-    some += lds.some[team][w], sure += lds.sure[team][w];
-  }
-  uint32_t want = (uint32_t)count - sure;         // first + last <= count
+  for (int g = 0; g < GROUPS; ++g) any_open |= lds.open[g] == 1;
+  high = wave_max(lane < W ? lds.high[team][lane] : 0) - 1;  // lane w has what wave w found
+  uint32_t low = ~wave_max(lane < W ? lds.low[team][lane] : 0) + 1;
   uint32_t least = want == 0 ? kAlways - 1 : 0, equal = 0;  // keys above it are chosen, and the first `equal` ones of those that are it
-  bool open = want != 0 && some > want;
-  while (__syncthreads_or(open)) {
-    const int bits = 32 - __builtin_clz((high - low) | 1u), shift = bits > kLogBins ? bits - kLogBins : 0;
-    if (open)
-      for (int i = id; i < kBins; i += kThreads) lds.bins[team][i] = 0;
-    __syncthreads();
-    if (open)
-      for (int j = id; j < n; j += kThreads) {
-        const uint32_t k = key(j);
-        if (k >= low && k <= high) atomicAdd(&lds.bins[team][(k - low) >> shift], 1u);
+#pragma unroll 1
+  while (any_open) {
+    const uint32_t range = high - low;
+    const int bits = 32 - __builtin_clz(range | 1u), shift = bits > kLogBins ? bits - kLogBins : 0;
+    if (open) {
+#pragma unroll 2
+      for (int g = begin + lane; g < stop; g += kWave) {
+        const u32x4 k = four(g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k[e] - low <= range) atomicAdd(&lds.bins[team][(k[e] - low) >> shift], 1u);
       }
+    }
     __syncthreads();
-    if (open && wave == 0) {  // the bin of the want-th from above: a lane has 16 of them
-      constexpr int kMine = kBins / kWave;
-      uint32_t mine[kMine], sum = 0;
+    if (wave == 0) {
+      uint32_t on = 0;  // 1: the search goes on; 2: there are not so many
+      if (open) {  // the bin of the want-th from above: a lane has 16 neighbouring ones
+        uint32_t sum = 0;
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) sum += mine[i] = lds.bins[team][lane * kMine + i];
-      uint32_t above = sum;  // of this lane and those behind it
-#pragma unroll
-      for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t x = __shfl_down(above, d);
-        if (lane + d < kWave) above += x;
-      }
-      above -= sum;
-      if (above < want && above + sum >= want) {
-#pragma unroll
-        for (int i = kMine - 1; i >= 0; --i) {
-          if (above < want && above + mine[i] >= want) lds.found[team][0] = lane * kMine + i, lds.found[team][1] = above, lds.found[team][2] = mine[i];
-          above += mine[i];
+        for (int i = 0; i < kLaneBins / 4; ++i) {
+          const u32x4 x = reinterpret_cast<const u32x4*>(lds.bins[team])[lane * (kLaneBins / 4) + i];
+          sum += x[0] + x[1] + x[2] + x[3];
+        }
+        uint32_t upto = row_sum_from(sum);
+        const uint32_t r1 = __builtin_amdgcn_readlane(upto, 16), r2 = __builtin_amdgcn_readlane(upto, 32), r3 = __builtin_amdgcn_readlane(upto, 48);
+        upto += (lane < 16 ? r1 : 0) + (lane < 32 ? r2 : 0) + (lane < 48 ? r3 : 0);
+        const uint64_t enough = __ballot(upto >= want);
+        if (enough == 0) {
+          on = 2;
+        } else {
+          const int at = 63 - __builtin_clzll(enough);  // the last lane with so many from it on
+          const uint32_t past = (uint32_t)__builtin_amdgcn_readlane(upto - sum, at);
+          const uint32_t mine = lds.bins[team][at * kLaneBins + (lane & (kLaneBins - 1))];
+          const uint32_t from = row_sum_from(mine) + past;
+          const int bin = 63 - __builtin_clzll(__ballot(lane < kLaneBins && from >= want));
+          const uint32_t inside = __builtin_amdgcn_readlane(mine, bin), before = (uint32_t)__builtin_amdgcn_readlane(from, bin) - inside;
+          on = shift != 0 && inside != want - before;
+          if (lane == 0) lds.found[team][0] = (uint32_t)(at * kLaneBins + bin), lds.found[team][1] = before;
         }
       }
+      if (lane == 0) lds.open[team] = on;
     }
     __syncthreads();
-    if (open) {
+    if (open && lds.open[team] == 2) {
+      open = false;  // all candidates: they are above 0
+    } else if (open) {
       want -= lds.found[team][1];
       low += lds.found[team][0] << shift;
-      if (shift == 0)
-        least = low, equal = want, open = false;
-      else if (lds.found[team][2] == want)
-        least = low - 1, open = false;
-      else
+      open = lds.open[team] == 1;
+      if (open)
         high = min(high, low + (1u << shift) - 1);
+      else if (shift == 0)
+        least = low, equal = want;
+      else
+        least = low - 1;
+    }
+    any_open = false;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) any_open |= lds.open[g] == 1;
+    if (any_open) {
+#pragma unroll 1
+      for (int i = wave * kWave + lane; i < kBins / 4; i += kThreads) reinterpret_cast<u32x4*>(lds.bins[team])[i] = u32x4{0, 0, 0, 0};
+      __syncthreads();
     }
   }
-  // The chosen ones in order: a wave has a run of the keys.
-  const int each = (n + kThreads - 1) / kThreads * kWave, begin = wave * each, stop = begin + each < n ? begin + each : n;
+  // Where a wave's chosen keys go, and how many of the equal ones lie before it.
   uint32_t more = 0, same = 0;
-  for (int j0 = begin; j0 < stop; j0 += kWave) {
-    const uint32_t k = j0 + lane < stop ? key(j0 + lane) : 0;
-    more += __popcll(__ballot(k > least)), same += __popcll(__ballot(k == least && k != 0));
-  }
-  if (lane == 0) lds.some[team][wave] = more, lds.sure[team][wave] = same;
-  __syncthreads();
-  uint32_t at = 0, before = 0, total = 0, alike = 0;
+#pragma unroll 2
+  for (int g = begin + lane; g < stop; g += kWave) {
+    const u32x4 k = four(g);
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    if (w == wave) at = total, before = alike;
-    total += lds.some[team][w], alike += lds.sure[team][w];
+    for (int e = 0; e < 4; ++e) more += k[e] > least, same += k[e] == least;
   }
-  at += min(before, equal), total += min(alike, equal);
-  const uint64_t under = ((uint64_t)1 << lane) - 1;
-  for (int j0 = begin; j0 < stop; j0 += kWave) {
-    const uint32_t k = j0 + lane < stop ? key(j0 + lane) : 0;
-    const uint64_t is = __ballot(k == least && k != 0);
-    const bool take = k > least || (k == least && k != 0 && before + __popcll(is & under) < equal);
-    const uint64_t taken = __ballot(take);
-    if (take) out[at + __popcll(taken & under)] = j0 + lane;
-    at += __popcll(taken), before += __popcll(is);
+  uint32_t all_more, all_same;
+  wave_sum_to(more, all_more), wave_sum_to(same, all_same);
+  if (lane == 0) lds.more[team][wave] = all_more, lds.same[team][wave] = all_same;
+  __syncthreads();
+  const uint32_t their_more = lane < W ? lds.more[team][lane] : 0, their_same = lane < W ? lds.same[team][lane] : 0;
+  uint32_t before = row_sum(lane < wave ? their_same : 0), at = row_sum(lane < wave ? their_more : 0) + min(before, equal);
+  const uint32_t total = row_sum(their_more) + min(row_sum(their_same), equal);
+#pragma unroll 1
+  for (int g0 = begin; g0 < stop; g0 += kWave) {
+    u32x4 k = {0, 0, 0, 0};
+    if (g0 + lane < stop) k = four(g0 + lane);
+    uint32_t alike = 0;
+    if (equal != 0) {  // the equal ones that are past the first `equal` become less
+      uint32_t here = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) here += k[e] == least;
+      uint32_t rank = before + wave_sum_to(here, alike) - here;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k[e] == least) k[e] = rank++ < equal ? kAlways : 0;
+    }
+    before += alike;
+    uint32_t mine = 0, all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += k[e] > least;
+    uint32_t to = at + wave_sum_to(mine, all) - mine;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (k[e] > least) out[to++] = 4 * (g0 + lane) + e;
+    at += all;
   }
-  if (out != nullptr)
-    for (int i = (int)total + id; i < count; i += kThreads) out[i] = -1;
+  if (out != nullptr) {
+#pragma unroll 1
+    for (int i = (int)total + wave * kWave + lane; i < count; i += kThreads) out[i] = -1;
+  }
 }
 
 // ---- kernels ------------------------------------------------------------------------------------------------------
@@ -290,21 +381,16 @@ constexpr int kSelectWaves = 8, kSelectThreads = kSelectWaves * kWave;
 // Scores and choice of TPT neighbouring tokens and a head.
 template <int DT, int D, int TPT>
 __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams a) {
-  constexpr int kRows = 16 / TPT, W = kSelectWaves / TPT;  // query heads of a token; waves of a team
+  constexpr int kRows = 16 / TPT, W = kSelectWaves / TPT;  // query heads that a product takes of a token; waves of a team
   __shared__ PickLds<W, TPT> lds;
-  extern __shared__ uint32_t keys[];
-  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave)), l16 = lane % 16, grp = lane / 16;
-  tell_refused(a.req, a.status);
+  __shared__ QueryLds<D> queries;
+  extern __shared__ __align__(16) uint32_t keys[];
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  tell_refused<kSelectThreads>(a.req, a.status);
   const uint32_t tile = a.by_heads.quotient(blockIdx.x);
   const int head = (int)(blockIdx.x - tile * a.heads), row0 = (int)tile * TPT;
   const int past = row0 + TPT < a.req.n_tokens ? row0 + TPT : a.req.n_tokens;
-  const uint16_t* rows = a.q + ((int64_t)row0 + l16 / kRows) * a.q_ts + (int64_t)head * a.group * D;
-  Queries<DT, D> q;
-  {
-    const int u = l16 % kRows;
-    const bool real = u < a.group && row0 + l16 / kRows < past;
-    q.load(real ? rows + u * D : a.q, real, grp);
-  }
+  u32x4 raw = load_queries<D, TPT>(a, row0, past, head, 0);
   for (int row = row0; row < past;) {
     int b;
     Request rq;
@@ -315,12 +401,26 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
     const int stop = rq.start + rq.n < past ? rq.start + rq.n : past;  // the request's rows of this tile
     int end[TPT];
 #pragma unroll
-    for (int i = 0; i < TPT; ++i) end[i] = row0 + i >= row && row0 + i < stop ? Asked(a, rq, row0 + i).end : 0;
-    const int most = Asked(a, rq, stop - 1).end;
+    for (int i = 0; i < TPT; ++i) end[i] = row0 + i >= row && row0 + i < stop ? pages_seen(a, rq, row0 + i) : 0;
+    const int most = pages_seen(a, rq, stop - 1);
     const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
     bool bad = false;
-    for (int base = wave * kWave; base < most; base += kSelectThreads)
-      bad |= score64<DT, D, TPT>(a, table, head, base, most, end, q, rows, lane, [&](int token, int j, uint32_t key) { keys[token * a.pitch + j] = key; });
+    for (int u0 = 0; u0 < a.group; u0 += kRows) {  // (one turn, but where a token has more than 16 query heads)
+      int entry[kTiles];
+      look_up(table, wave * kSpan, most, lane, entry);
+      if (u0 > 0) __syncthreads();
+      quantise<DT, D>(raw, queries);  // while the table's entries are on their way
+      if (kRows < a.group) raw = load_queries<D, TPT>(a, row0, past, head, u0 + kRows < a.group ? u0 + kRows : 0);
+      __syncthreads();
+      const Queries<D, TPT> q(a, queries, u0, lane);
+      for (int base = wave * kSpan; base < most; base += kSelectWaves * kSpan) {
+        const Boxes<D> boxes(a, entry, head, lane);
+        look_up(table, base + kSelectWaves * kSpan, most, lane, entry);
+        bad |= score_span<D, TPT>(a, boxes, base, most, end, q, u0 == 0, u0 + kRows >= a.group, lane,
+                               [&](int token, int j) { return __builtin_bit_cast(float, keys[token * a.pitch + j]); },
+                               [&](int token, int j, uint32_t key) { keys[token * a.pitch + j] = key; });
+      }
+    }
     if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
     __syncthreads();
     const int team = wave / W, mine = row0 + team;
@@ -328,74 +428,104 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
 #pragma unroll
     for (int i = 0; i < TPT; ++i) n = i == team ? end[i] : n;
     int32_t* out = mine >= row && mine < stop ? a.out + ((int64_t)mine * a.heads + head) * a.count : nullptr;
-    const uint32_t* from = keys + team * a.pitch;
-    pick<W, TPT>([&](int j) { return from[j]; }, n, a.count, out, lds, team, wave % W, lane);
+    uint32_t* from = keys + team * a.pitch;
+    if (n + lane < ((n + 3) & ~3)) from[n + lane] = 0;  // (all waves of the team do)
+    __syncthreads();
+    pick<W, TPT>([&](int g) { return reinterpret_cast<const u32x4*>(from)[g]; }, n, a.count, a.first, a.last, out, lds, team, wave % W, lane);
     __syncthreads();
     row = stop;
   }
 }
 
-// Scores of one token and head, 64 pages a wave, to memory.
+constexpr int kScorePages = kWavesPerBlock * kSpan;
+
+// Scores of one token and head, kSpan pages a wave, to memory.
 template <int DT, int D>
 __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
-  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave)), l16 = lane % 16, grp = lane / 16;
+  __shared__ QueryLds<D> queries;
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   if (a.token0 == 0) tell_refused(a.req, a.status);
   const uint32_t unit = a.by_tiles.quotient(blockIdx.x), tile = blockIdx.x - unit * a.tiles;
   const uint32_t token = a.by_heads.quotient(unit);
   const int head = (int)(unit - token * a.heads), row = a.token0 + (int)token;
-  const uint16_t* rows = a.q + (int64_t)row * a.q_ts + (int64_t)head * a.group * D;
-  Queries<DT, D> q;
-  q.load(rows + (l16 < a.group ? l16 : 0) * D, l16 < a.group, grp);
+  u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
   int b;
   Request rq;
   if (!request_of(a.req, row, lane, b, rq)) return;
-  const int end[1] = {Asked(a, rq, row).end};
-  const int base = (int)tile * kBlockThreads + wave * kWave;
-  if (base >= end[0]) return;
+  const int end[1] = {pages_seen(a, rq, row)};
+  if ((int)tile * kScorePages >= end[0]) return;
+  const int base = (int)tile * kScorePages + wave * kSpan;
+  int entry[kTiles];
+  look_up(a.req.table + (int64_t)b * a.req.table_stride, base, end[0], lane, entry);
   uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
-  const bool bad = score64<DT, D, 1>(a, a.req.table + (int64_t)b * a.req.table_stride, head, base, end[0], end, q, rows, lane,
-                                     [&](int, int j, uint32_t key) { keys[j] = key; });
+  bool bad = false;
+  const Boxes<D> boxes(a, entry, head, lane);
+  for (int u0 = 0; u0 < a.group; u0 += 16) {
+    if (u0 > 0) {
+      raw = load_queries<D, 1>(a, row, row + 1, head, u0);
+      __syncthreads();
+    }
+    quantise<DT, D>(raw, queries);
+    __syncthreads();
+    const Queries<D, 1> q(a, queries, u0, lane);
+    bad |= score_span<D, 1>(a, boxes, base, end[0], end, q, u0 == 0, u0 + 16 >= a.group, lane, [&](int, int j) { return __builtin_bit_cast(float, keys[j]); },
+                         [&](int, int j, uint32_t key) { keys[j] = key; });
+  }
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
-constexpr int kPickWaves = 16, kPickThreads = kPickWaves * kWave;
-
-__global__ __launch_bounds__(kPickThreads) void pick_kernel(SelectParams a) {
-  __shared__ PickLds<kPickWaves, 1> lds;
-  extern __shared__ uint32_t mine[];
+template <int W>
+__global__ __launch_bounds__(W * kWave) void pick_kernel(SelectParams a) {
+  constexpr int kThreads = W * kWave, kStaged = 8 * kThreads;
+  __shared__ PickLds<W, 1> lds;
+  __shared__ u32x4 staged[kStaged / 4];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   const uint32_t token = a.by_heads.quotient(blockIdx.x);
   const int head = (int)(blockIdx.x - token * a.heads), row = a.token0 + (int)token;
   int b;
   Request rq;
   if (!request_of(a.req, row, lane, b, rq)) return;
-  const int n = Asked(a, rq, row).end;
+  const int n = pages_seen(a, rq, row);
   const uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
   int32_t* out = a.out + ((int64_t)row * a.heads + head) * a.count;
-  if (a.in_lds) {
-    for (int j = threadIdx.x; j < n; j += kPickThreads) mine[j] = keys[j];
+  const u32x4* fours = reinterpret_cast<const u32x4*>(keys);
+  auto from_memory = [&](int g) {  // (what a row holds past its last key is of no account)
+    u32x4 k = fours[g];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (4 * g + e >= n) k[e] = 0;
+    return k;
+  };
+  if (n <= kStaged) {  // read again and again: from LDS
+    constexpr int kEach = kStaged / 4 / kThreads;
+    u32x4 k[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) k[i] = 4 * (i * kThreads + (int)threadIdx.x) < n ? from_memory(i * kThreads + threadIdx.x) : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) staged[i * kThreads + threadIdx.x] = k[i];
     __syncthreads();
-    pick<kPickWaves, 1>([&](int j) { return mine[j]; }, n, a.count, out, lds, 0, wave, lane);
+    pick<W, 1>([&](int g) { return staged[g]; }, n, a.count, a.first, a.last, out, lds, 0, wave, lane);
   } else {
-    pick<kPickWaves, 1>([&](int j) { return keys[j]; }, n, a.count, out, lds, 0, wave, lane);
+    pick<W, 1>(from_memory, n, a.count, a.first, a.last, out, lds, 0, wave, lane);
   }
 }
 
 // ---- launch -------------------------------------------------------------------------------------------------------
 constexpr int kMostListed = 4096;
 constexpr int kLds = 64 << 10;  // of a block
-constexpr int64_t kFewUnits = 256, kManyPages = 1024;
+constexpr int64_t kFewUnits = 1024, kManyPages = 256;
 
 int64_t pitch_of(int table_pages) { return ((int64_t)table_pages + 3) & ~(int64_t)3; }
 
 // Tokens that share a block's products; 0 where scores go through memory.
 int together(int n_requests, int n_tokens, int heads, int group, int table_pages, bool room) {
   const int64_t keys = pitch_of(table_pages) * (int64_t)sizeof(uint32_t);
-  if (keys + (int64_t)sizeof(PickLds<kSelectWaves, 1>) > kLds) return 0;
+  constexpr int64_t kQueries = sizeof(QueryLds<128>);
+  if (keys + (int64_t)sizeof(PickLds<kSelectWaves, 1>) + kQueries > kLds) return 0;
   if (room && (int64_t)n_tokens * heads < kFewUnits && table_pages > kManyPages) return 0;
   const int64_t each = (int64_t)n_tokens / n_requests;
-  if (each >= 4 && group <= 4 && 4 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 4, 4>) <= kLds) return 4;
-  if (each >= 2 && group <= 8 && 2 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 2, 2>) <= kLds) return 2;
+  if (each >= 4 && group <= 4 && 4 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 4, 4>) + kQueries <= kLds) return 4;
+  if (each >= 2 && group <= 8 && 2 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 2, 2>) + kQueries <= kLds) return 2;
   return 1;
 }
 
@@ -414,8 +544,10 @@ void launch_select(const SelectParams& a, int tokens, hipStream_t stream) {
 template <int DT, int D>
 void launch_score(const SelectParams& a, unsigned tokens, hipStream_t stream) {
   launch_kernel(score_kernel<DT, D>, dim3(tokens * a.heads * a.tiles), dim3(kBlockThreads), 0, stream, a);
-  const unsigned lds = a.in_lds ? (unsigned)(a.pitch * sizeof(uint32_t)) : 0;
-  hipLaunchKernelGGL(pick_kernel, dim3(tokens * a.heads), dim3(kPickThreads), lds, stream, a);
+  if (a.pitch <= 4096)
+    hipLaunchKernelGGL(pick_kernel<8>, dim3(tokens * a.heads), dim3(8 * kWave), 0, stream, a);
+  else
+    hipLaunchKernelGGL(pick_kernel<16>, dim3(tokens * a.heads), dim3(16 * kWave), 0, stream, a);
 }
 
 }  // namespace
@@ -469,8 +601,7 @@ int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* re
   }
   if (turn < 1) return KVH_E_SIZE;
   a.keys = static_cast<uint32_t*>(workspace_dev);
-  a.tiles = (uint32_t)((requests->table_pages + kBlockThreads - 1) / kBlockThreads);
-  a.in_lds = a.pitch * (int64_t)sizeof(uint32_t) + (int64_t)sizeof(PickLds<kPickWaves, 1>) <= kLds;
+  a.tiles = (uint32_t)((requests->table_pages + kScorePages - 1) / kScorePages);
   a.by_tiles = Divisor(a.tiles);
   if ((int64_t)a.heads * a.tiles >= (int64_t)1 << 31) return KVH_E_SHAPE;
   turn = std::min({turn, (int64_t)requests->n_tokens, (((int64_t)1 << 31) - 1) / ((int64_t)a.heads * a.tiles)});
