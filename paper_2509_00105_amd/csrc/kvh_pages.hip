@@ -23,12 +23,14 @@ struct CopyParams {
   uint32_t parts;             // blocks of a page and layer: those of K, those of V, one for the rest
   uint32_t layers;
   Divisor by_parts, by_layers, by_row;
+  int64_t each() const { return (int64_t)parts * layers; }  // blocks of a pair
 };
 
 constexpr int kCopyWords = 4;  // 16-byte words of a thread
+constexpr int64_t kMostBlocks = ((int64_t)1 << 31) - 1;
 
-__global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) {
-  const uint32_t unit = a.by_parts.quotient(blockIdx.x), part = blockIdx.x - unit * a.parts;
+__device__ __forceinline__ void copy_part(const CopyParams& a, uint32_t block) {
+  const uint32_t unit = a.by_parts.quotient(block), part = block - unit * a.parts;
   const uint32_t i = a.by_layers.quotient(unit), layer = unit - i * a.layers;
   const int src = a.src[i], dst = a.dst[i];
   if (src < 0 || src == dst) return;
@@ -73,9 +75,10 @@ __global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) {
   }
 }
 
-// `pairs` of them at most; what bounds and scales there are goes along.
-int launch_copy(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int64_t pairs, int32_t* status, hipStream_t stream) {
-  CopyParams a{};
+__global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) { copy_part(a, blockIdx.x); }
+
+// What bounds and scales there are goes along.
+int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int32_t* status, CopyParams& a) {
   const int width = c.kind == KVH_CACHE_16 ? 2 : 1;
   a.src = src, a.dst = dst, a.status = status;
   a.ck = static_cast<uint8_t*>(c.k), a.cv = static_cast<uint8_t*>(c.v);
@@ -94,11 +97,15 @@ int launch_copy(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, con
   a.parts = (uint32_t)(2 * half + 1);
   a.layers = (uint32_t)c.layers;
   a.by_parts = Divisor(a.parts), a.by_layers = Divisor(a.layers), a.by_row = Divisor(a.row_words);
-  const int64_t each = (int64_t)a.parts * a.layers, most = (((int64_t)1 << 31) - 1) / each;  // pairs of a launch
-  if (most < 1) return KVH_E_SHAPE;
+  return a.each() > kMostBlocks / 2 ? KVH_E_SHAPE : KVH_OK;
+}
+
+// `pairs` of them at most.
+int launch_copy(CopyParams& a, int64_t pairs, hipStream_t stream) {
+  const int64_t most = kMostBlocks / a.each();  // of a launch
   for (int64_t i = 0; i < pairs; i += most) {
     const int64_t n = std::min(most, pairs - i);
-    launch_kernel(copy_kernel, dim3((unsigned)(n * each)), dim3(kBlockThreads), 0, stream, a);
+    launch_kernel(copy_kernel, dim3((unsigned)(n * a.each())), dim3(kBlockThreads), 0, stream, a);
     KVH_HIP_CHECK_LAUNCH();
     a.src += n, a.dst += n;
     if (a.status != nullptr) a.status += n;
@@ -120,81 +127,102 @@ struct RowsParams {
   Divisor by_block;
 };
 
+// What becomes of a row, in the workspace.
+struct Child {
+  int32_t parent;  // -1: none
+  int32_t len;     // tokens after the call
+  int32_t full, kept, after;  // pages that are shared, that are not fresh, and all
+  int32_t ok, copies;  // whether an unfilled page is copied, which is entry `full` of the parent
+  int32_t base;    // its place among the fresh pages; -1 where there are too few
+};
+
 struct ForkParams {
   RowsParams r;
   const int32_t *parents, *grow;
   int32_t* lens_out;
   // workspace
-  int32_t *need, *base;  // of each row: fresh pages it needs; how many rows before it need, or -1 where it is refused
-  int32_t *src, *dst;    // pairs to copy
-  int32_t* fresh;        // free pages in order
+  Child* child;        // of each row
+  int32_t *src, *dst;  // pairs to copy
+  int32_t* fresh;      // free pages in order
 };
 
 __device__ __forceinline__ int pages_of(const RowsParams& r, int tokens) { return tokens > 0 ? (int)r.by_block.quotient((uint32_t)tokens - 1) + 1 : 0; }
-
-// What becomes of row b.
-struct Child {
-  int parent;       // -1: none
-  int old_len, len; // the parent's tokens, and the row's
-  int full, kept, after;  // pages that are shared, that are not fresh, and all
-  bool ok, copies;  // whether an unfilled page is copied
-};
 
 __global__ __launch_bounds__(kBlockThreads) void start_kernel(RowsParams r) {
   const int p = blockIdx.x * kBlockThreads + threadIdx.x;
   if (p < r.pages) r.refs_out[p] = r.refs[p];
 }
 
-// All threads of a block.  The lengths and the entries are checked, and whether the row is the first of its parent's children (those that are not refused here).
-__device__ __forceinline__ Child child_of(const ForkParams& a, int b) {
+// By a wave, or a block of kBlockThreads: whether it holds for one of the threads.
+template <int THREADS>
+__device__ __forceinline__ bool any_of(bool v) {
+  if constexpr (THREADS == kWave)
+    return __any(v);
+  else
+    return __syncthreads_or(v) != 0;
+}
+
+// The lengths and the entries are checked, and whether the row is the first of its parent's children (those that are not refused here).
+template <int THREADS>
+__device__ __forceinline__ Child child_of(const ForkParams& a, int b, int id) {
   const RowsParams& r = a.r;
   Child c;
   c.parent = a.parents == nullptr ? b : a.parents[b];
   if (c.parent < 0) c.parent = -1;
   const int64_t grow = a.grow == nullptr ? 0 : a.grow[b];
   c.ok = c.parent < r.n && grow >= 0;
-  c.old_len = c.ok && c.parent >= 0 ? r.lens[c.parent] : 0;
-  c.ok = c.ok && c.old_len >= 0 && c.old_len + grow <= r.capacity;
-  if (!c.ok) c.old_len = 0;
-  c.len = c.ok ? (int)(c.old_len + grow) : 0;
-  c.full = (int)r.by_block.quotient((uint32_t)c.old_len);
-  const bool open = c.old_len - c.full * r.block_tokens != 0;
+  int old_len = c.ok && c.parent >= 0 ? r.lens[c.parent] : 0;
+  c.ok = c.ok && old_len >= 0 && old_len + grow <= r.capacity;
+  if (!c.ok) old_len = 0;
+  c.len = c.ok ? (int)(old_len + grow) : 0;
+  c.full = (int)r.by_block.quotient((uint32_t)old_len);
+  const bool open = old_len - c.full * r.block_tokens != 0;
   c.after = pages_of(r, c.len);
   bool odd = false, other = false;
-  if (c.parent >= 0) {
+  if (c.ok && c.parent >= 0) {
     const int32_t* from = r.table + (int64_t)c.parent * r.ts;
-    for (int j = threadIdx.x; j < c.full + open; j += kBlockThreads) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
+#pragma unroll 4
+    for (int j = id; j < c.full + open; j += THREADS) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
     if (open && a.parents != nullptr)
-      for (int i = threadIdx.x; i < b; i += kBlockThreads)  // (what a child that is refused would keep is not kept, and may be handed out)
-        if (a.parents[i] == c.parent) other |= a.grow == nullptr || (a.grow[i] >= 0 && c.old_len + (int64_t)a.grow[i] <= r.capacity);
+      for (int i = id; i < b; i += THREADS)  // (what a child that is refused would keep is not kept, and may be handed out)
+        if (a.parents[i] == c.parent) other |= a.grow == nullptr || (a.grow[i] >= 0 && old_len + (int64_t)a.grow[i] <= r.capacity);
   }
-  odd = __syncthreads_or(odd) != 0;
-  other = __syncthreads_or(other) != 0;
-  if (odd) c.ok = false;
+  odd = any_of<THREADS>(odd);
+  other = any_of<THREADS>(other);
+  if (odd) c.ok = 0;
   if (!c.ok) c.len = c.full = c.after = 0;
   c.copies = c.ok && open && other;
   c.kept = c.full + (c.ok && open && !other);
+  c.base = 0;
+  if (id == 0) {
+    a.child[b] = c;
+    if (!c.ok && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
+  }
   return c;
 }
 
-__global__ __launch_bounds__(kBlockThreads) void count_kernel(ForkParams a) {
+// The row's references before the call and after it, but for fresh pages; those of a row that is its own child are the same as far as it keeps them.
+template <int THREADS>
+__device__ __forceinline__ void count_row(const ForkParams& a, int b, const Child& c, int32_t* refs, int id) {
   const RowsParams& r = a.r;
-  const int b = blockIdx.x;
-  const Child c = child_of(a, b);
   const int32_t len = r.lens[b];
+  const int32_t* old = r.table + (int64_t)b * r.ts;
+  const int same = c.parent == b ? c.kept : 0;
   if (len > 0 && len <= r.capacity) {
-    const int32_t* old = r.table + (int64_t)b * r.ts;
-    for (int j = threadIdx.x; j < pages_of(r, len); j += kBlockThreads)
-      if ((uint32_t)old[j] < (uint32_t)r.pages) atomicSub(&r.refs_out[old[j]], 1);
+#pragma unroll 4
+    for (int j = same + id; j < pages_of(r, len); j += THREADS)
+      if ((uint32_t)old[j] < (uint32_t)r.pages) atomicSub(&refs[old[j]], 1);
   }
   if (c.parent >= 0) {
     const int32_t* from = r.table + (int64_t)c.parent * r.ts;
-    for (int j = threadIdx.x; j < c.kept; j += kBlockThreads) atomicAdd(&r.refs_out[from[j]], 1);
+#pragma unroll 4
+    for (int j = same + id; j < c.kept; j += THREADS) atomicAdd(&refs[from[j]], 1);
   }
-  if (threadIdx.x == 0) {
-    a.need[b] = c.after - c.kept;
-    if (!c.ok && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
-  }
+}
+
+__global__ __launch_bounds__(kBlockThreads) void count_kernel(ForkParams a) {
+  const int b = blockIdx.x;
+  count_row<kBlockThreads>(a, b, child_of<kBlockThreads>(a, b, threadIdx.x), a.r.refs_out, threadIdx.x);
 }
 
 constexpr int kScanThreads = 1024, kScanWaves = kScanThreads / kWave;
@@ -220,38 +248,79 @@ __device__ __forceinline__ int64_t before_me(int64_t v, int64_t* lds, int64_t& a
   return base + x - v;
 }
 
-// The free pages in order, and each row's place among those that need some.
-__global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
-  __shared__ int64_t lds[kScanWaves];
+// Each row's place among those that need fresh pages, and these, in order, by one block; refs counts all other references.  A wave has a run of the pages.
+__device__ __forceinline__ void hand_out(const ForkParams& a, int32_t* refs, int64_t* lds) {
   const RowsParams& r = a.r;
-  int64_t many = 0;
-  for (int p0 = 0; p0 < r.pages; p0 += kScanThreads) {
-    const int p = p0 + threadIdx.x;
-    const bool free = p < r.pages && r.refs_out[p] == 0;
-    int64_t all;
-    const int64_t at = many + before_me(free, lds, all);
-    if (free) a.fresh[at] = p;
-    many += all;
-  }
-  int64_t wanted = 0;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int each = (r.pages + kScanThreads - 1) / kScanThreads * kWave, begin = wave * each, stop = begin + each < r.pages ? begin + each : r.pages;
+  int64_t mine = 0, many;
+#pragma unroll 4
+  for (int p = begin; p < stop; p += kWave) mine += __popcll(__ballot(p + lane < stop && refs[p + lane] == 0));
+  int64_t at = before_me(lane == 0 ? mine : 0, lds, many);
+  at = __shfl((long long)at, 0);
+  int64_t wanted = 0, given = 0;
   for (int b0 = 0; b0 < r.n; b0 += kScanThreads) {
     const int b = b0 + threadIdx.x;
-    const int need = b < r.n ? a.need[b] : 0;
+    Child c{};
+    if (b < r.n) c = a.child[b];
+    const int need = c.after - c.kept;
     int64_t all;
-    const int64_t at = wanted + before_me(need, lds, all);
-    if (b < r.n) a.base[b] = need == 0 ? 0 : at + need <= many ? (int32_t)at : -1;
+    const int64_t from = wanted + before_me(need, lds, all), to = from + need;
+    const bool served = need == 0 || to <= many;
+    if (b < r.n) {
+      a.child[b].base = need == 0 ? 0 : served ? (int32_t)from : -1;
+      a.lens_out[b] = served ? c.len : 0;
+      if (!served && r.status != nullptr) r.status[b] = KVH_DEV_NO_PAGES;
+      a.src[b] = served && c.copies ? r.table[(int64_t)c.parent * r.ts + c.full] : -1;
+    }
     wanted += all;
+    before_me(served ? need : 0, lds, all);  // those that are served come first among those that need some
+    given += all;
   }
+  if (at < given) {
+    for (int p = begin; p < stop && at < given; p += kWave) {
+      const bool free = p + lane < stop && refs[p + lane] == 0;
+      const uint64_t who = __ballot(free);
+      const int64_t rank = at + __popcll(who & (((uint64_t)1 << lane) - 1));
+      if (free && rank < given) a.fresh[rank] = p + lane, refs[p + lane] = 1;
+      at += __popcll(who);
+    }
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < r.n; b += kScanThreads) a.dst[b] = a.src[b] >= 0 ? a.fresh[a.child[b].base] : -1;
 }
 
-__global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a) {
+__global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
+  __shared__ int64_t lds[kScanWaves];
+  hand_out(a, a.r.refs_out, lds);
+}
+
+// All of that by one block, with the counts in LDS.
+__global__ __launch_bounds__(kScanThreads) void plan_kernel(ForkParams a) {
+  __shared__ int64_t lds[kScanWaves];
+  extern __shared__ int32_t refs[];
   const RowsParams& r = a.r;
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+#pragma unroll 4
+  for (int p = threadIdx.x; p < r.pages; p += kScanThreads) refs[p] = r.refs[p];
+  __syncthreads();
+  for (int b = wave; b < r.n; b += kScanWaves) count_row<kWave>(a, b, child_of<kWave>(a, b, lane), refs, lane);
+  __syncthreads();
+  hand_out(a, refs, lds);
+#pragma unroll 4
+  for (int p = threadIdx.x; p < r.pages; p += kScanThreads) r.refs_out[p] = refs[p];
+}
+
+// The rows, by the first n blocks, and the copies.
+__global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a, CopyParams copy) {
+  const RowsParams& r = a.r;
+  if (blockIdx.x >= (uint32_t)r.n) return copy_part(copy, blockIdx.x - r.n);
   const int b = blockIdx.x;
-  const Child c = child_of(a, b);
-  const int base = a.base[b];
-  const bool served = base >= 0;
-  const int32_t* from = r.table + (int64_t)(c.parent < 0 ? 0 : c.parent) * r.ts;
+  const Child c = a.child[b];
+  const bool served = c.base >= 0;
+  const int32_t* from = r.table + (int64_t)(c.parent < 0 || !c.ok ? 0 : c.parent) * r.ts;
   int32_t* to = r.table_out + (int64_t)b * r.to_ts;
+#pragma unroll 4
   for (int j = threadIdx.x; j < r.table_pages; j += kBlockThreads) {
     int page = -1;
     if (j < c.kept) {
@@ -261,17 +330,9 @@ __global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a) {
         page = -1;
       }
     } else if (j < c.after && served) {
-      page = a.fresh[base + j - c.kept];
-      r.refs_out[page] = 1;
+      page = a.fresh[c.base + j - c.kept];
     }
     to[j] = page;
-  }
-  if (threadIdx.x == 0) {
-    a.lens_out[b] = served ? c.len : 0;
-    if (!served && r.status != nullptr) r.status[b] = KVH_DEV_NO_PAGES;
-    const bool copies = served && c.copies;
-    a.src[b] = copies ? from[c.full] : -1;
-    a.dst[b] = copies ? a.fresh[base] : -1;
   }
 }
 
@@ -334,6 +395,9 @@ __global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a
   if (bad && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
+constexpr int kPlanPages = 15 << 10;          // whose counts a block has in LDS
+constexpr int64_t kPlanEntries = 512 << 10;   // of the table, that one block looks at
+
 // ---- arguments ----------------------------------------------------------------------------------------------------
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -370,12 +434,14 @@ int kvh_copy_pages(const kvh_cache* cache, const kvh_bounds* bounds, const int32
     if (int rc = check_bounds_of(bounds, cache)) return rc;
   if (n < 0 || n > 1 << 24 || (n > 0 && (src_dev == nullptr || dst_dev == nullptr))) return KVH_E_ARG;
   if (!aligned4(src_dev) || !aligned4(dst_dev)) return KVH_E_ALIGN;
-  return launch_copy(*cache, bounds, src_dev, dst_dev, n, status_dev, static_cast<hipStream_t>(stream));
+  CopyParams a{};
+  if (int rc = copy_params(*cache, bounds, src_dev, dst_dev, status_dev, a)) return rc;
+  return launch_copy(a, n, static_cast<hipStream_t>(stream));
 }
 
 size_t kvh_fork_workspace(int n_requests, int pages) {
   if (n_requests < 1 || n_requests > kMaxRequests || pages < 1) return 0;
-  return ((size_t)4 * n_requests + pages) * sizeof(int32_t);
+  return (size_t)n_requests * (sizeof(Child) + 2 * sizeof(int32_t)) + (size_t)pages * sizeof(int32_t);
 }
 
 int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, const int32_t* parents_dev, const int32_t* grow_dev,
@@ -386,18 +452,27 @@ int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of
   if (!aligned4(lens_out_dev) || !aligned4(parents_dev) || !aligned4(grow_dev) || !aligned4(workspace_dev)) return KVH_E_ALIGN;
   if (workspace_bytes < kvh_fork_workspace(a.r.n, a.r.pages)) return KVH_E_SIZE;
   a.parents = parents_dev, a.grow = grow_dev, a.lens_out = lens_out_dev;
-  a.need = static_cast<int32_t*>(workspace_dev);
-  a.base = a.need + a.r.n, a.src = a.base + a.r.n, a.dst = a.src + a.r.n, a.fresh = a.dst + a.r.n;
+  a.child = static_cast<Child*>(workspace_dev);
+  a.src = reinterpret_cast<int32_t*>(a.child + a.r.n), a.dst = a.src + a.r.n, a.fresh = a.dst + a.r.n;
+  CopyParams copy{};
+  if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
+  const int64_t copies = std::min<int64_t>(a.r.n, (kMostBlocks - a.r.n) / copy.each());  // that share the rows' launch
   hipStream_t s = static_cast<hipStream_t>(stream);
-  launch_kernel(start_kernel, dim3((unsigned)(((int64_t)a.r.pages + kBlockThreads - 1) / kBlockThreads)), dim3(kBlockThreads), 0, s, a.r);
+  if (a.r.pages <= kPlanPages && (int64_t)a.r.n * a.r.table_pages <= kPlanEntries) {
+    launch_kernel(plan_kernel, dim3(1), dim3(kScanThreads), (unsigned)(a.r.pages * sizeof(int32_t)), s, a);
+    KVH_HIP_CHECK_LAUNCH();
+  } else {
+    launch_kernel(start_kernel, dim3((unsigned)(((int64_t)a.r.pages + kBlockThreads - 1) / kBlockThreads)), dim3(kBlockThreads), 0, s, a.r);
+    KVH_HIP_CHECK_LAUNCH();
+    hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
+    KVH_HIP_CHECK_LAUNCH();
+    hipLaunchKernelGGL(hand_out_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
+    KVH_HIP_CHECK_LAUNCH();
+  }
+  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(a.r.n + copies * copy.each())), dim3(kBlockThreads), 0, s, a, copy);
   KVH_HIP_CHECK_LAUNCH();
-  hipLaunchKernelGGL(count_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
-  KVH_HIP_CHECK_LAUNCH();
-  hipLaunchKernelGGL(hand_out_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
-  KVH_HIP_CHECK_LAUNCH();
-  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
-  KVH_HIP_CHECK_LAUNCH();
-  return launch_copy(*cache, bounds, a.src, a.dst, a.r.n, nullptr, s);
+  copy.src += copies, copy.dst += copies;
+  return launch_copy(copy, a.r.n - copies, s);
 }
 
 size_t kvh_compact_workspace(int pages) { return pages < 1 ? 0 : (size_t)2 * (pages / 2 + 1) * sizeof(int32_t); }
@@ -411,12 +486,14 @@ int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows
   if (workspace_bytes < kvh_compact_workspace(a.r.pages)) return KVH_E_SIZE;
   a.moved = moved_out_dev;
   a.src = static_cast<int32_t*>(workspace_dev), a.dst = a.src + a.r.pages / 2 + 1;
+  CopyParams copy{};
+  if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   launch_kernel(place_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
   KVH_HIP_CHECK_LAUNCH();
   hipLaunchKernelGGL(renumber_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
   KVH_HIP_CHECK_LAUNCH();
-  return launch_copy(*cache, bounds, a.src, a.dst, a.r.pages / 2, nullptr, s);
+  return launch_copy(copy, a.r.pages / 2, s);
 }
 
 }  // extern "C"

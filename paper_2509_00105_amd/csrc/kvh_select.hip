@@ -62,8 +62,8 @@ struct SelectParams {
   uint32_t* keys;   // [token of this turn][head][pitch], where they go through memory
   int64_t pitch;    // keys of a token and head
   int token0;       // the turn's first token
-  uint32_t tiles;   // blocks that score a token and head
-  Divisor by_block, by_heads, by_tiles;
+  uint32_t units;   // tokens and heads of this turn
+  Divisor by_block, by_heads, by_units;
 };
 
 // The product's 16 rows: row r is query head u0 + r % (16 / TPT) of token row0 + r / (16 / TPT), as [q-, q+] in bytes, and a_u (0 where it counts as zeros).
@@ -437,29 +437,29 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
   }
 }
 
-constexpr int kScorePages = kWavesPerBlock * kSpan;
+constexpr int kScoreTurns = 2, kScorePages = kScoreTurns * kWavesPerBlock * kSpan;
 
-// Scores of one token and head, kSpan pages a wave, to memory.
+// Scores of one token and head, kScoreTurns times kSpan pages a wave, to memory.
 template <int DT, int D>
 __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
   __shared__ QueryLds<D> queries;
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   if (a.token0 == 0) tell_refused(a.req, a.status);
-  const uint32_t unit = a.by_tiles.quotient(blockIdx.x), tile = blockIdx.x - unit * a.tiles;
+  const uint32_t tile = a.by_units.quotient(blockIdx.x), unit = blockIdx.x - tile * a.units;  // the tiles that few requests reach come last
   const uint32_t token = a.by_heads.quotient(unit);
   const int head = (int)(unit - token * a.heads), row = a.token0 + (int)token;
-  u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
   int b;
   Request rq;
   if (!request_of(a.req, row, lane, b, rq)) return;
-  const int end[1] = {pages_seen(a, rq, row)};
-  if ((int)tile * kScorePages >= end[0]) return;
-  const int base = (int)tile * kScorePages + wave * kSpan;
-  int entry[kTiles];
-  look_up(a.req.table + (int64_t)b * a.req.table_stride, base, end[0], lane, entry);
+  const int end[1] = {pages_seen(a, rq, row)}, first = (int)tile * kScorePages;
+  if (first >= end[0]) return;
+  u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
+  const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
+  int entry[kScoreTurns][kTiles];
+#pragma unroll
+  for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, end[0], lane, entry[i]);
   uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
   bool bad = false;
-  const Boxes<D> boxes(a, entry, head, lane);
   for (int u0 = 0; u0 < a.group; u0 += 16) {
     if (u0 > 0) {
       raw = load_queries<D, 1>(a, row, row + 1, head, u0);
@@ -468,8 +468,14 @@ __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
     quantise<DT, D>(raw, queries);
     __syncthreads();
     const Queries<D, 1> q(a, queries, u0, lane);
-    bad |= score_span<D, 1>(a, boxes, base, end[0], end, q, u0 == 0, u0 + 16 >= a.group, lane, [&](int, int j) { return __builtin_bit_cast(float, keys[j]); },
-                         [&](int, int j, uint32_t key) { keys[j] = key; });
+#pragma unroll
+    for (int i = 0; i < kScoreTurns; ++i) {
+      const int base = first + (i * kWavesPerBlock + wave) * kSpan;
+      if (base >= end[0]) break;
+      const Boxes<D> boxes(a, entry[i], head, lane);
+      bad |= score_span<D, 1>(a, boxes, base, end[0], end, q, u0 == 0, u0 + 16 >= a.group, lane, [&](int, int j) { return __builtin_bit_cast(float, keys[j]); },
+                              [&](int, int j, uint32_t key) { keys[j] = key; });
+    }
   }
   if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
 }
@@ -542,12 +548,12 @@ void launch_select(const SelectParams& a, int tokens, hipStream_t stream) {
 }
 
 template <int DT, int D>
-void launch_score(const SelectParams& a, unsigned tokens, hipStream_t stream) {
-  launch_kernel(score_kernel<DT, D>, dim3(tokens * a.heads * a.tiles), dim3(kBlockThreads), 0, stream, a);
+void launch_score(const SelectParams& a, int64_t tiles, hipStream_t stream) {
+  launch_kernel(score_kernel<DT, D>, dim3((unsigned)(a.units * tiles)), dim3(kBlockThreads), 0, stream, a);
   if (a.pitch <= 4096)
-    hipLaunchKernelGGL(pick_kernel<8>, dim3(tokens * a.heads), dim3(8 * kWave), 0, stream, a);
+    hipLaunchKernelGGL(pick_kernel<8>, dim3(a.units), dim3(8 * kWave), 0, stream, a);
   else
-    hipLaunchKernelGGL(pick_kernel<16>, dim3(tokens * a.heads), dim3(16 * kWave), 0, stream, a);
+    hipLaunchKernelGGL(pick_kernel<16>, dim3(a.units), dim3(16 * kWave), 0, stream, a);
 }
 
 }  // namespace
@@ -601,17 +607,18 @@ int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* re
   }
   if (turn < 1) return KVH_E_SIZE;
   a.keys = static_cast<uint32_t*>(workspace_dev);
-  a.tiles = (uint32_t)((requests->table_pages + kScorePages - 1) / kScorePages);
-  a.by_tiles = Divisor(a.tiles);
-  if ((int64_t)a.heads * a.tiles >= (int64_t)1 << 31) return KVH_E_SHAPE;
-  turn = std::min({turn, (int64_t)requests->n_tokens, (((int64_t)1 << 31) - 1) / ((int64_t)a.heads * a.tiles)});
+  const int64_t tiles = ((int64_t)requests->table_pages + kScorePages - 1) / kScorePages;
+  if (a.heads * tiles >= (int64_t)1 << 31) return KVH_E_SHAPE;
+  turn = std::min({turn, (int64_t)requests->n_tokens, (((int64_t)1 << 31) - 1) / (a.heads * tiles)});
   for (int64_t t0 = 0; t0 < requests->n_tokens; t0 += turn) {
     a.token0 = (int)t0;
     const unsigned here = (unsigned)std::min<int64_t>(turn, requests->n_tokens - t0);
+    a.units = here * a.heads;
+    a.by_units = Divisor(a.units);
     if (f16)
-      wide ? launch_score<KVH_F16, 128>(a, here, s) : launch_score<KVH_F16, 64>(a, here, s);
+      wide ? launch_score<KVH_F16, 128>(a, tiles, s) : launch_score<KVH_F16, 64>(a, tiles, s);
     else
-      wide ? launch_score<KVH_BF16, 128>(a, here, s) : launch_score<KVH_BF16, 64>(a, here, s);
+      wide ? launch_score<KVH_BF16, 128>(a, tiles, s) : launch_score<KVH_BF16, 64>(a, tiles, s);
     KVH_HIP_CHECK_LAUNCH();
   }
   return KVH_OK;
