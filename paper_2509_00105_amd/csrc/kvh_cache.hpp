@@ -119,6 +119,42 @@ __device__ __forceinline__ float over_groups_sum(float v) {
   return over_halves_sum(x[0] + x[1]);
 }
 
+// Lanes of a row of 16 exchange by moves; rows through scalar registers.
+template <int CTRL>
+__device__ __forceinline__ uint32_t of_row(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }  // 0 from past the row
+constexpr int kFromAbove = 0x100, kFromBelow = 0x110;  // + n: the lane n above, n below
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, of_row<kFromBelow + 1>(v));
+  v = max(v, of_row<kFromBelow + 2>(v));
+  v = max(v, of_row<kFromBelow + 4>(v));
+  v = max(v, of_row<kFromBelow + 8>(v));
+  const uint32_t a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47), d = __builtin_amdgcn_readlane(v, 63);
+  return max(max(a, b), max(c, d));
+}
+// The sum of the lane's value and those of the lanes above it in its row.
+__device__ __forceinline__ uint32_t row_sum_from(uint32_t v) {
+  v += of_row<kFromAbove + 1>(v);
+  v += of_row<kFromAbove + 2>(v);
+  v += of_row<kFromAbove + 4>(v);
+  v += of_row<kFromAbove + 8>(v);
+  return v;
+}
+
+// The sum over the first row's lanes, where the others are of no account.
+__device__ __forceinline__ uint32_t row_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)row_sum_from(v), 0); }
+
+// The sum of the lane's value and those of all lanes below it, and the sum of all.
+__device__ __forceinline__ uint32_t wave_sum_to(uint32_t v, uint32_t& all) {
+  v += of_row<kFromBelow + 1>(v);
+  v += of_row<kFromBelow + 2>(v);
+  v += of_row<kFromBelow + 4>(v);
+  v += of_row<kFromBelow + 8>(v);
+  const uint32_t a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31), c = b + __builtin_amdgcn_readlane(v, 47), lane = threadIdx.x % kWave;
+  all = c + __builtin_amdgcn_readlane(v, 63);
+  return v + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
+}
+
 // The request that a row of the packed tensors belongs to; all lanes of a wave ask for the same row.  False where it is in none, or in one that is refused.
 __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
   int32_t start, end, len;

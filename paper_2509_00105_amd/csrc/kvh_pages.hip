@@ -153,76 +153,68 @@ __global__ __launch_bounds__(kBlockThreads) void start_kernel(RowsParams r) {
   if (p < r.pages) r.refs_out[p] = r.refs[p];
 }
 
-// By a wave, or a block of kBlockThreads: whether it holds for one of the threads.
-template <int THREADS>
-__device__ __forceinline__ bool any_of(bool v) {
-  if constexpr (THREADS == kWave)
-    return __any(v);
-  else
-    return __syncthreads_or(v) != 0;
-}
-
-// The lengths and the entries are checked, and whether the row is the first of its parent's children (those that are not refused here).
-template <int THREADS>
-__device__ __forceinline__ Child child_of(const ForkParams& a, int b, int id) {
+// A row's child as its numbers say, without a look at the table and at the other rows; `tokens` are the parent's.
+__device__ __forceinline__ Child child_of(const ForkParams& a, int b, int& tokens, bool& open) {
   const RowsParams& r = a.r;
-  Child c;
+  Child c{};
   c.parent = a.parents == nullptr ? b : a.parents[b];
   if (c.parent < 0) c.parent = -1;
   const int64_t grow = a.grow == nullptr ? 0 : a.grow[b];
   c.ok = c.parent < r.n && grow >= 0;
-  int old_len = c.ok && c.parent >= 0 ? r.lens[c.parent] : 0;
-  c.ok = c.ok && old_len >= 0 && old_len + grow <= r.capacity;
-  if (!c.ok) old_len = 0;
-  c.len = c.ok ? (int)(old_len + grow) : 0;
-  c.full = (int)r.by_block.quotient((uint32_t)old_len);
-  const bool open = old_len - c.full * r.block_tokens != 0;
+  tokens = c.ok && c.parent >= 0 ? r.lens[c.parent] : 0;
+  c.ok = c.ok && tokens >= 0 && tokens + grow <= r.capacity;
+  if (!c.ok) tokens = 0;
+  c.len = c.ok ? (int)(tokens + grow) : 0;
+  c.full = (int)r.by_block.quotient((uint32_t)tokens);
+  open = tokens - c.full * r.block_tokens != 0;
   c.after = pages_of(r, c.len);
-  bool odd = false, other = false;
-  if (c.ok && c.parent >= 0) {
-    const int32_t* from = r.table + (int64_t)c.parent * r.ts;
-#pragma unroll 4
-    for (int j = id; j < c.full + open; j += THREADS) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
-    if (open && a.parents != nullptr)
-      for (int i = id; i < b; i += THREADS)  // (what a child that is refused would keep is not kept, and may be handed out)
-        if (a.parents[i] == c.parent) other |= a.grow == nullptr || (a.grow[i] >= 0 && old_len + (int64_t)a.grow[i] <= r.capacity);
-  }
-  odd = any_of<THREADS>(odd);
-  other = any_of<THREADS>(other);
+  return c;
+}
+// With what the table says - an entry of the parent's is none of the cache's - and whether a row before it has the parent's unfilled page.
+__device__ __forceinline__ void settle(const ForkParams& a, int b, Child& c, bool open, bool odd, bool other) {
   if (odd) c.ok = 0;
   if (!c.ok) c.len = c.full = c.after = 0;
   c.copies = c.ok && open && other;
   c.kept = c.full + (c.ok && open && !other);
-  c.base = 0;
-  if (id == 0) {
-    a.child[b] = c;
-    if (!c.ok && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
-  }
-  return c;
+  a.child[b] = c;
+  if (!c.ok && a.r.status != nullptr) a.r.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
 // The row's references before the call and after it, but for fresh pages; those of a row that is its own child are the same as far as it keeps them.
 template <int THREADS>
-__device__ __forceinline__ void count_row(const ForkParams& a, int b, const Child& c, int32_t* refs, int id) {
-  const RowsParams& r = a.r;
-  const int32_t len = r.lens[b];
+__device__ __forceinline__ void count_row(const RowsParams& r, int b, int len, int parent, int kept, int32_t* refs, int id) {
   const int32_t* old = r.table + (int64_t)b * r.ts;
-  const int same = c.parent == b ? c.kept : 0;
+  const int same = parent == b ? kept : 0;
   if (len > 0 && len <= r.capacity) {
 #pragma unroll 4
     for (int j = same + id; j < pages_of(r, len); j += THREADS)
       if ((uint32_t)old[j] < (uint32_t)r.pages) atomicSub(&refs[old[j]], 1);
   }
-  if (c.parent >= 0) {
-    const int32_t* from = r.table + (int64_t)c.parent * r.ts;
+  if (parent >= 0) {
+    const int32_t* from = r.table + (int64_t)parent * r.ts;
 #pragma unroll 4
-    for (int j = same + id; j < c.kept; j += THREADS) atomicAdd(&refs[from[j]], 1);
+    for (int j = same + id; j < kept; j += THREADS) atomicAdd(&refs[from[j]], 1);
   }
 }
 
 __global__ __launch_bounds__(kBlockThreads) void count_kernel(ForkParams a) {
+  const RowsParams& r = a.r;
   const int b = blockIdx.x;
-  count_row<kBlockThreads>(a, b, child_of<kBlockThreads>(a, b, threadIdx.x), a.r.refs_out, threadIdx.x);
+  int tokens;
+  bool open, odd = false, other = false;
+  Child c = child_of(a, b, tokens, open);
+  if (c.ok && c.parent >= 0) {
+    const int32_t* from = r.table + (int64_t)c.parent * r.ts;
+    for (int j = threadIdx.x; j < c.full + open; j += kBlockThreads) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
+    if (open && a.parents != nullptr)
+      for (int i = threadIdx.x; i < b; i += kBlockThreads)  // (what a child that is refused would keep is not kept, and may be handed out)
+        if (a.parents[i] == c.parent) other |= a.grow == nullptr || (a.grow[i] >= 0 && tokens + (int64_t)a.grow[i] <= r.capacity);
+  }
+  odd = __syncthreads_or(odd) != 0;
+  other = __syncthreads_or(other) != 0;
+  if (threadIdx.x == 0) settle(a, b, c, open, odd, other);
+  const bool ok = c.ok && !odd;
+  count_row<kBlockThreads>(r, b, r.lens[b], c.parent, ok ? c.full + (open && !other) : 0, r.refs_out, threadIdx.x);
 }
 
 constexpr int kScanThreads = 1024, kScanWaves = kScanThreads / kWave;
@@ -248,65 +240,131 @@ __device__ __forceinline__ int64_t before_me(int64_t v, int64_t* lds, int64_t& a
   return base + x - v;
 }
 
-// Each row's place among those that need fresh pages, and these, in order, by one block; refs counts all other references.  A wave has a run of the pages.
-__device__ __forceinline__ void hand_out(const ForkParams& a, int32_t* refs, int64_t* lds) {
-  const RowsParams& r = a.r;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int each = (r.pages + kScanThreads - 1) / kScanThreads * kWave, begin = wave * each, stop = begin + each < r.pages ? begin + each : r.pages;
-  int64_t mine = 0, many;
+// How many pages of a wave's run are free: refs counts all references but those to fresh pages.
+struct Run {
+  int begin, stop;
+  __device__ __forceinline__ explicit Run(int pages) {
+    const int each = (pages + kScanThreads - 1) / kScanThreads * kWave;
+    begin = uniform((int32_t)(threadIdx.x / kWave)) * each;
+    stop = begin + each < pages ? begin + each : pages;
+  }
+  __device__ __forceinline__ uint32_t count(const int32_t* refs, int lane) const {
+    uint32_t n = 0;
 #pragma unroll 4
-  for (int p = begin; p < stop; p += kWave) mine += __popcll(__ballot(p + lane < stop && refs[p + lane] == 0));
-  int64_t at = before_me(lane == 0 ? mine : 0, lds, many);
-  at = __shfl((long long)at, 0);
-  int64_t wanted = 0, given = 0;
+    for (int p = begin; p < stop; p += kWave) n += __popcll(__ballot(p + lane < stop && refs[p + lane] == 0));
+    return n;
+  }
+  // The first `given` free pages of all, from the at-th on, and the counts of what is handed out.
+  __device__ __forceinline__ void give(int32_t* refs, int32_t* fresh, int64_t at, int64_t given, int lane) const {
+    for (int p = begin; p < stop && at < given; p += kWave) {
+      const bool free = p + lane < stop && refs[p + lane] == 0;
+      const uint64_t who = __ballot(free);
+      const int64_t rank = at + __popcll(who & (((uint64_t)1 << lane) - 1));
+      if (free && rank < given) fresh[rank] = p + lane, refs[p + lane] = 1;
+      at += __popcll(who);
+    }
+  }
+};
+
+// What a row gets, which needs `need` fresh pages after `from` of the rows before it, of `many`.  Rows that get some come first among those that need some.
+__device__ __forceinline__ bool serve(const ForkParams& a, int b, const Child& c, int64_t from, int64_t many) {
+  const int need = c.after - c.kept;
+  const bool served = need == 0 || from + need <= many;
+  a.child[b].base = need == 0 ? 0 : served ? (int32_t)from : -1;
+  a.lens_out[b] = served ? c.len : 0;
+  if (!served && a.r.status != nullptr) a.r.status[b] = KVH_DEV_NO_PAGES;
+  a.src[b] = served && c.copies ? a.r.table[(int64_t)c.parent * a.r.ts + c.full] : -1;
+  return served;
+}
+
+__global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
+  __shared__ int64_t lds[kScanWaves];
+  const RowsParams& r = a.r;
+  const int lane = threadIdx.x % kWave;
+  const Run run(r.pages);
+  const uint32_t mine = run.count(r.refs_out, lane);
+  int64_t many, wanted = 0, given = 0, all;
+  const int64_t at = before_me(lane == 0 ? mine : 0, lds, many) - (lane == 0 ? 0 : mine);
   for (int b0 = 0; b0 < r.n; b0 += kScanThreads) {
     const int b = b0 + threadIdx.x;
     Child c{};
     if (b < r.n) c = a.child[b];
     const int need = c.after - c.kept;
-    int64_t all;
-    const int64_t from = wanted + before_me(need, lds, all), to = from + need;
-    const bool served = need == 0 || to <= many;
-    if (b < r.n) {
-      a.child[b].base = need == 0 ? 0 : served ? (int32_t)from : -1;
-      a.lens_out[b] = served ? c.len : 0;
-      if (!served && r.status != nullptr) r.status[b] = KVH_DEV_NO_PAGES;
-      a.src[b] = served && c.copies ? r.table[(int64_t)c.parent * r.ts + c.full] : -1;
-    }
+    const int64_t from = wanted + before_me(need, lds, all);
     wanted += all;
-    before_me(served ? need : 0, lds, all);  // those that are served come first among those that need some
+    const bool served = b < r.n && serve(a, b, c, from, many);
+    before_me(served ? need : 0, lds, all);
     given += all;
   }
-  if (at < given) {
-    for (int p = begin; p < stop && at < given; p += kWave) {
-      const bool free = p + lane < stop && refs[p + lane] == 0;
-      const uint64_t who = __ballot(free);
-      const int64_t rank = at + __popcll(who & (((uint64_t)1 << lane) - 1));
-      if (free && rank < given) a.fresh[rank] = p + lane, refs[p + lane] = 1;
-      at += __popcll(who);
-    }
-  }
+  run.give(r.refs_out, a.fresh, at, given, lane);
   __syncthreads();
   for (int b = threadIdx.x; b < r.n; b += kScanThreads) a.dst[b] = a.src[b] >= 0 ? a.fresh[a.child[b].base] : -1;
 }
 
-__global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
-  __shared__ int64_t lds[kScanWaves];
-  hand_out(a, a.r.refs_out, lds);
-}
+// All of that by one block, with the counts in LDS, for kScanThreads rows at most: thread b has row b.
+struct PlanRow {
+  int32_t parent, limit;  // whose entries are looked at, and how many
+  int32_t len, kept;
+  int32_t first, odd;     // of its own children, the first one; whether an entry is none of the cache's
+};
 
-// All of that by one block, with the counts in LDS.
 __global__ __launch_bounds__(kScanThreads) void plan_kernel(ForkParams a) {
-  __shared__ int64_t lds[kScanWaves];
-  extern __shared__ int32_t refs[];
+  __shared__ uint32_t free_of[kScanWaves], need_of[kScanWaves], given_of[kScanWaves];
+  extern __shared__ int32_t plan_lds[];
   const RowsParams& r = a.r;
-  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  PlanRow* rows = reinterpret_cast<PlanRow*>(plan_lds);
+  int32_t* refs = plan_lds + r.n * (int)(sizeof(PlanRow) / sizeof(int32_t));
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave)), b = threadIdx.x;
+  const bool real = b < r.n;
+  Child c{};
+  int tokens = 0;
+  bool open = false;
+  if (real) {
+    rows[b].first = INT32_MAX, rows[b].odd = 0;
+    rows[b].len = r.lens[b];
+    c = child_of(a, b, tokens, open);
+    rows[b].parent = c.parent;
+    rows[b].limit = c.ok && c.parent >= 0 ? c.full + open : 0;
+  }
 #pragma unroll 4
   for (int p = threadIdx.x; p < r.pages; p += kScanThreads) refs[p] = r.refs[p];
   __syncthreads();
-  for (int b = wave; b < r.n; b += kScanWaves) count_row<kWave>(a, b, child_of<kWave>(a, b, lane), refs, lane);
+  if (real && c.ok && c.parent >= 0) atomicMin(&rows[c.parent].first, b);  // (what a child that is refused here would keep is not kept, and may be handed out)
+  for (int i = wave; i < r.n; i += kScanWaves) {
+    const int limit = uniform(rows[i].limit);
+    const int32_t* from = r.table + (int64_t)uniform(rows[i].parent) * r.ts;
+    bool odd = false;
+#pragma unroll 8
+    for (int j = lane; j < limit; j += kWave) odd |= (uint32_t)from[j] >= (uint32_t)r.pages;
+    if (odd) rows[i].odd = 1;
+  }
   __syncthreads();
-  hand_out(a, refs, lds);
+  if (real) {
+    settle(a, b, c, open, rows[b].odd != 0, c.parent >= 0 && c.parent < r.n && rows[c.parent].first < b);
+    rows[b].kept = c.kept;
+  }
+  __syncthreads();
+  for (int i = wave; i < r.n; i += kScanWaves) {
+    const int kept = uniform(rows[i].kept), len = uniform(rows[i].len), parent = uniform(rows[i].parent);
+    count_row<kWave>(r, i, len, kept > 0 ? parent : -1, kept, refs, lane);
+  }
+  const int need = c.after - c.kept;
+  uint32_t sum;
+  const uint32_t before = wave_sum_to((uint32_t)need, sum) - (uint32_t)need;
+  __syncthreads();
+  const Run run(r.pages);
+  const uint32_t mine = run.count(refs, lane);
+  if (lane == 0) free_of[wave] = mine, need_of[wave] = sum;
+  __syncthreads();
+  const uint32_t frees = lane < kScanWaves ? free_of[lane] : 0, needs = lane < kScanWaves ? need_of[lane] : 0;
+  const uint32_t many = row_sum(frees), at = row_sum(lane < wave ? frees : 0), from = row_sum(lane < wave ? needs : 0) + before;
+  const bool served = real && serve(a, b, c, from, many);
+  const uint32_t most = wave_max(served && need != 0 ? from + need : 0);
+  if (lane == 0) given_of[wave] = most;
+  __syncthreads();
+  run.give(refs, a.fresh, at, wave_max(lane < kScanWaves ? given_of[lane] : 0), lane);
+  __syncthreads();
+  if (real) a.dst[b] = served && c.copies ? a.fresh[from] : -1;
 #pragma unroll 4
   for (int p = threadIdx.x; p < r.pages; p += kScanThreads) r.refs_out[p] = refs[p];
 }
@@ -395,8 +453,8 @@ __global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a
   if (bad && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
-constexpr int kPlanPages = 15 << 10;          // whose counts a block has in LDS
-constexpr int64_t kPlanEntries = 512 << 10;   // of the table, that one block looks at
+constexpr int64_t kPlanLds = 63 << 10;        // of a block that plans by itself
+constexpr int64_t kPlanEntries = 512 << 10;   // of the table, that it looks at
 
 // ---- arguments ----------------------------------------------------------------------------------------------------
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -458,8 +516,9 @@ int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of
   if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
   const int64_t copies = std::min<int64_t>(a.r.n, (kMostBlocks - a.r.n) / copy.each());  // that share the rows' launch
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a.r.pages <= kPlanPages && (int64_t)a.r.n * a.r.table_pages <= kPlanEntries) {
-    launch_kernel(plan_kernel, dim3(1), dim3(kScanThreads), (unsigned)(a.r.pages * sizeof(int32_t)), s, a);
+  const int64_t lds = (int64_t)a.r.pages * sizeof(int32_t) + (int64_t)a.r.n * sizeof(PlanRow);
+  if (a.r.n <= kScanThreads && lds <= kPlanLds && (int64_t)a.r.n * a.r.table_pages <= kPlanEntries) {
+    launch_kernel(plan_kernel, dim3(1), dim3(kScanThreads), (unsigned)lds, s, a);
     KVH_HIP_CHECK_LAUNCH();
   } else {
     launch_kernel(start_kernel, dim3((unsigned)(((int64_t)a.r.pages + kBlockThreads - 1) / kBlockThreads)), dim3(kBlockThreads), 0, s, a.r);
