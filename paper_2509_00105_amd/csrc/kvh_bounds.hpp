@@ -16,4 +16,16 @@ struct Part127 {
   __device__ __forceinline__ float of(float x) const { return x * (127.0f / 128.0f) / by; }
 };
 
+// Its floor and ceiling without a division each: the nearest whole number n of a quotient that is off by 2^-16 at most is one of the two, or the quotient itself,
+// and the sign of x - n a says which (the fused product and sum is rounded once, which leaves a sign as it is).
+struct Around127 {
+  float by, inv;
+  __device__ __forceinline__ explicit Around127(float a) : by(a * (1.0f / 128.0f)), inv(1.0f / by) {}
+  __device__ __forceinline__ float down(float x) const {
+    const float y = x * (127.0f / 128.0f), n = __builtin_rintf(y * inv);
+    return __builtin_fmaf(-n, by, y) < 0.0f ? n - 1.0f : n;
+  }
+  __device__ __forceinline__ float up(float x) const { return -down(-x); }
+};
+
 }  // namespace kvh
