@@ -22,16 +22,16 @@ struct CopyParams {
   uint32_t row_words, words;  // 16-byte words of a row, and of a page
   uint32_t parts;             // blocks of a page and layer: those of K, those of V, one for the rest
   uint32_t layers;
-  Divisor by_parts, by_layers, by_row;
+  Divisor by_parts, by_each, by_row;  // by_each: blocks of a pair
   int64_t each() const { return (int64_t)parts * layers; }  // blocks of a pair
 };
 
 constexpr int kCopyWords = 4;  // 16-byte words of a thread
 constexpr int64_t kMostBlocks = ((int64_t)1 << 31) - 1;
 
-__device__ __forceinline__ void copy_part(const CopyParams& a, uint32_t block) {
-  const uint32_t unit = a.by_parts.quotient(block), part = block - unit * a.parts;
-  const uint32_t i = a.by_layers.quotient(unit), layer = unit - i * a.layers;
+// Part `in_pair` of a pair's parts * layers.
+__device__ __forceinline__ void copy_part(const CopyParams& a, uint32_t i, uint32_t in_pair) {
+  const uint32_t layer = a.by_parts.quotient(in_pair), part = in_pair - layer * a.parts;
   const int src = a.src[i], dst = a.dst[i];
   if (src < 0 || src == dst) return;
   if (src >= a.pages || dst < 0 || dst >= a.pages) {
@@ -75,7 +75,23 @@ __device__ __forceinline__ void copy_part(const CopyParams& a, uint32_t block) {
   }
 }
 
-__global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) { copy_part(a, blockIdx.x); }
+__global__ __launch_bounds__(kBlockThreads) void copy_kernel(CopyParams a) {
+  const uint32_t i = a.by_each.quotient(blockIdx.x);
+  copy_part(a, i, blockIdx.x - i * a.by_each.d);
+}
+
+// Pairs whose number the device knows, by the blocks of a launch from `first` on.
+__device__ __forceinline__ void copy_many(const CopyParams& a, const int32_t* many, uint32_t first) {
+  const uint32_t each = a.by_each.d, blocks = gridDim.x - first;
+  const uint64_t units = (uint64_t)(uint32_t)uniform(*many) * each;
+  for (uint64_t u = blockIdx.x - first; u < units; u += blocks) {
+    const uint32_t i = u < (1u << 31) ? a.by_each.quotient((uint32_t)u) : (uint32_t)(u / each);
+    copy_part(a, i, (uint32_t)(u - (uint64_t)i * each));
+  }
+}
+// Blocks that such a launch has for them at most: enough to fill the chip, and not one for each copy that there might be (64 rows of a cache of 32 layers that
+// copy nothing: TIME with).
+constexpr int64_t kCopyBlocks = 16384;
 
 // What bounds and scales there are goes along.
 int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int32_t* status, CopyParams& a) {
@@ -96,8 +112,10 @@ int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, con
   a.words = (uint32_t)words;
   a.parts = (uint32_t)(2 * half + 1);
   a.layers = (uint32_t)c.layers;
-  a.by_parts = Divisor(a.parts), a.by_layers = Divisor(a.layers), a.by_row = Divisor(a.row_words);
-  return a.each() > kMostBlocks / 2 ? KVH_E_SHAPE : KVH_OK;
+  a.by_parts = Divisor(a.parts), a.by_row = Divisor(a.row_words);
+  if (a.each() > kMostBlocks / 2) return KVH_E_SHAPE;
+  a.by_each = Divisor((uint32_t)a.each());
+  return KVH_OK;
 }
 
 // `pairs` of them at most.
@@ -142,7 +160,8 @@ struct ForkParams {
   int32_t* lens_out;
   // workspace
   Child* child;        // of each row
-  int32_t *src, *dst;  // pairs to copy
+  int32_t *src, *dst;  // pairs to copy, and how many
+  int32_t* pairs;
   int32_t* fresh;      // free pages in order
 };
 
@@ -273,8 +292,11 @@ __device__ __forceinline__ bool serve(const ForkParams& a, int b, const Child& c
   a.child[b].base = need == 0 ? 0 : served ? (int32_t)from : -1;
   a.lens_out[b] = served ? c.len : 0;
   if (!served && a.r.status != nullptr) a.r.status[b] = KVH_DEV_NO_PAGES;
-  a.src[b] = served && c.copies ? a.r.table[(int64_t)c.parent * a.r.ts + c.full] : -1;
   return served;
+}
+__device__ __forceinline__ void note_copy(const ForkParams& a, const Child& c, int64_t pair, int64_t from) {
+  a.src[pair] = a.r.table[(int64_t)c.parent * a.r.ts + c.full];
+  a.dst[pair] = a.fresh[from];
 }
 
 __global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
@@ -298,7 +320,17 @@ __global__ __launch_bounds__(kScanThreads) void hand_out_kernel(ForkParams a) {
   }
   run.give(r.refs_out, a.fresh, at, given, lane);
   __syncthreads();
-  for (int b = threadIdx.x; b < r.n; b += kScanThreads) a.dst[b] = a.src[b] >= 0 ? a.fresh[a.child[b].base] : -1;
+  int64_t pairs = 0;
+  for (int b0 = 0; b0 < r.n; b0 += kScanThreads) {
+    const int b = b0 + threadIdx.x;
+    Child c{};
+    if (b < r.n) c = a.child[b];
+    const bool copies = c.copies && c.base >= 0;
+    const int64_t pair = pairs + before_me(copies, lds, all);
+    if (copies) note_copy(a, c, pair, c.base);
+    pairs += all;
+  }
+  if (threadIdx.x == 0) *a.pairs = (int32_t)pairs;
 }
 
 // All of that by one block, with the counts in LDS, for kScanThreads rows at most: thread b has row b.
@@ -309,7 +341,7 @@ struct PlanRow {
 };
 
 __global__ __launch_bounds__(kScanThreads) void plan_kernel(ForkParams a) {
-  __shared__ uint32_t free_of[kScanWaves], need_of[kScanWaves], given_of[kScanWaves];
+  __shared__ uint32_t free_of[kScanWaves], need_of[kScanWaves], given_of[kScanWaves], copies_of[kScanWaves];
   extern __shared__ int32_t plan_lds[];
   const RowsParams& r = a.r;
   PlanRow* rows = reinterpret_cast<PlanRow*>(plan_lds);
@@ -360,11 +392,14 @@ __global__ __launch_bounds__(kScanThreads) void plan_kernel(ForkParams a) {
   const uint32_t many = row_sum(frees), at = row_sum(lane < wave ? frees : 0), from = row_sum(lane < wave ? needs : 0) + before;
   const bool served = real && serve(a, b, c, from, many);
   const uint32_t most = wave_max(served && need != 0 ? from + need : 0);
-  if (lane == 0) given_of[wave] = most;
+  const uint64_t copying = __ballot(served && c.copies);
+  if (lane == 0) given_of[wave] = most, copies_of[wave] = __popcll(copying);
   __syncthreads();
   run.give(refs, a.fresh, at, wave_max(lane < kScanWaves ? given_of[lane] : 0), lane);
+  const uint32_t copies = lane < kScanWaves ? copies_of[lane] : 0, earlier = row_sum(lane < wave ? copies : 0), pairs = row_sum(copies);
   __syncthreads();
-  if (real) a.dst[b] = served && c.copies ? a.fresh[from] : -1;
+  if (served && c.copies) note_copy(a, c, earlier + __popcll(copying & (((uint64_t)1 << lane) - 1)), from);
+  if (threadIdx.x == 0) *a.pairs = (int32_t)pairs;
 #pragma unroll 4
   for (int p = threadIdx.x; p < r.pages; p += kScanThreads) r.refs_out[p] = refs[p];
 }
@@ -372,7 +407,7 @@ __global__ __launch_bounds__(kScanThreads) void plan_kernel(ForkParams a) {
 // The rows, by the first n blocks, and the copies.
 __global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a, CopyParams copy) {
   const RowsParams& r = a.r;
-  if (blockIdx.x >= (uint32_t)r.n) return copy_part(copy, blockIdx.x - r.n);
+  if (blockIdx.x >= (uint32_t)r.n) return copy_many(copy, a.pairs, r.n);
   const int b = blockIdx.x;
   const Child c = a.child[b];
   const bool served = c.base >= 0;
@@ -398,32 +433,46 @@ __global__ __launch_bounds__(kBlockThreads) void rows_kernel(ForkParams a, CopyP
 struct CompactParams {
   RowsParams r;
   int32_t* moved;
-  int32_t *src, *dst;  // pairs to copy, pages / 2 of them at most
+  int32_t *src, *dst;  // pairs to copy, pages / 2 of them at most, and how many
+  int32_t* pairs;
 };
 
+// By one block: with U pages in use, the free ones below U and those in use from U on are as many, and go together in order.
 __global__ __launch_bounds__(kScanThreads) void place_kernel(CompactParams a) {
-  __shared__ int64_t lds[kScanWaves];
+  __shared__ uint32_t used_of[kScanWaves], below_of[kScanWaves];
   const RowsParams& r = a.r;
-  int64_t mine = 0, used;
-  for (int p = threadIdx.x; p < r.pages; p += kScanThreads) mine += r.refs[p] > 0;
-  before_me(mine, lds, used);
-  for (int i = threadIdx.x; i < r.pages / 2; i += kScanThreads) a.src[i] = a.dst[i] = -1;
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  const Run run(r.pages);
+  auto in_use = [&](int p) { return p + lane < run.stop && r.refs[p + lane] > 0; };
+  uint32_t mine = 0;
+#pragma unroll 4
+  for (int p = run.begin; p < run.stop; p += kWave) mine += __popcll(__ballot(in_use(p)));
+  if (lane == 0) used_of[wave] = mine;
   __syncthreads();
-  int64_t holes = 0, strays = 0;  // free pages below `used` and pages in use above, so far: as many of both in the end
-  for (int p0 = 0; p0 < r.pages; p0 += kScanThreads) {
-    const int p = p0 + threadIdx.x;
-    const bool in_use = p < r.pages && r.refs[p] > 0;
-    const bool hole = p < used && !in_use, stray = p >= used && in_use;
-    int64_t all;
-    const int64_t at = before_me((int64_t)hole | (int64_t)stray << 32, lds, all);
-    if (hole) a.dst[holes + (at & 0xffffffff)] = p;
-    if (stray) a.src[strays + (at >> 32)] = p;
-    holes += all & 0xffffffff, strays += all >> 32;
-    if (p < r.pages) {
-      a.moved[p] = in_use ? p : -1;
-      r.refs_out[p] = in_use ? r.refs[p] : 0;
-    }
+  uint32_t of = lane < kScanWaves ? used_of[lane] : 0;
+  const int used = (int)row_sum(of);
+  uint32_t before = row_sum(lane < wave ? of : 0);  // pages in use before the run's next ones
+  uint32_t below = 0;
+#pragma unroll 4
+  for (int p = run.begin; p < run.stop; p += kWave) below += __popcll(__ballot(in_use(p) && p + lane < used));
+  if (lane == 0) below_of[wave] = below;
+  __syncthreads();
+  of = lane < kScanWaves ? below_of[lane] : 0;
+  const int stay = (int)row_sum(of), strays = used - stay;
+  const uint64_t under = ((uint64_t)1 << lane) - 1;
+  for (int p0 = run.begin; p0 < run.stop; p0 += kWave) {
+    const int p = p0 + lane;
+    const bool is = in_use(p0);
+    const uint64_t who = __ballot(is);
+    const int rank = (int)(before + __popcll(who & under));  // pages in use before it
+    before += __popcll(who);
+    if (p >= run.stop) continue;
+    if (is && p >= used) a.src[rank - stay] = p;
+    if (!is && p < used) a.dst[p - rank] = p;
+    a.moved[p] = is ? p : -1;
+    r.refs_out[p] = is ? r.refs[p] : 0;
   }
+  if (threadIdx.x == 0) *a.pairs = strays;
   __syncthreads();
   for (int i = threadIdx.x; i < strays; i += kScanThreads) {
     const int src = a.src[i], dst = a.dst[i];
@@ -433,14 +482,17 @@ __global__ __launch_bounds__(kScanThreads) void place_kernel(CompactParams a) {
   }
 }
 
-__global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a) {
+// The rows, by the first n blocks, and the copies.
+__global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a, CopyParams copy) {
   const RowsParams& r = a.r;
+  if (blockIdx.x >= (uint32_t)r.n) return copy_many(copy, a.pairs, r.n);
   const int b = blockIdx.x;
   const int32_t len = r.lens[b];
   bool bad = len < 0 || len > r.capacity;
   const int held = bad ? 0 : pages_of(r, len);
   const int32_t* from = r.table + (int64_t)b * r.ts;
   int32_t* to = r.table_out + (int64_t)b * r.to_ts;
+#pragma unroll 4
   for (int j = threadIdx.x; j < r.table_pages; j += kBlockThreads) {
     int page = -1;
     if (j < held) {
@@ -499,7 +551,7 @@ int kvh_copy_pages(const kvh_cache* cache, const kvh_bounds* bounds, const int32
 
 size_t kvh_fork_workspace(int n_requests, int pages) {
   if (n_requests < 1 || n_requests > kMaxRequests || pages < 1) return 0;
-  return (size_t)n_requests * (sizeof(Child) + 2 * sizeof(int32_t)) + (size_t)pages * sizeof(int32_t);
+  return (size_t)n_requests * (sizeof(Child) + 2 * sizeof(int32_t)) + ((size_t)pages + 1) * sizeof(int32_t);
 }
 
 int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, const int32_t* parents_dev, const int32_t* grow_dev,
@@ -511,10 +563,9 @@ int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of
   if (workspace_bytes < kvh_fork_workspace(a.r.n, a.r.pages)) return KVH_E_SIZE;
   a.parents = parents_dev, a.grow = grow_dev, a.lens_out = lens_out_dev;
   a.child = static_cast<Child*>(workspace_dev);
-  a.src = reinterpret_cast<int32_t*>(a.child + a.r.n), a.dst = a.src + a.r.n, a.fresh = a.dst + a.r.n;
+  a.src = reinterpret_cast<int32_t*>(a.child + a.r.n), a.dst = a.src + a.r.n, a.pairs = a.dst + a.r.n, a.fresh = a.pairs + 1;
   CopyParams copy{};
   if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
-  const int64_t copies = std::min<int64_t>(a.r.n, (kMostBlocks - a.r.n) / copy.each());  // that share the rows' launch
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t lds = (int64_t)a.r.pages * sizeof(int32_t) + (int64_t)a.r.n * sizeof(PlanRow);
   if (a.r.n <= kScanThreads && lds <= kPlanLds && (int64_t)a.r.n * a.r.table_pages <= kPlanEntries) {
@@ -528,13 +579,12 @@ int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of
     hipLaunchKernelGGL(hand_out_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
     KVH_HIP_CHECK_LAUNCH();
   }
-  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(a.r.n + copies * copy.each())), dim3(kBlockThreads), 0, s, a, copy);
+  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(a.r.n + std::min(a.r.n * copy.each(), kCopyBlocks))), dim3(kBlockThreads), 0, s, a, copy);
   KVH_HIP_CHECK_LAUNCH();
-  copy.src += copies, copy.dst += copies;
-  return launch_copy(copy, a.r.n - copies, s);
+  return KVH_OK;
 }
 
-size_t kvh_compact_workspace(int pages) { return pages < 1 ? 0 : (size_t)2 * (pages / 2 + 1) * sizeof(int32_t); }
+size_t kvh_compact_workspace(int pages) { return pages < 1 ? 0 : (size_t)(2 * ((int64_t)pages / 2) + 1) * sizeof(int32_t); }
 
 int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, int32_t* moved_out_dev, void* workspace_dev,
                 size_t workspace_bytes, int32_t* status_dev, void* stream) {
@@ -544,15 +594,16 @@ int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows
   if (!aligned4(moved_out_dev) || !aligned4(workspace_dev)) return KVH_E_ALIGN;
   if (workspace_bytes < kvh_compact_workspace(a.r.pages)) return KVH_E_SIZE;
   a.moved = moved_out_dev;
-  a.src = static_cast<int32_t*>(workspace_dev), a.dst = a.src + a.r.pages / 2 + 1;
+  a.pairs = static_cast<int32_t*>(workspace_dev), a.src = a.pairs + 1, a.dst = a.src + a.r.pages / 2;
   CopyParams copy{};
   if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   launch_kernel(place_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
   KVH_HIP_CHECK_LAUNCH();
-  hipLaunchKernelGGL(renumber_kernel, dim3((unsigned)a.r.n), dim3(kBlockThreads), 0, s, a);
+  const int64_t copies = std::min(a.r.pages / 2 * copy.each(), kCopyBlocks);
+  hipLaunchKernelGGL(renumber_kernel, dim3((unsigned)(a.r.n + copies)), dim3(kBlockThreads), 0, s, a, copy);
   KVH_HIP_CHECK_LAUNCH();
-  return launch_copy(copy, a.r.pages / 2, s);
+  return KVH_OK;
 }
 
 }  // extern "C"

@@ -164,7 +164,7 @@ def fork(kvh, pool, held, parents=None, grow=None, **kw):
 
 
 @pytest.mark.parametrize("store", ["fp16", "i8"])
-@pytest.mark.parametrize("n,bt,columns,share", [(1, 16, 4, 1), (8, 4, 40, 4), (5, 1, 30, 1), (70, 7, 12, 2), (300, 16, 5, 3), (3, 24, 700, 3)])
+@pytest.mark.parametrize("n,bt,columns,share", [(1, 16, 4, 1), (8, 4, 40, 4), (5, 1, 30, 1), (70, 7, 12, 2), (300, 16, 5, 3), (3, 24, 700, 3), (1100, 2, 6, 2), (4, 1, 9000, 1)])
 def test_fork_step_after_step(kvh, n, bt, columns, share, store):
     """Growth, beams that change places, rows that end, rows that begin, again and again; sooner or later the pages run out."""
     rng = random.Random(n * bt + columns)
@@ -231,7 +231,7 @@ def test_fork_first_child_refused(kvh):
 
 
 @pytest.mark.parametrize("store", ["fp16", "e4m3"])
-@pytest.mark.parametrize("n,bt,columns,spare,share", [(1, 16, 4, 0, 1), (6, 7, 20, 50, 2), (30, 16, 40, 3000, 3), (2, 1, 3, 1, 1), (90, 4, 30, 700, 1)])
+@pytest.mark.parametrize("n,bt,columns,spare,share", [(1, 16, 4, 0, 1), (6, 7, 20, 50, 2), (30, 16, 40, 3000, 3), (2, 1, 3, 1, 1), (90, 4, 30, 700, 1), (5, 1, 3000, 40000, 1)])
 def test_compact(kvh, n, bt, columns, spare, share, store):
     rng = random.Random(n + spare)
     held = Held(rng, n, columns * bt, bt, columns, spare, share, extra=3)
