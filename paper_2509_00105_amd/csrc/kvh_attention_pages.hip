@@ -107,11 +107,14 @@ __global__ __launch_bounds__(kBlockThreads) void join_kernel(AttnParams a, ListP
 
 // ---- launch -------------------------------------------------------------------------------------------------------
 constexpr int kMostListed = 4096, kMostSplits = 64;
-constexpr int kFill = 512;       // blocks that fill the chip
-constexpr int kLeastSteps = 4;   // of a share: one for each wave
+// Rules with both sides measured (us, 8 KV heads of 128, 32 query heads, bf16, pages of 16).  Tokens and heads are shared by blocks until there are 256 of these:
+// 32 of 64 pages 31 whole and 36 in two, 4 of 256 pages (int8) 17 for 256 blocks and 21 for 512, 16 of 64 pages 21 and 22.  8 steps a block at least (one
+// of 256 pages: 16.5, with 4 steps 20.6), and only where that takes 16 from a block's (one of 16 pages, 8 steps: 8.5 whole, 11.2 in two; of 32 pages 10.7
+// and 12.4; of 64 pages 12.7 in four, 14.3 in two).
+constexpr int kFill = 256, kLeastSteps = 8, kGain = 16;
 
 struct Plan {
-  int row_tiles, splits, each;
+  int row_tiles, splits;
   size_t slot;  // bytes of a partial result, of all heads
   int64_t tiles;
 };
@@ -122,6 +125,7 @@ Plan plan_of(int n_tokens, int heads, int q_heads, int head_dim, int block_token
   p.tiles = (int64_t)n_tokens * p.row_tiles;
   const int64_t units = p.tiles * heads, steps = ((int64_t)count * block_tokens + kStep - 1) / kStep;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kFill / units, steps / kLeastSteps, (int64_t)kMostSplits}));
+  if (steps - (steps + p.splits - 1) / p.splits < kGain) p.splits = 1;
   p.slot = (size_t)heads * 16 * (head_dim + 2) * sizeof(float);
   return p;
 }
