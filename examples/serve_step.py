@@ -1,7 +1,9 @@
 """A cache hit and the answer that follows it, end to end on the GPU: a stored entry is decoded, moves into an 8-bit serving cache, and
 new tokens are appended to it and attend over it, one layer after the other.
 
-  python examples/serve_step.py [--context 2000] [--question 40] [--answer 8] [--cache i8|e4m3|16] [--layers 4]
+  python examples/serve_step.py [--context 2000] [--question 40] [--answer 8] [--cache i8|e4m3|16] [--layers 4] [--pages 0]
+
+With --pages N the answer's tokens read N pages each, chosen for every KV head by the bounds of the pages' keys, and not the whole request.
 
 The "model" is random queries, keys and values of the right shapes: what runs is the path around the cache, as a serving program runs it.  Prints what the
 cache holds and how far the attention is from one over the keys and values before they were compressed.
@@ -35,9 +37,17 @@ class ServingCache:
         self.k, self.v = (torch.zeros((layers, pages, PAGE, C), dtype=dtype, device="cuda") for _ in range(2))
         self.k_scale, self.v_scale = (None, None) if kind == "16" else \
             (torch.zeros((layers, pages, HEADS), device="cuda") for _ in range(2))
+        # the bounds of the pages' keys, for answers that read chosen pages
+        self.bounds = torch.zeros((layers, pages, HEADS, 2, DIM), dtype=torch.int8, device="cuda")
+        self.bound_scale = torch.zeros((layers, pages, HEADS), device="cuda")
         self.table = torch.randperm(pages, device="cuda").to(torch.int32).view(1, pages)
         self.length = torch.zeros(1, dtype=torch.int32, device="cuda")
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def bound(self, layer: slice, starts: torch.Tensor, n: int) -> None:
+        """The bounds of the pages that the last n tokens lie on."""
+        kvh.bound_keys(self.k[layer], self.bounds[layer], self.bound_scale[layer], starts, self.length, self.table, n,
+                       k_scale=None if self.k_scale is None else self.k_scale[layer], status=self.status)
 
     def of(self, layer: int) -> dict:
         """The arguments of a call on one layer."""
@@ -45,7 +55,7 @@ class ServingCache:
         return dict(k_cache=cut(self.k), v_cache=cut(self.v), k_scale=cut(self.k_scale), v_scale=cut(self.v_scale))
 
 
-def run(context: int, question: int, answer: int, kind: str, layers: int, seed: int = 0) -> dict:
+def run(context: int, question: int, answer: int, kind: str, layers: int, seed: int = 0, pages: int = 0) -> dict:
     g = torch.Generator(device="cuda").manual_seed(seed)
     rows = lambda n, ch: torch.randn((layers, n, ch), generator=g, device="cuda").bfloat16()  # noqa: E731
     table = rotation_table(context + question + answer)
@@ -60,6 +70,7 @@ def run(context: int, question: int, answer: int, kind: str, layers: int, seed: 
     cache.length += context
     starts = torch.tensor([0, context], dtype=torch.int32, device="cuda")
     kvh.append(k, v, cache.k, cache.v, starts, cache.length, cache.table, context, k_scale=cache.k_scale, v_scale=cache.v_scale, status=cache.status)
+    cache.bound(slice(None), starts, context)
 
     # The question's tokens at once, then the answer's one by one; a layer appends before it attends.
     workspace = torch.empty(max(kvh.attention_workspace(1, n, n, HEADS, HEADS * GROUP) for n in (question, 1)), dtype=torch.uint8, device="cuda")
@@ -74,6 +85,13 @@ def run(context: int, question: int, answer: int, kind: str, layers: int, seed: 
             one = slice(layer, layer + 1)
             turned = kvh.append(k[one], v[one], starts=starts, lens=cache.length, page_table=cache.table, max_new=n, q=q[one], q_out=torch.empty_like(q[one]),
                                 rotation=table, status=cache.status, **at)
+            cache.bound(one, starts, n)
+            if pages and n == 1:
+                chosen = kvh.select_pages(turned[0], cache.bounds[one], cache.bound_scale[one], 0, starts, cache.length, cache.table, n, pages, block_tokens=PAGE,
+                                          first=1, last=min(2, pages - 1), status=cache.status)
+                out.append(kvh.attention_pages(turned[0], layer=0, pages=chosen, starts=starts, lens=cache.length, page_table=cache.table, max_new=n,
+                                               status=cache.status, **at))
+                continue
             out.append(kvh.attention(turned[0], layer=0, starts=starts, lens=cache.length, page_table=cache.table, max_new=n, out=torch.empty_like(turned[0]),
                                      workspace=workspace, status=cache.status, **at))
         # the same over what was never compressed
@@ -108,9 +126,10 @@ def main() -> None:
     ap.add_argument("--question", type=int, default=40)
     ap.add_argument("--answer", type=int, default=8)
     ap.add_argument("--layers", type=int, default=4)
+    ap.add_argument("--pages", type=int, default=0, help="pages that a token of the answer reads (2 at least); 0: all")
     ap.add_argument("--cache", choices=("16", "i8", "e4m3"), default="i8")
     a = ap.parse_args()
-    r = run(a.context, a.question, a.answer, a.cache, a.layers)
+    r = run(a.context, a.question, a.answer, a.cache, a.layers, pages=a.pages)
     print("%d tokens in %d layers of a %s cache: %.1f MB; attention %.4f off that over uncompressed keys and values"
           % (r["tokens"], a.layers, a.cache, r["bytes"] / 1e6, r["error"]))
 

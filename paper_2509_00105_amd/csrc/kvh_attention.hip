@@ -34,11 +34,11 @@ __global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void attention_kernel(A
   // The head groups of an item run on one XCD (consecutive blocks go to the 8 of them in turn), one after the other: they read neighbouring memory.
   const uint32_t g = blockIdx.x / 8, hi = a.by_heads.quotient(g), k = hi * 8 + blockIdx.x % 8;
   const int head = (int)(g - hi * a.by_heads.d) << a.log_hw;
-  tell_refused(a.req, a.status);
+  tell_refused(a);
   Item it;
   for (Items items; items.next(a, few_log_rows(NR), k, head == 0 && wave == 0, lane, it);) {
     if (it.split && it.slot >= a.slots) continue;  // requests that share rows of the batch
-    attend<DT, KIND, D, NR, PAGE16>(a, it, a.req.table + (int64_t)it.b * a.req.table_stride, head, wave, lane, lds, lds_ml);
+    attend<DT, KIND, D, NR, PAGE16>(a, it, [&] { return a.req.table + (int64_t)it.b * a.req.table_stride; }, head, wave, lane, lds, lds_ml);
     __syncthreads();
   }
 }

@@ -403,8 +403,9 @@ constexpr int kLogFewWaves = 2, kFewWaves = 1 << kLogFewWaves, kFewThreads = kFe
 
 constexpr int few_log_rows(int nr) { return nr == 1 ? 4 : 5; }
 
-template <int DT, int KIND, int D, int NR, bool PAGE16>
-__device__ __forceinline__ void attend(const AttnParams& a, const Item& it, const int32_t* table, int head0, int wave, int lane, float* lds, float (*lds_ml)[16 * NR][2]) {
+// `table_of()`: the table of the item's pages.
+template <int DT, int KIND, int D, int NR, bool PAGE16, typename Table>
+__device__ __forceinline__ void attend(const AttnParams& a, const Item& it, Table&& table_of, int head0, int wave, int lane, float* lds, float (*lds_ml)[16 * NR][2]) {
   using W = Worker<DT, KIND, D, NR, PAGE16>;
   constexpr int kTile = 16 * NR;
   constexpr int kPitch = D + 4;  // floats of a row in LDS
@@ -418,7 +419,7 @@ __device__ __forceinline__ void attend(const AttnParams& a, const Item& it, cons
   w.p_least = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)w.row0);
   w.p_most = it.rq.len - it.rq.n + (int)a.by_group.quotient((uint32_t)(w.row0 + w.rows - 1));
   w.end = a.causal && w.p_most + 1 < it.rq.len ? w.p_most + 1 : it.rq.len;
-  w.table = table;
+  w.table = table_of();
   w.begin();
   const Steps steps(a, w.p_least, w.end);
   int s0, s1;

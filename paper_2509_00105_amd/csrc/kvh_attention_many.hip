@@ -690,7 +690,7 @@ __global__ __launch_bounds__(kBlockThreads, 2) void attention_many_kernel(AttnPa
   const int wave = uniform((int32_t)(threadIdx.x / kWave));
   const uint32_t k = a.by_heads.quotient(blockIdx.x);
   const int head = (int)(blockIdx.x - k * (uint32_t)a.heads);
-  tell_refused(a.req, a.status);
+  tell_refused(a);
   Item it;
   if constexpr (!CUT) {
     if (Schedule(a, kLogManyRows, lane).whole(k, it)) attend<DT, KIND, D, PAGE16>(a, it, head, wave, lane, shared);

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void pages_kernel(AttnP
   __shared__ int32_t entries;
   extern __shared__ int32_t pages[];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
-  tell_refused(a.req, a.status);
+  tell_refused(a);
   const uint32_t part = x.by_splits.quotient(blockIdx.x), split = blockIdx.x - part * x.splits;
   const uint32_t unit = x.by_row_tiles.quotient(part), row_tile = part - unit * x.row_tiles;
   const uint32_t row = a.by_heads.quotient(unit);
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void pages_kernel(AttnP
   it.from = (int)split * x.each, it.count = x.each;
   it.last = split == (uint32_t)x.splits - 1, it.split = x.splits > 1;
   it.slot = ((int64_t)row * x.row_tiles + row_tile) * x.splits + split;
-  attend<DT, KIND, D, 1, PAGE16>(a, it, pages, head, wave, lane, lds, lds_ml);
+  attend<DT, KIND, D, 1, PAGE16>(a, it, [&] { return pages; }, head, wave, lane, lds, lds_ml);
 }
 
 // Joins the parts of a query row: a wave a row.
