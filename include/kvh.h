@@ -445,7 +445,7 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
  *
  * Bounds: for each page, KV head and channel the lowest and the highest key, as int8 codes rounded outwards with one fp32 scale
  * per page and head.  With x the values of a 16-bit page (or the codes of an 8-bit one) over the page's tokens, a the largest |x| of the
- * head: lowest = floor(127 min x / a), highest = ceil(127 max x / a), scale = a / 127 times the page's K scale, quotients in fp32; zeros
+ * head: lowest = floor(127 min x / a), highest = ceil(127 max x / a), scale = a / 127 times the page's K scale, rounded to fp32 each time; zeros
  * where a < 2^-100.  A page and head that holds an infinity or NaN (its K scale among that) has codes of zero and a scale of NaN. */
 typedef struct {
   int8_t* codes;  /* [layers][pages][heads][2][head_dim]: lowest, highest; 16-byte aligned, a page dense */
@@ -587,7 +587,7 @@ int kvh_stream_probe(void* dst_dev, const void* src_dev, size_t n_units, int rea
 
 /* Timing of one launch, for callers that profile (not part of the codec; Design section, Estimator: the decompression
  * overhead of an entry is something to be measured).  The two events (hipEvent_t, created by the caller with timing
- * enabled) are recorded by the NEXT encode, decode, transcode, append or attention kernel that this host thread launches through the
+ * enabled) are recorded by the NEXT kernel of a codec, serving-cache or page call that this host thread launches through the
  * library: `start_event` when that kernel starts executing, `stop_event` when it has finished, on the launch's
  * stream, so that hipEventElapsedTime(start, stop) is the kernel's own duration - what a kernel trace reports -
  * without the queue packets that events recorded around a launch put between neighbouring kernels.  The pair is

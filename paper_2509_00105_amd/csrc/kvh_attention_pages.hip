@@ -3,6 +3,10 @@
 // The listed pages, one after the other, are a request of their own for the worker of kvh_attention: its page table is the list, looked up in the request's
 // table and kept in LDS, its length ends with the last listed page, or at the token's own position where that page is the last.  The query heads of the KV head
 // are the rows, 16 a tile.
+//
+// A token's pages are read once for its own KV head, 2 D bytes of each token at a time (of 16 bits), which memory bounds: 64 requests, 64 pages of 16 each for 8 heads of 128, bf16: 54 us =
+// 4.8 TB/s (over all 4096 tokens kvh_attention takes 186), int8: 36 us.  Where tokens of a request read the same pages from the caches, widening codes and the softmax take most of
+// the time: the rows of other tokens would fit into the tile, but have lists of their own.  512 tokens after 32768, int8: 107 us (kvh_attention: 396).
 #include "kvh_attention_few.hpp"
 
 #include <algorithm>

