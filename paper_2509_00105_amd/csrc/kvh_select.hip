@@ -374,20 +374,31 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
     const int most = pages_seen(a, rq, stop - 1);
     const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
     bool bad = false;
-    for (int u0 = 0; u0 < a.group; u0 += kRows) {  // (one turn, but where a token has more than 16 query heads)
-      int entry[kTiles];
-      look_up(table, wave * kSpan, most, lane, entry);
-      if (u0 > 0) __syncthreads();
-      quantise<DT, D>(raw, queries);  // while the table's entries are on their way
-      if (kRows < a.group) raw = load_queries<D, TPT>(a, row0, past, head, u0 + kRows < a.group ? u0 + kRows : 0);
-      __syncthreads();
-      const Queries<D, TPT> q(a, queries, u0, lane);
-      for (int base = wave * kSpan; base < most; base += kSelectWaves * kSpan) {
-        const Boxes<D> boxes(a, entry, head, lane);
-        look_up(table, base + kSelectWaves * kSpan, most, lane, entry);
-        bad |= score_span<D, TPT>(a, boxes, base, most, end, q, u0 == 0, u0 + kRows >= a.group, lane,
-                               [&](int token, int j) { return __builtin_bit_cast(float, keys[token * a.pitch + j]); },
-                               [&](int token, int j, uint32_t key) { keys[token * a.pitch + j] = key; });
+    if (most <= a.count) {  // all there are: no score decides
+      for (int j = threadIdx.x; j < most; j += kSelectThreads) {
+        const int page = table[j];
+        const bool there = page >= 0 && page < a.pages;
+        bad |= !there;
+#pragma unroll
+        for (int i = 0; i < TPT; ++i)
+          if (j < end[i]) keys[i * a.pitch + j] = there;
+      }
+    } else {
+      for (int u0 = 0; u0 < a.group; u0 += kRows) {  // (one turn, but where a token has more than 16 query heads)
+        int entry[kTiles];
+        look_up(table, wave * kSpan, most, lane, entry);
+        if (u0 > 0) __syncthreads();
+        quantise<DT, D>(raw, queries);  // while the table's entries are on their way
+        if (kRows < a.group) raw = load_queries<D, TPT>(a, row0, past, head, u0 + kRows < a.group ? u0 + kRows : 0);
+        __syncthreads();
+        const Queries<D, TPT> q(a, queries, u0, lane);
+        for (int base = wave * kSpan; base < most; base += kSelectWaves * kSpan) {
+          const Boxes<D> boxes(a, entry, head, lane);
+          look_up(table, base + kSelectWaves * kSpan, most, lane, entry);
+          bad |= score_span<D, TPT>(a, boxes, base, most, end, q, u0 == 0, u0 + kRows >= a.group, lane,
+                                 [&](int token, int j) { return __builtin_bit_cast(float, keys[token * a.pitch + j]); },
+                                 [&](int token, int j, uint32_t key) { keys[token * a.pitch + j] = key; });
+        }
       }
     }
     if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
@@ -422,13 +433,23 @@ __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
   if (!request_of(a.req, row, lane, b, rq)) return;
   const int end[1] = {pages_seen(a, rq, row)}, first = (int)tile * kScorePages;
   if (first >= end[0]) return;
+  uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
+  bool bad = false;
+  if (end[0] <= a.count) {  // all there are: no score decides
+    for (int j = first + (int)threadIdx.x; j < end[0] && j < first + kScorePages; j += kBlockThreads) {
+      const int page = a.req.table[(int64_t)b * a.req.table_stride + j];
+      const bool there = page >= 0 && page < a.pages;
+      keys[j] = there;
+      bad |= !there;
+    }
+    if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
+    return;
+  }
   u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
   const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
   int entry[kScoreTurns][kTiles];
 #pragma unroll
   for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, end[0], lane, entry[i]);
-  uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
-  bool bad = false;
   for (int u0 = 0; u0 < a.group; u0 += 16) {
     if (u0 > 0) {
       raw = load_queries<D, 1>(a, row, row + 1, head, u0);
