@@ -41,8 +41,8 @@ struct SelectParams {
   int32_t* status;
   uint32_t* keys;   // [token of this turn][head][pitch], where they go through memory
   int64_t pitch;    // keys of a token and head
-  int token0;       // the turn's first token
-  uint32_t units;   // tokens and heads of this turn
+  int token0, tokens;  // of this turn
+  uint32_t units;   // groups of tokens, and heads, that a block scores
   Divisor by_block, by_heads, by_units;
 };
 
@@ -119,9 +119,9 @@ __device__ __forceinline__ int pages_seen(const SelectParams& a, const Request& 
   return p < 0 ? 0 : (int)a.by_block.quotient((uint32_t)p) + 1;
 }
 
-// The scores of pages [base, base + kSpan) for TPT tokens, by one wave, 16 of them a product; entry[t] is the table's entry of page base + 16 t + l % 16 in lane l.  end[i] is
-// 0 for what is no token of the request.  `best_of(token, page)` and `put(token, page, word)` are called by the lanes that hold a score: where the query heads come in
-// several turns of 16, the largest so far is kept as it is, and the last turn makes the key of it.
+// The scores of pages [base, base + kSpan) for TPT tokens, by one wave, 16 of them a product; entry[t] is the table's entry of page base + 16 t + l % 16 in lane l.  A lane
+// gets those of token lane / 16 * TPT / 4, which chooses among `own` pages (0: it is no token of the request).  `best_of(page)` and `put(page, word)` are called by the lanes that
+// hold a score: where the query heads come in several turns of 16, the largest so far is kept as it is, and the last turn makes the key of it.
 constexpr int kTiles = 2, kSpan = 16 * kTiles;
 
 template <int D>
@@ -144,12 +144,11 @@ struct Boxes {
 };
 
 template <int D, int TPT, typename Best, typename Put>
-__device__ __forceinline__ bool score_span(const SelectParams& a, const Boxes<D>& x, int base, int most, const int (&end)[TPT], const Queries<D, TPT>& q,
-                                           bool first, bool last, int lane, Best&& best_of, Put&& put) {
+__device__ __forceinline__ bool score_span(const SelectParams& a, const Boxes<D>& x, int base, int most, int own, const Queries<D, TPT>& q, bool first, bool last,
+                                           int lane, Best&& best_of, Put&& put) {
   constexpr int kSums = 2 * D / 64;
   const int l16 = lane % 16, grp = lane / 16;
   bool bad = false;
-  const int token = grp * TPT / 4, own = end[token];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     i32x4 dot = {0, 0, 0, 0};
@@ -167,15 +166,15 @@ __device__ __forceinline__ bool score_span(const SelectParams& a, const Boxes<D>
     const int j = base + 16 * t + l16;
     bad |= j < most && !x.there[t];
     if (grp % (4 / TPT) != 0 || j >= own) continue;
-    if (!first) best = fmaxf(best, best_of(token, j));
+    if (!first) best = fmaxf(best, best_of(j));
     if (!last) {
-      put(token, j, __builtin_bit_cast(uint32_t, best));
+      put(j, __builtin_bit_cast(uint32_t, best));
       continue;
     }
     const float score = best * x.scale[t];
     uint32_t key = !(score == score) || !(fabsf(x.scale[t]) < INFINITY) ? kInfinite : order_of(score);
     if (j < a.first || j >= own - a.last) key = kAlways;
-    put(token, j, x.there[t] ? key : 0u);
+    put(j, x.there[t] ? key : 0u);
   }
   return bad;
 }
@@ -374,6 +373,11 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
     const int most = pages_seen(a, rq, stop - 1);
     const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
     bool bad = false;
+    const int token = lane / 16 * TPT / 4;
+    int own = end[0];
+#pragma unroll
+    for (int i = 1; i < TPT; ++i) own = token == i ? end[i] : own;
+    uint32_t* mine = keys + token * a.pitch;
     if (most <= a.count) {  // all there are: no score decides
       for (int j = threadIdx.x; j < most; j += kSelectThreads) {
         const int page = table[j];
@@ -395,19 +399,18 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
         for (int base = wave * kSpan; base < most; base += kSelectWaves * kSpan) {
           const Boxes<D> boxes(a, entry, head, lane);
           look_up(table, base + kSelectWaves * kSpan, most, lane, entry);
-          bad |= score_span<D, TPT>(a, boxes, base, most, end, q, u0 == 0, u0 + kRows >= a.group, lane,
-                                 [&](int token, int j) { return __builtin_bit_cast(float, keys[token * a.pitch + j]); },
-                                 [&](int token, int j, uint32_t key) { keys[token * a.pitch + j] = key; });
+          bad |= score_span<D, TPT>(a, boxes, base, most, own, q, u0 == 0, u0 + kRows >= a.group, lane, [&](int j) { return __builtin_bit_cast(float, mine[j]); },
+                                    [&](int j, uint32_t key) { mine[j] = key; });
         }
       }
     }
     if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
     __syncthreads();
-    const int team = wave / W, mine = row0 + team;
+    const int team = wave / W, its = row0 + team;
     int n = 0;
 #pragma unroll
     for (int i = 0; i < TPT; ++i) n = i == team ? end[i] : n;
-    int32_t* out = mine >= row && mine < stop ? a.out + ((int64_t)mine * a.heads + head) * a.count : nullptr;
+    int32_t* out = its >= row && its < stop ? a.out + ((int64_t)its * a.heads + head) * a.count : nullptr;
     uint32_t* from = keys + team * a.pitch;
     if (n + lane < ((n + 3) & ~3)) from[n + lane] = 0;  // (all waves of the team do)
     __syncthreads();
@@ -419,60 +422,79 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
 
 constexpr int kScoreTurns = 2, kScorePages = kScoreTurns * kWavesPerBlock * kSpan;
 
-// Scores of one token and head, kScoreTurns times kSpan pages a wave, to memory.
-template <int DT, int D>
+// Scores of M times TPT neighbouring tokens and a head, kScoreTurns times kSpan pages a wave, to memory.  What is loaded of a page serves all tokens.
+template <int DT, int D, int TPT, int M>
 __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
-  __shared__ QueryLds<D> queries;
+  constexpr int kRows = 16 / TPT, kTokens = TPT * M;
+  __shared__ QueryLds<D> queries[M];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   if (a.token0 == 0) tell_refused(a.req, a.status);
   const uint32_t tile = a.by_units.quotient(blockIdx.x), unit = blockIdx.x - tile * a.units;  // the tiles that few requests reach come last
-  const uint32_t token = a.by_heads.quotient(unit);
-  const int head = (int)(unit - token * a.heads), row = a.token0 + (int)token;
-  int b;
-  Request rq;
-  if (!request_of(a.req, row, lane, b, rq)) return;
-  const int end[1] = {pages_seen(a, rq, row)}, first = (int)tile * kScorePages;
-  if (first >= end[0]) return;
-  uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
-  bool bad = false;
-  if (end[0] <= a.count) {  // all there are: no score decides
-    for (int j = first + (int)threadIdx.x; j < end[0] && j < first + kScorePages; j += kBlockThreads) {
-      const int page = a.req.table[(int64_t)b * a.req.table_stride + j];
-      const bool there = page >= 0 && page < a.pages;
-      keys[j] = there;
-      bad |= !there;
+  const uint32_t group = a.by_heads.quotient(unit);
+  const int head = (int)(unit - group * a.heads), row0 = a.token0 + (int)group * kTokens, first = (int)tile * kScorePages;
+  const int past = row0 + kTokens < a.token0 + a.tokens ? row0 + kTokens : a.token0 + a.tokens;
+  bool ready = false;  // the queries
+  for (int row = row0; row < past;) {
+    int b;
+    Request rq;
+    if (!request_of(a.req, row, lane, b, rq)) {
+      ++row;
+      continue;
+    }
+    const int begin = row, stop = rq.start + rq.n < past ? rq.start + rq.n : past;  // the request's rows of this tile
+    row = stop;
+    const int most = pages_seen(a, rq, stop - 1);
+    if (first >= most) continue;
+    const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
+    auto keys_of = [&](int r) { return a.keys + ((int64_t)(r - a.token0) * a.heads + head) * a.pitch; };
+    bool bad = false;
+    if (most <= a.count) {  // all there are: no score decides
+      for (int j = first + (int)threadIdx.x; j < most && j < first + kScorePages; j += kBlockThreads) {
+        const int page = table[j];
+        const bool there = page >= 0 && page < a.pages;
+        for (int r = begin; r < stop; ++r)
+          if (j < pages_seen(a, rq, r)) keys_of(r)[j] = there;
+        bad |= !there;
+      }
+    } else {
+      int entry[kScoreTurns][kTiles];
+#pragma unroll
+      for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, most, lane, entry[i]);
+      for (int u0 = 0; u0 < a.group; u0 += kRows) {  // (one turn, but where a token has more than 16 query heads)
+        if (!ready || a.group > kRows) {
+          u32x4 raw[M];
+#pragma unroll
+          for (int m = 0; m < M; ++m) raw[m] = load_queries<D, TPT>(a, row0 + m * TPT, past, head, u0);
+          if (ready) __syncthreads();
+#pragma unroll
+          for (int m = 0; m < M; ++m) quantise<DT, D>(raw[m], queries[m]);
+          __syncthreads();
+          ready = true;
+        }
+#pragma unroll
+        for (int i = 0; i < kScoreTurns; ++i) {
+          const int base = first + (i * kWavesPerBlock + wave) * kSpan;
+          if (base >= most) break;
+          const Boxes<D> boxes(a, entry[i], head, lane);
+#pragma unroll 1
+          for (int m = 0; m < M; ++m) {
+            const int r = row0 + m * TPT + lane / 16 * TPT / 4, own = r >= begin && r < stop ? pages_seen(a, rq, r) : 0;
+            if (M > 1 && !__any(own != 0)) continue;
+            uint32_t* keys = keys_of(own != 0 ? r : begin);
+            const Queries<D, TPT> q(a, queries[m], u0, lane);
+            bad |= score_span<D, TPT>(a, boxes, base, most, own, q, u0 == 0, u0 + kRows >= a.group, lane, [&](int j) { return __builtin_bit_cast(float, keys[j]); },
+                                      [&](int j, uint32_t key) { keys[j] = key; });
+          }
+        }
+      }
     }
     if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
-    return;
   }
-  u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
-  const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
-  int entry[kScoreTurns][kTiles];
-#pragma unroll
-  for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, end[0], lane, entry[i]);
-  for (int u0 = 0; u0 < a.group; u0 += 16) {
-    if (u0 > 0) {
-      raw = load_queries<D, 1>(a, row, row + 1, head, u0);
-      __syncthreads();
-    }
-    quantise<DT, D>(raw, queries);
-    __syncthreads();
-    const Queries<D, 1> q(a, queries, u0, lane);
-#pragma unroll
-    for (int i = 0; i < kScoreTurns; ++i) {
-      const int base = first + (i * kWavesPerBlock + wave) * kSpan;
-      if (base >= end[0]) break;
-      const Boxes<D> boxes(a, entry[i], head, lane);
-      bad |= score_span<D, 1>(a, boxes, base, end[0], end, q, u0 == 0, u0 + 16 >= a.group, lane, [&](int, int j) { return __builtin_bit_cast(float, keys[j]); },
-                              [&](int, int j, uint32_t key) { keys[j] = key; });
-    }
-  }
-  if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
 template <int W>
 __global__ __launch_bounds__(W * kWave) void pick_kernel(SelectParams a) {
-  constexpr int kThreads = W * kWave, kStaged = 8 * kThreads;
+  constexpr int kThreads = W * kWave, kStaged = W == 4 ? 4096 : 8 * kThreads;
   __shared__ PickLds<W, 1> lds;
   __shared__ u32x4 staged[kStaged / 4];
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
@@ -511,20 +533,22 @@ constexpr int kMostListed = 4096;
 constexpr int kLds = 64 << 10;  // of a block
 // Tokens and heads below which scores of more pages than that go through memory: 64 requests of 4096 (lognormal) 19.1 us so, 20.6 in one launch (the longest has 1364 pages); one of 1000
 // pages 9.3 and 16; 64 of 512 pages 21.9 and 20.1, of 1000 32.3 and 32.8.  A table of 256 pages or less: 64 requests 13 us in one launch, one request 8.5.
-constexpr int64_t kFewUnits = 1024, kManyPages = 256;
+constexpr int64_t kFewUnits = 1024, kManyPages = 256, kShared = 1024;
 
 int64_t pitch_of(int table_pages) { return ((int64_t)table_pages + 3) & ~(int64_t)3; }
 
-// Tokens that share a block's products; 0 where scores go through memory.
-int together(int n_requests, int n_tokens, int heads, int group, int table_pages, bool room) {
-  const int64_t keys = pitch_of(table_pages) * (int64_t)sizeof(uint32_t);
-  constexpr int64_t kQueries = sizeof(QueryLds<128>);
-  if (keys + (int64_t)sizeof(PickLds<kSelectWaves, 1>) + kQueries > kLds) return 0;
-  if (room && (int64_t)n_tokens * heads < kFewUnits && table_pages > kManyPages) return 0;
+// Tokens that share a product: their query heads are its rows.
+int together(int n_requests, int n_tokens, int group) {
   const int64_t each = (int64_t)n_tokens / n_requests;
-  if (each >= 4 && group <= 4 && 4 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 4, 4>) + kQueries <= kLds) return 4;
-  if (each >= 2 && group <= 8 && 2 * keys + (int64_t)sizeof(PickLds<kSelectWaves / 2, 2>) + kQueries <= kLds) return 2;
-  return 1;
+  return each >= 4 && group <= 4 ? 4 : each >= 2 && group <= 8 ? 2 : 1;
+}
+// Whether a block keeps its scores in LDS.
+bool fits(int tokens, int table_pages) {
+  const int64_t picks = tokens == 4 ? sizeof(PickLds<kSelectWaves / 4, 4>) : tokens == 2 ? sizeof(PickLds<kSelectWaves / 2, 2>) : sizeof(PickLds<kSelectWaves, 1>);
+  return tokens * pitch_of(table_pages) * (int64_t)sizeof(uint32_t) + picks + (int64_t)sizeof(QueryLds<128>) <= kLds;
+}
+bool by_memory(int n_tokens, int heads, int tokens, int table_pages) {
+  return table_pages > kManyPages && ((int64_t)n_tokens * heads < kFewUnits || (tokens > 1 && table_pages > kShared));
 }
 
 template <int DT, int D>
@@ -539,13 +563,25 @@ void launch_select(const SelectParams& a, int tokens, hipStream_t stream) {
     launch_kernel(select_kernel<DT, D, 1>, grid, block, lds, stream, a);
 }
 
+constexpr unsigned kManyPicks = 1024;
+constexpr int kMany = 4;  // products of a block that scores neighbouring tokens
+
 template <int DT, int D>
-void launch_score(const SelectParams& a, int64_t tiles, hipStream_t stream) {
-  launch_kernel(score_kernel<DT, D>, dim3((unsigned)(a.units * tiles)), dim3(kBlockThreads), 0, stream, a);
-  if (a.pitch <= 4096)
-    hipLaunchKernelGGL(pick_kernel<8>, dim3(a.units), dim3(8 * kWave), 0, stream, a);
+void launch_score(const SelectParams& a, int together, int64_t tiles, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.units * tiles)), block(kBlockThreads);
+  if (together == 4)
+    launch_kernel(score_kernel<DT, D, 4, kMany>, grid, block, 0, stream, a);
+  else if (together == 2)
+    launch_kernel(score_kernel<DT, D, 2, kMany>, grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL(pick_kernel<16>, dim3(a.units), dim3(16 * kWave), 0, stream, a);
+    launch_kernel(score_kernel<DT, D, 1, 1>, grid, block, 0, stream, a);
+  const dim3 picks((unsigned)(a.tokens * a.heads));
+  if (a.pitch <= 4096 && picks.x >= kManyPicks)
+    hipLaunchKernelGGL(pick_kernel<4>, picks, dim3(4 * kWave), 0, stream, a);
+  else if (a.pitch <= 4096)
+    hipLaunchKernelGGL(pick_kernel<8>, picks, dim3(8 * kWave), 0, stream, a);
+  else
+    hipLaunchKernelGGL(pick_kernel<16>, picks, dim3(16 * kWave), 0, stream, a);
 }
 
 }  // namespace
@@ -557,7 +593,8 @@ extern "C" {
 
 size_t kvh_select_workspace(int n_requests, int n_tokens, int heads, int table_pages) {
   if (n_requests < 1 || n_requests > kMaxRequests || n_tokens < 1 || heads < 1 || heads > 4096 || table_pages < 1) return 0;
-  if (together(n_requests, n_tokens, heads, 1, table_pages, true) != 0) return 0;
+  // (The query heads are not known here: with few a KV head, neighbouring tokens share products.)
+  if (fits(1, table_pages) && !by_memory(n_tokens, heads, together(n_requests, n_tokens, 1), table_pages)) return 0;
   const size_t token = (size_t)heads * pitch_of(table_pages) * sizeof(uint32_t), most = (size_t)64 << 20;
   return std::max(token, std::min((size_t)n_tokens, most / token) * token);
 }
@@ -587,30 +624,36 @@ int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* re
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t token = (int64_t)a.heads * a.pitch * sizeof(uint32_t);
   int64_t turn = workspace_dev == nullptr ? 0 : (int64_t)(workspace_bytes / (size_t)token);
-  const int tokens = together(requests->n_requests, requests->n_tokens, a.heads, a.group, requests->table_pages, turn > 0);
   const bool f16 = dt == KVH_F16, wide = bounds->head_dim == 128;
-  if (tokens != 0) {
-    if (f16)
-      wide ? launch_select<KVH_F16, 128>(a, tokens, s) : launch_select<KVH_F16, 64>(a, tokens, s);
-    else
-      wide ? launch_select<KVH_BF16, 128>(a, tokens, s) : launch_select<KVH_BF16, 64>(a, tokens, s);
-    KVH_HIP_CHECK_LAUNCH();
-    return KVH_OK;
+  int tokens = together(requests->n_requests, requests->n_tokens, a.group);
+  if (turn < 1 || !by_memory(requests->n_tokens, a.heads, tokens, requests->table_pages)) {
+    int here = tokens;
+    while (here > 1 && !fits(here, requests->table_pages)) here /= 2;
+    if (fits(here, requests->table_pages)) {
+      if (f16)
+        wide ? launch_select<KVH_F16, 128>(a, here, s) : launch_select<KVH_F16, 64>(a, here, s);
+      else
+        wide ? launch_select<KVH_BF16, 128>(a, here, s) : launch_select<KVH_BF16, 64>(a, here, s);
+      KVH_HIP_CHECK_LAUNCH();
+      return KVH_OK;
+    }
   }
   if (turn < 1) return KVH_E_SIZE;
   a.keys = static_cast<uint32_t*>(workspace_dev);
-  const int64_t tiles = ((int64_t)requests->table_pages + kScorePages - 1) / kScorePages;
-  if (a.heads * tiles >= (int64_t)1 << 31) return KVH_E_SHAPE;
-  turn = std::min({turn, (int64_t)requests->n_tokens, (((int64_t)1 << 31) - 1) / (a.heads * tiles)});
+  const int64_t tiles = ((int64_t)requests->table_pages + kScorePages - 1) / kScorePages, most = ((int64_t)1 << 31) - 1;
+  if (a.heads * tiles > most) return KVH_E_SHAPE;
+  if (turn < tokens * kMany || requests->n_tokens / requests->n_requests < tokens * kMany) tokens = 1;
+  const int each = tokens > 1 ? tokens * kMany : 1;  // tokens of a block
+  turn = std::min<int64_t>({turn, (int64_t)requests->n_tokens, most / a.heads / tiles * each});
+  if (turn < requests->n_tokens) turn -= turn % each;
   for (int64_t t0 = 0; t0 < requests->n_tokens; t0 += turn) {
-    a.token0 = (int)t0;
-    const unsigned here = (unsigned)std::min<int64_t>(turn, requests->n_tokens - t0);
-    a.units = here * a.heads;
+    a.token0 = (int)t0, a.tokens = (int)std::min<int64_t>(turn, requests->n_tokens - t0);
+    a.units = (uint32_t)((a.tokens + each - 1) / each * a.heads);
     a.by_units = Divisor(a.units);
     if (f16)
-      wide ? launch_score<KVH_F16, 128>(a, tiles, s) : launch_score<KVH_F16, 64>(a, tiles, s);
+      wide ? launch_score<KVH_F16, 128>(a, tokens, tiles, s) : launch_score<KVH_F16, 64>(a, tokens, tiles, s);
     else
-      wide ? launch_score<KVH_BF16, 128>(a, tiles, s) : launch_score<KVH_BF16, 64>(a, tiles, s);
+      wide ? launch_score<KVH_BF16, 128>(a, tokens, tiles, s) : launch_score<KVH_BF16, 64>(a, tokens, tiles, s);
     KVH_HIP_CHECK_LAUNCH();
   }
   return KVH_OK;
