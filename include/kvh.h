@@ -516,7 +516,8 @@ typedef struct {
 /* Fork: row b becomes a child of row a = parents[b] and grows by grow[b] tokens: lens_out[b] = lens[a] + grow[b].  parents NULL: every row is its own child;
  * parents[b] < 0: of none, an empty row.  grow NULL: zeros.  A step's growth, beams that are reordered, samples of one prompt, requests that begin and end are
  * one call of this.  The full pages of lens[a] tokens are shared.  A page that they do not fill stays with the first of a's children that is no KVH_DEV_BAD_REQUEST; the others get a
- * copy of it (all layers, scales, bounds) on a fresh page, so that each row appends to a page of its own: such a page must be in no other row before the call.
+ * copy of it (all layers, scales, bounds) on a fresh page, so that each row appends to a page of its own: such a page must be in no other row before the call, and held by
+ * nothing else.
  * Fresh pages are those that no row holds afterwards and nothing else does, lowest numbers first, handed to the rows in order; refs_out counts what rows hold after the
  * call in place of what they held before it.  A page that is given up and one that is handed out may be the same: the old rows are of no use afterwards.
  * Refused rows become empty (lens_out 0): KVH_DEV_BAD_REQUEST for parents[b] >= n_requests, grow[b] < 0, a parent's length below 0 or past the

@@ -3,8 +3,8 @@
 // Contents move by pairs of pages, 16 KiB a block; memory bounds that.  Who holds what is integer work on the table and the counts, which is bound by the trips to
 // memory that wait for each other: a block plans, with the counts in LDS where they fit, and a second launch writes the rows and copies at the same
 // time.  Counts change by atomic additions of whole numbers, whose order is of no account.
-// Measured, calls among others: 512 pages of 8 layers (268 MB) copied 113 us = 4.76 TB/s, what a plain copy reaches; 3 pages of 32 layers, int8: 4.6 us; fork, 64 rows of 4096 tokens
-// (lognormal) that grow by one: 14.5 us (plan 8 to 12), 16 requests of 4 beams: 14; compact, 450 pages of 8 layers: 102 us = 4.6 TB/s, 1024 pages of one layer: 7.1.
+// Measured, calls among others: 512 pages of 8 layers (268 MB) copied 109 us = 4.9 TB/s (a plain copy of 4 GiB reaches 5.5); 3 pages of 32 layers, int8: 4.6 us; fork, 64 rows of 4096 tokens
+// (lognormal) that grow by one: 14.5 us (plan 8 to 12), 16 requests of 4 beams: 14; compact, 450 pages of 8 layers: 89 us = 5.3 TB/s, 1024 pages of one layer: 7.2.
 #include "kvh_cache.hpp"
 
 #include <algorithm>
@@ -25,6 +25,7 @@ struct CopyParams {
   uint32_t row_words, words;  // 16-byte words of a row, and of a page
   uint32_t parts;             // blocks of a page and layer: those of K, those of V, one for the rest
   uint32_t layers;
+  int past;                   // many pages pass by the caches
   Divisor by_parts, by_each, by_row;  // by_each: blocks of a pair
   int64_t each() const { return (int64_t)parts * layers; }  // blocks of a pair
 };
@@ -53,11 +54,19 @@ __device__ __forceinline__ void copy_part(const CopyParams& a, uint32_t i, uint3
     for (int e = 0; e < kCopyWords; ++e) {
       const uint32_t w = w0 + e * kBlockThreads, row = a.by_row.quotient(w);
       at[e] = row * a.c_ts + (int64_t)(w - row * a.row_words) * 16;
-      if (w < a.words) x[e] = *reinterpret_cast<const u32x4*>(from + at[e]);
     }
+    auto move = [&](auto&& get, auto&& put) {
 #pragma unroll
-    for (int e = 0; e < kCopyWords; ++e)
-      if (w0 + e * kBlockThreads < a.words) *reinterpret_cast<u32x4*>(to + at[e]) = x[e];
+      for (int e = 0; e < kCopyWords; ++e)
+        if (w0 + e * kBlockThreads < a.words) x[e] = get(reinterpret_cast<const u32x4*>(from + at[e]));
+#pragma unroll
+      for (int e = 0; e < kCopyWords; ++e)
+        if (w0 + e * kBlockThreads < a.words) put(x[e], reinterpret_cast<u32x4*>(to + at[e]));
+    };
+    if (a.past)
+      move([](const u32x4* p) { return __builtin_nontemporal_load(p); }, [](const u32x4& v, u32x4* p) { __builtin_nontemporal_store(v, p); });
+    else
+      move([](const u32x4* p) { return *p; }, [](const u32x4& v, u32x4* p) { *p = v; });
     return;
   }
   for (int h = threadIdx.x; h < a.heads; h += kBlockThreads) {
@@ -97,8 +106,12 @@ __device__ __forceinline__ void copy_many(const CopyParams& a, const int32_t* ma
 // 104 with 4096, 111 with 2048).
 constexpr int64_t kForkBlocks = 4096, kCompactBlocks = 16384;
 
+// Bytes of K and V from which on copies pass by the caches: 512 pages of 8 layers 108.7 us so, 112.9 through them; compact, 450 pages of 8 layers, 89 and 100.  Fork copies
+// a page that is appended to next.
+constexpr int64_t kPastBytes = 16 << 20;
+
 // What bounds and scales there are goes along.
-int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int32_t* status, CopyParams& a) {
+int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, const int32_t* dst, int64_t pairs, int32_t* status, CopyParams& a) {
   const int width = c.kind == KVH_CACHE_16 ? 2 : 1;
   a.src = src, a.dst = dst, a.status = status;
   a.ck = static_cast<uint8_t*>(c.k), a.cv = static_cast<uint8_t*>(c.v);
@@ -116,6 +129,7 @@ int copy_params(const kvh_cache& c, const kvh_bounds* b, const int32_t* src, con
   a.words = (uint32_t)words;
   a.parts = (uint32_t)(2 * half + 1);
   a.layers = (uint32_t)c.layers;
+  a.past = pairs * words * 32 * c.layers >= kPastBytes;
   a.by_parts = Divisor(a.parts), a.by_row = Divisor(a.row_words);
   if (a.each() > kMostBlocks / 2) return KVH_E_SHAPE;
   a.by_each = Divisor((uint32_t)a.each());
@@ -549,7 +563,7 @@ int kvh_copy_pages(const kvh_cache* cache, const kvh_bounds* bounds, const int32
   if (n < 0 || n > 1 << 24 || (n > 0 && (src_dev == nullptr || dst_dev == nullptr))) return KVH_E_ARG;
   if (!aligned4(src_dev) || !aligned4(dst_dev)) return KVH_E_ALIGN;
   CopyParams a{};
-  if (int rc = copy_params(*cache, bounds, src_dev, dst_dev, status_dev, a)) return rc;
+  if (int rc = copy_params(*cache, bounds, src_dev, dst_dev, n, status_dev, a)) return rc;
   return launch_copy(a, n, static_cast<hipStream_t>(stream));
 }
 
@@ -569,7 +583,7 @@ int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of
   a.child = static_cast<Child*>(workspace_dev);
   a.src = reinterpret_cast<int32_t*>(a.child + a.r.n), a.dst = a.src + a.r.n, a.pairs = a.dst + a.r.n, a.fresh = a.pairs + 1;
   CopyParams copy{};
-  if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
+  if (int rc = copy_params(*cache, bounds, a.src, a.dst, 0, nullptr, copy)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int64_t lds = (int64_t)a.r.pages * sizeof(int32_t) + (int64_t)a.r.n * sizeof(PlanRow);
   if (a.r.n <= kScanThreads && lds <= kPlanLds && (int64_t)a.r.n * a.r.table_pages <= kPlanEntries) {
@@ -600,7 +614,7 @@ int kvh_compact(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows
   a.moved = moved_out_dev;
   a.pairs = static_cast<int32_t*>(workspace_dev), a.src = a.pairs + 1, a.dst = a.src + a.r.pages / 2;
   CopyParams copy{};
-  if (int rc = copy_params(*cache, bounds, a.src, a.dst, nullptr, copy)) return rc;
+  if (int rc = copy_params(*cache, bounds, a.src, a.dst, a.r.pages / 2, nullptr, copy)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   launch_kernel(place_kernel, dim3(1), dim3(kScanThreads), 0, s, a);
   KVH_HIP_CHECK_LAUNCH();

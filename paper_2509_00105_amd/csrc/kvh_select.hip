@@ -10,8 +10,8 @@
 //
 // What bounds it: the bounds' bytes (256 of a page and head) come at 4 TB/s where many tokens have many pages (64 of 1000 pages: 32 us); below that, trips to memory that wait for
 // each other - request, table, bounds - and for one token the picking.  A single block takes in 13 bytes a clock, so that one token of 1000 pages took 16 us in one launch and takes 9.3 in two.
-// Measured, 8 KV heads of 128, 32 query heads, calls among others: 64 requests of 4096 tokens (lognormal, pages of 16) 19 us (scores 13.8, picking 5.3), one of 131072 16 us (6.2
-// and 8.6), 64 of 64 pages 7, 64 of 256 pages 13.
+// Measured, 8 KV heads of 128, 32 query heads, calls among others: 64 requests of 4096 tokens (lognormal, pages of 16) 19.5 us (scores 13.8, picking 5.3), one of 131072 16 us (6.2
+// and 8.6), 64 of 64 pages 6, 64 of 256 pages 13, 512 new tokens of a request of 2080 pages 71 (48 and 22).
 #include "kvh_bounds.hpp"
 
 #include <algorithm>
@@ -422,14 +422,55 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
 
 constexpr int kScoreTurns = 2, kScorePages = kScoreTurns * kWavesPerBlock * kSpan;
 
-// Scores of M times TPT neighbouring tokens and a head, kScoreTurns times kSpan pages a wave, to memory.  What is loaded of a page serves all tokens.
-template <int DT, int D, int TPT, int M>
+// Scores of one token and head, kScoreTurns times kSpan pages a wave, to memory.
+template <int DT, int D>
 __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
-  constexpr int kRows = 16 / TPT, kTokens = TPT * M;
-  __shared__ QueryLds<D> queries[M];
+  __shared__ QueryLds<D> queries;
   const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
   if (a.token0 == 0) tell_refused(a.req, a.status);
   const uint32_t tile = a.by_units.quotient(blockIdx.x), unit = blockIdx.x - tile * a.units;  // the tiles that few requests reach come last
+  const uint32_t token = a.by_heads.quotient(unit);
+  const int head = (int)(unit - token * a.heads), row = a.token0 + (int)token;
+  int b;
+  Request rq;
+  if (!request_of(a.req, row, lane, b, rq)) return;
+  const int end = pages_seen(a, rq, row), first = (int)tile * kScorePages;
+  if (first >= end) return;
+  u32x4 raw = load_queries<D, 1>(a, row, row + 1, head, 0);
+  const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
+  int entry[kScoreTurns][kTiles];
+#pragma unroll
+  for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, end, lane, entry[i]);
+  uint32_t* keys = a.keys + ((int64_t)token * a.heads + head) * a.pitch;
+  bool bad = false;
+  for (int u0 = 0; u0 < a.group; u0 += 16) {
+    if (u0 > 0) {
+      raw = load_queries<D, 1>(a, row, row + 1, head, u0);
+      __syncthreads();
+    }
+    quantise<DT, D>(raw, queries);
+    __syncthreads();
+    const Queries<D, 1> q(a, queries, u0, lane);
+#pragma unroll
+    for (int i = 0; i < kScoreTurns; ++i) {
+      const int base = first + (i * kWavesPerBlock + wave) * kSpan;
+      if (base >= end) break;
+      const Boxes<D> boxes(a, entry[i], head, lane);
+      bad |= score_span<D, 1>(a, boxes, base, end, end, q, u0 == 0, u0 + 16 >= a.group, lane, [&](int j) { return __builtin_bit_cast(float, keys[j]); },
+                              [&](int j, uint32_t key) { keys[j] = key; });
+    }
+  }
+  if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
+}
+
+// Scores of M times TPT neighbouring tokens and a head in the same way.  What is loaded of a page serves all tokens.
+template <int DT, int D, int TPT, int M>
+__global__ __launch_bounds__(kBlockThreads) void score_many_kernel(SelectParams a) {
+  constexpr int kTokens = TPT * M;
+  __shared__ QueryLds<D> queries[M];
+  const int lane = threadIdx.x % kWave, wave = uniform((int32_t)(threadIdx.x / kWave));
+  if (a.token0 == 0) tell_refused(a.req, a.status);
+  const uint32_t tile = a.by_units.quotient(blockIdx.x), unit = blockIdx.x - tile * a.units;
   const uint32_t group = a.by_heads.quotient(unit);
   const int head = (int)(unit - group * a.heads), row0 = a.token0 + (int)group * kTokens, first = (int)tile * kScorePages;
   const int past = row0 + kTokens < a.token0 + a.tokens ? row0 + kTokens : a.token0 + a.tokens;
@@ -445,47 +486,32 @@ __global__ __launch_bounds__(kBlockThreads) void score_kernel(SelectParams a) {
     row = stop;
     const int most = pages_seen(a, rq, stop - 1);
     if (first >= most) continue;
+    if (!ready) {
+      u32x4 raw[M];
+#pragma unroll
+      for (int m = 0; m < M; ++m) raw[m] = load_queries<D, TPT>(a, row0 + m * TPT, past, head, 0);
+#pragma unroll
+      for (int m = 0; m < M; ++m) quantise<DT, D>(raw[m], queries[m]);
+      __syncthreads();
+      ready = true;
+    }
     const int32_t* table = a.req.table + (int64_t)b * a.req.table_stride;
-    auto keys_of = [&](int r) { return a.keys + ((int64_t)(r - a.token0) * a.heads + head) * a.pitch; };
+    int entry[kScoreTurns][kTiles];
+#pragma unroll
+    for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, most, lane, entry[i]);
     bool bad = false;
-    if (most <= a.count) {  // all there are: no score decides
-      for (int j = first + (int)threadIdx.x; j < most && j < first + kScorePages; j += kBlockThreads) {
-        const int page = table[j];
-        const bool there = page >= 0 && page < a.pages;
-        for (int r = begin; r < stop; ++r)
-          if (j < pages_seen(a, rq, r)) keys_of(r)[j] = there;
-        bad |= !there;
-      }
-    } else {
-      int entry[kScoreTurns][kTiles];
 #pragma unroll
-      for (int i = 0; i < kScoreTurns; ++i) look_up(table, first + (i * kWavesPerBlock + wave) * kSpan, most, lane, entry[i]);
-      for (int u0 = 0; u0 < a.group; u0 += kRows) {  // (one turn, but where a token has more than 16 query heads)
-        if (!ready || a.group > kRows) {
-          u32x4 raw[M];
-#pragma unroll
-          for (int m = 0; m < M; ++m) raw[m] = load_queries<D, TPT>(a, row0 + m * TPT, past, head, u0);
-          if (ready) __syncthreads();
-#pragma unroll
-          for (int m = 0; m < M; ++m) quantise<DT, D>(raw[m], queries[m]);
-          __syncthreads();
-          ready = true;
-        }
-#pragma unroll
-        for (int i = 0; i < kScoreTurns; ++i) {
-          const int base = first + (i * kWavesPerBlock + wave) * kSpan;
-          if (base >= most) break;
-          const Boxes<D> boxes(a, entry[i], head, lane);
+    for (int i = 0; i < kScoreTurns; ++i) {
+      const int base = first + (i * kWavesPerBlock + wave) * kSpan;
+      if (base >= most) break;
+      const Boxes<D> boxes(a, entry[i], head, lane);
 #pragma unroll 1
-          for (int m = 0; m < M; ++m) {
-            const int r = row0 + m * TPT + lane / 16 * TPT / 4, own = r >= begin && r < stop ? pages_seen(a, rq, r) : 0;
-            if (M > 1 && !__any(own != 0)) continue;
-            uint32_t* keys = keys_of(own != 0 ? r : begin);
-            const Queries<D, TPT> q(a, queries[m], u0, lane);
-            bad |= score_span<D, TPT>(a, boxes, base, most, own, q, u0 == 0, u0 + kRows >= a.group, lane, [&](int j) { return __builtin_bit_cast(float, keys[j]); },
-                                      [&](int j, uint32_t key) { keys[j] = key; });
-          }
-        }
+      for (int m = 0; m < M; ++m) {
+        const int r = row0 + m * TPT + lane / 16 * TPT / 4, own = r >= begin && r < stop ? pages_seen(a, rq, r) : 0;
+        if (!__any(own != 0)) continue;
+        uint32_t* keys = a.keys + ((int64_t)((own != 0 ? r : begin) - a.token0) * a.heads + head) * a.pitch;
+        const Queries<D, TPT> q(a, queries[m], 0, lane);
+        bad |= score_span<D, TPT>(a, boxes, base, most, own, q, true, true, lane, [](int) { return 0.0f; }, [&](int j, uint32_t key) { keys[j] = key; });
       }
     }
     if (__any(bad) && lane == 0 && a.status != nullptr) a.status[b] = KVH_DEV_BAD_REQUEST;
@@ -531,8 +557,9 @@ __global__ __launch_bounds__(W * kWave) void pick_kernel(SelectParams a) {
 // ---- launch -------------------------------------------------------------------------------------------------------
 constexpr int kMostListed = 4096;
 constexpr int kLds = 64 << 10;  // of a block
-// Tokens and heads below which scores of more pages than that go through memory: 64 requests of 4096 (lognormal) 19.1 us so, 20.6 in one launch (the longest has 1364 pages); one of 1000
+// Tokens and heads below which scores of more pages than kManyPages go through memory: 64 requests of 4096 (lognormal) 19.1 us so, 20.6 in one launch (the longest has 1364 pages); one of 1000
 // pages 9.3 and 16; 64 of 512 pages 21.9 and 20.1, of 1000 32.3 and 32.8.  A table of 256 pages or less: 64 requests 13 us in one launch, one request 8.5.
+// More tokens and heads, where neighbouring tokens share products: 512 of 2080 pages 71 us through memory and 83 in one launch, of 500 pages 40 and 31.
 constexpr int64_t kFewUnits = 1024, kManyPages = 256, kShared = 1024;
 
 int64_t pitch_of(int table_pages) { return ((int64_t)table_pages + 3) & ~(int64_t)3; }
@@ -563,18 +590,20 @@ void launch_select(const SelectParams& a, int tokens, hipStream_t stream) {
     launch_kernel(select_kernel<DT, D, 1>, grid, block, lds, stream, a);
 }
 
+// Picks from which on a team has 4 waves and not 8, of which more wait at a time: 4096 of 2080 keys 22 us, 32 with 8; 512 of them 7.2 and 6.3.
 constexpr unsigned kManyPicks = 1024;
-constexpr int kMany = 4;  // products of a block that scores neighbouring tokens
+// Products of a block that scores neighbouring tokens: 512 tokens of 2080 pages 48 us, with 2 65, with 8 56; 64 tokens 12.5, 11 and 19.
+constexpr int kMany = 4;
 
 template <int DT, int D>
 void launch_score(const SelectParams& a, int together, int64_t tiles, hipStream_t stream) {
   const dim3 grid((unsigned)(a.units * tiles)), block(kBlockThreads);
   if (together == 4)
-    launch_kernel(score_kernel<DT, D, 4, kMany>, grid, block, 0, stream, a);
+    launch_kernel(score_many_kernel<DT, D, 4, kMany>, grid, block, 0, stream, a);
   else if (together == 2)
-    launch_kernel(score_kernel<DT, D, 2, kMany>, grid, block, 0, stream, a);
+    launch_kernel(score_many_kernel<DT, D, 2, kMany>, grid, block, 0, stream, a);
   else
-    launch_kernel(score_kernel<DT, D, 1, 1>, grid, block, 0, stream, a);
+    launch_kernel(score_kernel<DT, D>, grid, block, 0, stream, a);
   const dim3 picks((unsigned)(a.tokens * a.heads));
   if (a.pitch <= 4096 && picks.x >= kManyPicks)
     hipLaunchKernelGGL(pick_kernel<4>, picks, dim3(4 * kWave), 0, stream, a);

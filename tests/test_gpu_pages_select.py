@@ -303,6 +303,31 @@ def test_with_and_without_a_workspace(kvh, group):
     assert torch.equal(one, two) and np.array_equal(one.cpu().numpy(), b.want(50))
 
 
+@pytest.mark.parametrize("group", [1, 3, 4, 6, 8])
+@pytest.mark.parametrize("count", [20, 400])
+def test_many_new_tokens_share_products(kvh, group, count):
+    """Tiles of 8 and 16 tokens that begin and end inside requests, a request without tokens, rows behind the last one; in turns too, and without a workspace."""
+    b = Batch([45, 0, 21, 70], [1300, 5, 30, 72], heads=2, group=group, dim=64, bt=1, seed=38, layers=1, behind=3)
+    want = b.want(count, 2, 3)
+    assert np.array_equal(b.run(kvh, count, 2, 3).cpu().numpy(), want)
+    token = 2 * 1300 * 4
+    for size in (0, 16 * token, 37 * token, 3 * token):
+        room = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        assert np.array_equal(b.run(kvh, count, 2, 3, workspace=room).cpu().numpy(), want), size
+    assert not b.status.any()
+
+
+def test_many_new_tokens_refused(kvh):
+    b = Batch([45, 33, 21, 70], [1300, 900, 30, 72], heads=1, group=4, dim=128, bt=1, seed=39, layers=1)
+    b.lens[1] = -1
+    b.table_h[0][700], b.table_h[3][9] = -1, b.pages
+    b.table = ints(b.table_h)
+    out = b.run(kvh, 40).cpu().numpy()
+    want = b.want(40)
+    assert b.status.tolist() == [BAD, BAD, 0, BAD] and (out[45:78] == -9).all()
+    assert np.array_equal(out[:45], want[:45]) and np.array_equal(out[78:], want[78:])
+
+
 def test_selection_refusals(kvh):
     shape = dict(news=[1, 6, 2], lens=[400, 500, 170], heads=1, dim=64, seed=35)
     b = Batch(**shape)
