@@ -287,7 +287,6 @@ struct Run {
   }
   __device__ __forceinline__ uint32_t count(const int32_t* refs, int lane) const {
     uint32_t n = 0;
-#pragma unroll 4
     for (int p = begin; p < stop; p += kWave) n += __popcll(__ballot(p + lane < stop && refs[p + lane] == 0));
     return n;
   }
@@ -463,7 +462,6 @@ __global__ __launch_bounds__(kScanThreads) void place_kernel(CompactParams a) {
   const Run run(r.pages);
   auto in_use = [&](int p) { return p + lane < run.stop && r.refs[p + lane] > 0; };
   uint32_t mine = 0;
-#pragma unroll 4
   for (int p = run.begin; p < run.stop; p += kWave) mine += __popcll(__ballot(in_use(p)));
   if (lane == 0) used_of[wave] = mine;
   __syncthreads();
@@ -471,7 +469,6 @@ __global__ __launch_bounds__(kScanThreads) void place_kernel(CompactParams a) {
   const int used = (int)row_sum(of);
   uint32_t before = row_sum(lane < wave ? of : 0);  // pages in use before the run's next ones
   uint32_t below = 0;
-#pragma unroll 4
   for (int p = run.begin; p < run.stop; p += kWave) below += __popcll(__ballot(in_use(p) && p + lane < used));
   if (lane == 0) below_of[wave] = below;
   __syncthreads();
