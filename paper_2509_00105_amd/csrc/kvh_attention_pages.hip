@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kFewThreads, 8 / kFewWaves) void pages_kernel(AttnP
   __syncthreads();
   for (int i = threadIdx.x; i < x.count; i += kFewThreads) {
     const int e = list[i], before = i > 0 ? list[i - 1] : -1;
-    if (e <= before || e > own)
+    if (e < 0 || e <= before || e > own)  // (what follows the end is anything: a negative entry may be larger than the one before)
       atomicMin(&entries, i);
     else
       pages[i] = table[e];
