@@ -232,6 +232,9 @@ __device__ __forceinline__ void pick(const Four& four, int n, int count, int fir
   for (int g = 0; g < GROUPS; ++g) any_open |= lds.open[g] == 1;
   high = wave_max(lane < W ? lds.high[team][lane] : 0) - 1;  // lane w has what wave w found
   uint32_t low = ~wave_max(lane < W ? lds.low[team][lane] : 0) + 1;
+  // Without a key of another sort than those two there is no range, and nothing to look for: high is then 0, or kAlways, and what is chosen in any case is all.  (With one, a key
+  // of 0 is further from low than high is, in numbers that wrap.)
+  open = open && high - 1 < kInfinite;
   uint32_t least = want == 0 ? kAlways - 1 : 0, equal = 0;  // keys above it are chosen, and the first `equal` ones of those that are it
 #pragma unroll 1
   while (any_open) {

@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 
 from test_gpu_pages_attention import Listed
+from test_gpu_pages_select import Batch as Choice
+from test_gpu_pages_select import ints
 from test_gpu_serving_attention import BAD
 
 torch = pytest.importorskip("torch")
@@ -48,3 +50,33 @@ def test_long_lists_past_their_end(kvh):
     b.lists[1, 1] = -1
     b.check(b.run(kvh))
     assert not b.status.any()
+
+
+# How the scores are laid out: in LDS, tokens by themselves, in pairs and in fours, and through memory, with picks of 8 and of 16 waves and of 4 that are many.
+LAYOUTS = [dict(news=[1, 1], lens=[300, 3300]), dict(news=[2, 3], lens=[400, 90], group=6), dict(news=[5, 8], lens=[900, 400], group=4),
+           dict(news=[1, 1], lens=[500, 90], bt=1), dict(news=[1, 2], lens=[9000, 500], bt=2, dim=64), dict(news=[1], lens=[9000], bt=1, dim=64, heads=1),
+           dict(news=[20, 5], lens=[1300, 700], group=3, bt=1, dim=64), dict(news=[260, 253], lens=[1100, 1201], group=4, bt=1, dim=64)]
+
+
+def spoil(b, keep):
+    """Table entries that are no pages, but for the places that keep(n) gives of a request with n pages."""
+    bad = [-1, b.pages, 1 << 30, -2 ** 31]
+    for r, n in enumerate(b.lens_h):
+        held = -(-n // b.bt)
+        stay = {j % held for j in keep(held)}
+        for j in range(held):
+            if j not in stay:
+                b.table_h[r][j] = bad[j % 4]
+    b.table = ints(b.table_h)
+
+
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+@pytest.mark.parametrize("keep", [(), (0, -1), (0,), (0, -1, 3), (5,), (2, 3, 4, -2)])
+def test_pages_that_are_none_are_not_chosen(kvh, layout, keep):
+    """All of a request's pages lie outside of the cache, or all but those that are chosen in any case, or a few others: what is left is listed, and -1."""
+    b = Choice(seed=50 + layout, layers=1, **LAYOUTS[layout])
+    spoil(b, lambda n: keep)
+    for count, first, last in ((2, 0, 1), (5, 1, 1), (4, 2, 2)) if len(b.q) < 100 else ((5, 1, 1),):
+        b.status.zero_()
+        b.check(kvh, count, first, last)
+        assert (b.status == BAD).all()
