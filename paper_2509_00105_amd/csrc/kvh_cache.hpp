@@ -155,8 +155,10 @@ __device__ __forceinline__ uint32_t wave_sum_to(uint32_t v, uint32_t& all) {
   return v + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
 }
 
-// The request that a row of the packed tensors belongs to; all lanes of a wave ask for the same row.  False where it is in none, or in one that is refused.
-__device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
+// The request that a row of the packed tensors belongs to, one that is not refused; all lanes of a wave ask for the same row.  False where there is none: the next row that
+// one has is `next` then, INT32_MAX if none has.
+__device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq, int& next) {
+  // As long as starts do not fall it is the last one whose start is not past the row.
   int32_t start, end, len;
   if (r.n <= kWave) {  // all of them at once: one trip to memory, not two
     start = INT32_MAX, end = len = 0;
@@ -165,7 +167,7 @@ __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane,
     b = below == 0 ? 0 : 63 - __builtin_clzll(below);
     start = __builtin_amdgcn_readlane(start, b), end = __builtin_amdgcn_readlane(end, b), len = __builtin_amdgcn_readlane(len, b);
   } else {
-    int first = 0, many = r.n;  // the last start that is not past the row is one of these
+    int first = 0, many = r.n;
     while (many > 1) {
       const int step = (many + kWave - 1) / kWave, at = lane * step;
       const uint64_t below = __ballot(at < many && r.starts[first + at] <= row);
@@ -177,7 +179,32 @@ __device__ __forceinline__ bool request_of(const Requests& r, int row, int lane,
     start = uniform(r.starts[b]), end = uniform(r.starts[b + 1]), len = uniform(r.lens[b]);
   }
   rq = Request{start, end - start, len, request_ok(r, start, end, len) && start <= row && row < end};
-  return rq.ok;
+  if (__builtin_expect(rq.ok, 1)) return true;
+  // It is refused, or the row is none's, or the start of a refused request behind the row's own has led astray: all are looked at.
+  uint32_t after = 0;  // the inverse of the least start past the row
+#pragma unroll 1
+  for (int b0 = 0; b0 < r.n; b0 += kWave) {
+    const int at = b0 + lane;
+    start = end = len = 0;
+    if (at < r.n) start = r.starts[at], end = r.starts[at + 1], len = r.lens[at];
+    const bool has = end > start && request_ok(r, start, end, len);
+    const uint64_t who = __ballot(has && start <= row && row < end);
+    if (who != 0) {
+      const int l = __builtin_ctzll(who);
+      b = b0 + l;
+      start = __builtin_amdgcn_readlane(start, l);
+      rq = Request{start, __builtin_amdgcn_readlane(end, l) - start, __builtin_amdgcn_readlane(len, l), true};
+      return true;
+    }
+    if (has && start > row) after = max(after, ~(uint32_t)start);
+  }
+  after = wave_max(after);
+  next = after == 0 ? INT32_MAX : (int)~after;
+  return false;
+}
+__device__ __forceinline__ bool request_of(const Requests& r, int row, int lane, int& b, Request& rq) {
+  int next;
+  return request_of(r, row, lane, b, rq, next);
 }
 
 // Says which requests are refused; the kernels, of THREADS threads a block, pass over them.

@@ -363,10 +363,10 @@ __global__ __launch_bounds__(kSelectThreads, 4) void select_kernel(SelectParams 
   const int past = row0 + TPT < a.req.n_tokens ? row0 + TPT : a.req.n_tokens;
   u32x4 raw = load_queries<D, TPT>(a, row0, past, head, 0);
   for (int row = row0; row < past;) {
-    int b;
+    int b, next;
     Request rq;
-    if (!request_of(a.req, row, lane, b, rq)) {
-      ++row;
+    if (!request_of(a.req, row, lane, b, rq, next)) {
+      row = next;
       continue;
     }
     const int stop = rq.start + rq.n < past ? rq.start + rq.n : past;  // the request's rows of this tile
@@ -479,10 +479,10 @@ __global__ __launch_bounds__(kBlockThreads) void score_many_kernel(SelectParams 
   const int past = row0 + kTokens < a.token0 + a.tokens ? row0 + kTokens : a.token0 + a.tokens;
   bool ready = false;  // the queries
   for (int row = row0; row < past;) {
-    int b;
+    int b, next;
     Request rq;
-    if (!request_of(a.req, row, lane, b, rq)) {
-      ++row;
+    if (!request_of(a.req, row, lane, b, rq, next)) {
+      row = next;
       continue;
     }
     const int begin = row, stop = rq.start + rq.n < past ? rq.start + rq.n : past;  // the request's rows of this tile

@@ -80,3 +80,59 @@ def test_pages_that_are_none_are_not_chosen(kvh, layout, keep):
         b.status.zero_()
         b.check(kvh, count, first, last)
         assert (b.status == BAD).all()
+
+
+# starts that fall, how many of the first rows belong to requests ahead of that, max_new
+FALLS = [([0, 3, -5, 5, 9], 3, 9), ([0, 2, 6, 0, 9], 6, 4), ([0, 3, 6, -2 ** 31, 9], 6, 9), ([0, 1, 2 ** 31 - 1, 2, 9], 1, 9)]
+
+
+def refused(starts, max_new, rows=9):
+    return [BAD if not 0 <= s <= e <= rows or e - s > max_new else 0 for s, e in zip(starts, starts[1:])]
+
+
+@pytest.mark.parametrize("more", [0, 100])
+@pytest.mark.parametrize("starts,rows,max_new", FALLS)
+@pytest.mark.parametrize("lens,bt", [([400, 310, 290, 333], 16), ([400, 310, 290, 333], 1), ([1100, 310, 290, 333], 1)])
+def test_selection_ahead_of_falling_starts(kvh, lens, bt, starts, rows, max_new, more):
+    """Requests that share no rows with others and lie ahead are what they are without those behind them."""
+    b = Choice([3, 3, 2, 1] + [0] * more, lens + [20] * more, heads=2, group=2, dim=64, bt=bt, seed=60, layers=1)
+    b.starts = ints(starts + [9] * more)
+    out = b.run(kvh, 7, max_new=max_new).cpu().numpy()
+    assert b.status.tolist() == refused(starts, max_new) + [0] * more
+    ahead = starts.index(rows)
+    b.starts_h, b.lens_h = starts[:ahead + 1], lens[:ahead]
+    assert np.array_equal(out[:rows], b.want(7)[:rows])
+
+
+@pytest.mark.parametrize("more", [0, 100])
+@pytest.mark.parametrize("starts,rows,max_new", FALLS)
+@pytest.mark.parametrize("most,count", [(5000, 300), (60, 4)])
+def test_attention_ahead_of_falling_starts(kvh, most, count, starts, rows, max_new, more):
+    """The same, lists shared by blocks and joined among them."""
+    ahead = starts.index(rows)
+    news = [e - s for s, e in zip(starts[:ahead], starts[1:])] + [9 - rows] + [0] * (3 - ahead + more)
+    b = Listed(news, [most, 40, 50, 60] + [20] * more, heads=2, group=4, dim=64, kind="16", dt="fp16", seed=61, layers=1).choose(count, 1)
+    want, lse = b.run(kvh, max_new=9), b.lse
+    assert not b.status.any()
+    b.starts = ints(starts + [9] * more)
+    out = b.run(kvh, max_new=max_new)
+    assert torch.equal(out[:rows], want[:rows]) and torch.equal(b.lse[:rows], lse[:rows])
+    assert b.status.tolist() == refused(starts, max_new) + [0] * more
+
+
+@pytest.mark.parametrize("longest,bt", [(300, 16), (1100, 1)])
+@pytest.mark.parametrize("group", [2, 7])
+def test_gaps_among_many_requests(kvh, group, longest, bt):
+    """Refused requests, one after the other and alone, among more than 64, where neighbouring tokens share products; rows behind the last one."""
+    n = 300
+    lens = [int(x) for x in np.random.default_rng(8).integers(3, 90, n)]
+    lens[200] = longest
+    b = Choice([3] * n, lens, heads=1, group=group, dim=64, bt=bt, seed=62, layers=1, behind=40)
+    gone = [0, 1, 2, 70, 71, 90, 150, *range(220, 260), 299]
+    b.lens[gone] = -1
+    out = b.run(kvh, 5).cpu().numpy()
+    assert b.status.tolist() == [BAD if r in gone else 0 for r in range(n)]
+    want = b.want(5)
+    for r in gone:
+        want[3 * r:3 * r + 3] = -9
+    assert np.array_equal(out, want)
