@@ -446,7 +446,8 @@ int kvh_attention(const kvh_cache* cache, int layer, const kvh_requests* request
  * Bounds: for each page, KV head and channel the lowest and the highest key, as int8 codes rounded outwards with one fp32 scale
  * per page and head.  With x the values of a 16-bit page (or the codes of an 8-bit one) over the page's tokens, a the largest |x| of the
  * head: lowest = floor(127 min x / a), highest = ceil(127 max x / a), scale = a / 127 times the page's K scale, rounded to fp32 each time; zeros
- * where a < 2^-100.  A page and head that holds an infinity or NaN (its K scale among that) has codes of zero and a scale of NaN. */
+ * where a < 2^-100.  A page and head that holds an infinity or NaN has codes of zero and a scale of NaN; one whose K scale is no finite number, or whose product with it is none,
+ * has a scale of NaN beside the codes that it has otherwise.  Both are chosen first. */
 typedef struct {
   int8_t* codes;  /* [layers][pages][heads][2][head_dim]: lowest, highest; 16-byte aligned, a page dense */
   float* scale;   /* [layers][pages][heads], heads dense */
@@ -472,8 +473,9 @@ int kvh_bound_keys(const kvh_cache* cache, const kvh_requests* requests, kvh_dty
  * pages_dev: int32 [n_tokens][heads][count], dense: logical pages, ascending, then -1.  first >= 0, last >= 1, first + last <= count <= 4096.
  * A page outside [0, pages) in the table is not chosen (status_dev).  Rows of refused requests, and rows of no request, are left as they are; a token at a
  * position below 0 gets -1 throughout.
- * workspace_dev: scores, 16-byte aligned, where there are few tokens or very many pages; kvh_select_workspace says how much serves best (0 where none is used; 64 MiB at
- * most, where a token's own scores do not take more).  With less the call takes the tokens in turns, or a slower way; KVH_E_SIZE where the table has room for more than 14000 pages and
+ * workspace_dev: scores, 16-byte aligned, where there are few tokens or very many pages; kvh_select_workspace says how much serves best whatever the number of query heads (64 MiB at
+ * most, where a token's own scores do not take more).  It does not know that number: 0 says that none is used, but with more than one query head a KV head a batch of many
+ * new tokens may use less than it says, or none.  With less the call takes the tokens in turns, or a slower way; KVH_E_SIZE where the table has room for more than 14220 pages and
  * the workspace does not hold one token's scores (4 heads table_pages bytes, table_pages rounded up to a multiple of 4).  It needs no preparation and keeps nothing that another call reads. */
 size_t kvh_select_workspace(int n_requests, int n_tokens, int heads, int table_pages);
 int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* requests, kvh_dtype dt, const kvh_rows* q, int q_heads, int first, int last,
@@ -482,7 +484,9 @@ int kvh_select_pages(const kvh_bounds* bounds, int layer, const kvh_requests* re
 /* Attention of the new tokens over the pages listed for each of them and each KV head: kvh_attention with causal set, where query i of head h sees only tokens on pages
  * of its list, up to its own position.  pages_dev: int32 [n_tokens][heads][count], dense, count 1 .. 4096: logical pages, ascending, -1 past the last
  * one; a list ends at its first negative entry.  An entry that is not larger than the one before it, or past the token's own page, ends its list too, with status_dev.
+ * What a list holds past its end is of no account, and is not looked up.
  * Types, precision, lse, refusals, infinities and NaN: as kvh_attention.  count * block_tokens is at most 2^31 - 128.
+ * Speed: few tokens' lists are cut by what `count` has room for, not by what they hold: with lists much shorter than count some blocks find nothing to do, and the parts are joined all the same.
  * workspace_dev: partial results where few tokens read many pages, as for kvh_attention; kvh_attention_pages_workspace says how much serves best, less or none is
  * slower where it is used. */
 size_t kvh_attention_pages_workspace(int n_tokens, int heads, int q_heads, int head_dim, int block_tokens, int count);
@@ -522,6 +526,7 @@ typedef struct {
  * call in place of what they held before it.  A page that is given up and one that is handed out may be the same: the old rows are of no use afterwards.
  * Refused rows become empty (lens_out 0): KVH_DEV_BAD_REQUEST for parents[b] >= n_requests, grow[b] < 0, a parent's length below 0 or past the
  * table, an entry of its outside [0, pages), a new length past the table or 2^31 - 128; KVH_DEV_NO_PAGES where the fresh pages that rows up to this one need are more than there are.
+ * Such a row's tokens are lost, as its pages are given back at once: a program that would have it wait asks for no more than is free (refs of 0), for instance by a grow of 0.
  * workspace_dev: kvh_fork_workspace bytes, 4-byte aligned; KVH_E_SIZE with less. */
 size_t kvh_fork_workspace(int n_requests, int pages);
 int kvh_fork(const kvh_cache* cache, const kvh_bounds* bounds, const kvh_rows_of_pages* rows, const int32_t* parents_dev, const int32_t* grow_dev,

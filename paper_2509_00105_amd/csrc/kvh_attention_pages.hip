@@ -4,8 +4,8 @@
 // table and kept in LDS, its length ends with the last listed page, or at the token's own position where that page is the last.  The query heads of the KV head
 // are the rows, 16 a tile.
 //
-// A token's pages are read once for its own KV head, 2 D bytes of each token at a time (of 16 bits), which memory bounds: 64 requests, 64 pages of 16 each for 8 heads of 128, bf16: 54 us =
-// 4.8 TB/s (over all 4096 tokens kvh_attention takes 186), int8: 36 us.  Where tokens of a request read the same pages, an XCD's 4 MiB hold part of a head's: 512 tokens after
+// A token's pages are read once for its own KV head, 2 D bytes of each token at a time (of 16 bits), which memory bounds: 64 requests, 64 pages of 16 each for 8 heads of 128, bf16: 53 us =
+// 4.8 TB/s (over all 4096 tokens kvh_attention takes 186), int8 and e4m3: 34 us.  Where tokens of a request read the same pages, an XCD's 4 MiB hold part of a head's: 512 tokens after
 // 32768, 64 pages each at random, int8: 107 us, in which 1.07 GB are read through the caches and 0.53 come from behind them (kvh_attention: 396).  The tile has rows for other
 // tokens, which have lists of their own: where neighbours choose the same pages, those are read again for each.
 #include "kvh_attention_few.hpp"

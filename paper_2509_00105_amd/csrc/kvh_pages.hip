@@ -3,8 +3,9 @@
 // Contents move by pairs of pages, 16 KiB a block; memory bounds that.  Who holds what is integer work on the table and the counts, which is bound by the trips to
 // memory that wait for each other: a block plans, with the counts in LDS where they fit, and a second launch writes the rows and copies at the same
 // time.  Counts change by atomic additions of whole numbers, whose order is of no account.
-// Measured, calls among others: 512 pages of 8 layers (268 MB) copied 109 us = 4.9 TB/s (a plain copy of 4 GiB reaches 5.5); 3 pages of 32 layers, int8: 4.6 us; fork, 64 rows of 4096 tokens
-// (lognormal) that grow by one: 14.5 us (plan 8 to 12), 16 requests of 4 beams: 14; compact, 450 pages of 8 layers: 89 us = 5.3 TB/s, 1024 pages of one layer: 7.2.
+// Measured, calls among others: 512 pages of 8 layers (268 MB) copied 103 us = 5.2 TB/s (a plain copy of 4 GiB reaches 5.5); 3 pages of 32 layers, int8: 4.4 us; fork, 64 rows of 4096 tokens
+// (lognormal) that grow by one: 14.9 us (plan 8 to 12), 16 requests of 4 beams: 13.2; compact, 450 pages of 8 layers: 84.5 us = 5.6 TB/s, 1024 pages of one layer: 6.8.  One block walks
+// the counts, so large pools take their time: 64 rows that grow in a pool of 50000 pages 32 us, of 100000 49, of 200000 127; compact, one small layer, 15000 pages 30, 50000 72, 100000 132, 200000 230.
 #include "kvh_cache.hpp"
 
 #include <algorithm>
@@ -102,11 +103,11 @@ __device__ __forceinline__ void copy_many(const CopyParams& a, const int32_t* ma
   }
 }
 // Blocks that such a launch has for them at most: enough to fill the chip, and not one for each copy that there might be.  Fork, where most rows copy nothing (32
-// layers, 64 rows: 9.5 us, 10.8 with 16384; 256 rows: 17.8 and 20.5, one for each 25.6); compact, where many pages move (8 layers of 450 pages: 102 us,
-// 104 with 4096, 111 with 2048).
+// layers, 64 rows: 9.8 us, 10.2 with 16384; 256 rows: 17.8 and 20.4); compact, where many pages move (8 layers of 450 pages: 84.5 us, 90.5 with 4096, 96
+// with 2048).
 constexpr int64_t kForkBlocks = 4096, kCompactBlocks = 16384;
 
-// Bytes of K and V from which on copies pass by the caches: 512 pages of 8 layers 108.7 us so, 112.9 through them; compact, 450 pages of 8 layers, 89 and 100.  Fork copies
+// Bytes of K and V from which on copies pass by the caches: 512 pages of 8 layers 4 us less than through them, of 113; compact, 450 pages of 8 layers, 11 of 100.  Fork copies
 // a page that is appended to next.
 constexpr int64_t kPastBytes = 16 << 20;
 
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(kBlockThreads) void renumber_kernel(CompactParams a
   if (bad && r.status != nullptr) r.status[b] = KVH_DEV_BAD_REQUEST;
 }
 
-// One block plans by itself where the counts and rows fit into its LDS and the table is no larger than this: 64 rows, 14895 pages 14.5 us, in three launches 39.
+// One block plans by itself where the counts and rows fit into its LDS and the table has no more entries than this, whatever they hold: 64 rows, 14895 pages 14.5 us, in three launches 39.
 constexpr int64_t kPlanLds = 63 << 10, kPlanEntries = 512 << 10;
 
 // ---- arguments ----------------------------------------------------------------------------------------------------

@@ -8,10 +8,10 @@
 // the scores in LDS as numbers in their order, and picks the best by counting them in bins.  Where there are too few tokens to fill the chip, or too many pages for LDS,
 // the scores go through memory, from one grid that is as wide as the pages to one that picks.
 //
-// What bounds it: the bounds' bytes (256 of a page and head) come at 4 TB/s where many tokens have many pages (64 of 1000 pages: 32 us); below that, trips to memory that wait for
-// each other - request, table, bounds - and for one token the picking.  A single block takes in 13 bytes a clock, so that one token of 1000 pages took 16 us in one launch and takes 9.3 in two.
-// Measured, 8 KV heads of 128, 32 query heads, calls among others: 64 requests of 4096 tokens (lognormal, pages of 16) 19.5 us (scores 13.8, picking 5.3), one of 131072 16 us (6.2
-// and 8.6), 64 of 64 pages 6, 64 of 256 pages 13, 512 new tokens of a request of 2080 pages 71 (48 and 22).
+// What bounds it: the bounds' bytes (256 of a page and head) come at 3.2 TB/s where many tokens have many pages (64 of 1000 pages: 41 us); below that, trips to memory that wait for
+// each other - request, table, bounds - and for one token the picking.  A single block takes in 13 bytes a clock, so that one token of 1000 pages took 16 us in one launch and takes 10.5 in two.
+// Measured, 8 KV heads of 128, 32 query heads, calls among others with other inputs in turn (in brackets scores and picking, each by itself in a trace): 64 requests of 4096 tokens (lognormal, pages of
+// 16) 19.3 us (13.0 and 5.2), one of 131072 16 us (5.8 and 8.8), 16 of 64 pages for each of 64 9, of 256 pages 12.7, 512 new tokens of a request of 2080 pages 62 (44 and 22).
 #include "kvh_bounds.hpp"
 
 #include <algorithm>
@@ -560,9 +560,9 @@ __global__ __launch_bounds__(W * kWave) void pick_kernel(SelectParams a) {
 // ---- launch -------------------------------------------------------------------------------------------------------
 constexpr int kMostListed = 4096;
 constexpr int kLds = 64 << 10;  // of a block
-// Tokens and heads below which scores of more pages than kManyPages go through memory: 64 requests of 4096 (lognormal) 19.1 us so, 20.6 in one launch (the longest has 1364 pages); one of 1000
-// pages 9.3 and 16; 64 of 512 pages 21.9 and 20.1, of 1000 32.3 and 32.8.  A table of 256 pages or less: 64 requests 13 us in one launch, one request 8.5.
-// More tokens and heads, where neighbouring tokens share products: 512 of 2080 pages 71 us through memory and 83 in one launch, of 500 pages 40 and 31.
+// Tokens and heads below which scores of more pages than kManyPages go through memory: 64 requests of 4096 (lognormal) 19.3 us so, 20.4 in one launch (the longest has 1364 pages); one of 1000
+// pages 10.5 and 16; where 64 are of one length the other way is the faster one, of 512 pages 23.5 and 19.1, of 1000 41 and 36.  A table of 256 pages: 64 requests 15.7 and 12.7, one request 10.5 and 8.4.
+// More tokens and heads, where neighbouring tokens share products: 512 of 2080 pages 62 us through memory and 79 in one launch, of 500 pages 28.6 and 30.4.
 constexpr int64_t kFewUnits = 1024, kManyPages = 256, kShared = 1024;
 
 int64_t pitch_of(int table_pages) { return ((int64_t)table_pages + 3) & ~(int64_t)3; }
@@ -595,7 +595,7 @@ void launch_select(const SelectParams& a, int tokens, hipStream_t stream) {
 
 // Picks from which on a team has 4 waves and not 8, of which more wait at a time: 4096 of 2080 keys 22 us, 32 with 8; 512 of them 7.2 and 6.3.
 constexpr unsigned kManyPicks = 1024;
-// Products of a block that scores neighbouring tokens: 512 tokens of 2080 pages 48 us, with 2 65, with 8 56; 64 tokens 12.5, 11 and 19.
+// Products of a block that scores neighbouring tokens (the kernel alone, one after the other): 512 tokens of 2080 pages 48 us, with 2 65, with 8 56; 64 tokens 12.5, 11 and 19.
 constexpr int kMany = 4;
 
 template <int DT, int D>

@@ -136,3 +136,15 @@ def test_gaps_among_many_requests(kvh, group, longest, bt):
     for r in gone:
         want[3 * r:3 * r + 3] = -9
     assert np.array_equal(out, want)
+
+
+def test_widest_table_without_a_workspace(kvh):
+    """14220 pages are the most whose scores a block keeps by itself; a table for one more needs the workspace."""
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    b = Choice([1], [14220], heads=1, group=4, dim=64, bt=1, seed=63, layers=1)
+    b.check(kvh, 30, workspace=none)
+    b = Choice([1], [14221], heads=1, group=4, dim=64, bt=1, seed=64, layers=1)
+    with pytest.raises(kvh.KVHError) as e:
+        b.run(kvh, 30, workspace=none)
+    assert e.value.status == -4
+    b.check(kvh, 30)
